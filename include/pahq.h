@@ -435,6 +435,70 @@ enum { PAHQ_NOALLOC_MAX_ROWS = 32768 };
 int pahq_quantize_rows_noalloc(void* hip_stream, const float* x, int32_t rows, int32_t cols, uint8_t* codes,
                                float* scales);
 
+/* ---- operators on device tensors -------------------------------------------------
+ * Parts of a layer as functions, for programs that run their own loop: like pahq_quantize_rows_noalloc they need no model,
+ * take device pointers and a stream, allocate nothing, keep nothing between calls, enqueue and do not wait.  They can be
+ * recorded into a HIP graph, and any number of calls may be in flight, on one stream or several, as long as one does not
+ * write what another uses.  The device that owns the pointers and the stream must be the current one.  Arguments the host
+ * can see are checked before anything is enqueued: PAHQ_EINVAL (null or misaligned pointer, size or stride out of range, a
+ * result that shares memory with an operand unless said otherwise), PAHQ_ETOOBIG (more than a launch counts).  A size
+ * of zero rows (columns, tokens, heads) does nothing and looks at no pointer.  Strides (ld) count elements; tensors need the
+ * alignment of their element only. */
+enum { PAHQ_F32 = 0, PAHQ_BF16 = 1, PAHQ_F16 = 2 };
+
+/* Matrices in 4 microscaled bits (the OCP microscaling format MXFP4): elements E2M1 (0 0.5 1 1.5 2 3 4 6 and their
+ * negatives), one power-of-two scale per block of 32 neighbouring elements of a row:
+ *     top = max |x| of the block;  s = max(floor(log2 top) - 2, -127), 0 for a block of zeros
+ *     code = E2M1 value nearest to x * 2^-s, ties to the even code, |.| > 6 saturating; the sign of zero is kept
+ *     scale byte = s + 127;  a block with an infinity or NaN gets scale byte 255 (NaN) and codes 0: all of it reads as NaN
+ * A matrix [rows][cols] is held as rows of K = cols rounded up to 256 elements, padded with codes 0 (and blocks of scale
+ * byte 127):
+ *     codes   [rows][K / 2] bytes, element 2 i of a row in the low half of byte i; 16-byte aligned
+ *     scales  [rows][K / 32] bytes; 8-byte aligned
+ * pahq_mx4_bytes gives the sizes of the two.
+ * pahq_mx4_quantize: by = PAHQ_MX4_BY_ROWS: x [rows][cols], row stride ld >= cols.  PAHQ_MX4_BY_COLUMNS: x [cols][rows], row
+ * stride ld >= rows, so that the blocks run down the columns of x: a weight master [k][n] becomes the [n][k] the product takes.
+ * pahq_mx4_dequantize: the values; exact in PAHQ_F32 and PAHQ_BF16, rounded once in PAHQ_F16.
+ * pahq_mx4_gemm: out[i][j] = sum_k a[i][k] w[j][k] (+ bias[j]) (+ residual[i][j]); a [m][k], w [n][k] in this format, bias
+ * fp32 [n] or NULL, residual of out's type or NULL (it may be out itself, with the same stride).  Sums in fp32, one rounding
+ * to out's type.  The order of a sum depends on the sizes alone: the same call gives the same bits. */
+enum { PAHQ_MX4_BY_ROWS = 0, PAHQ_MX4_BY_COLUMNS = 1 };
+int pahq_mx4_bytes(int32_t rows, int32_t cols, size_t* codes, size_t* scales);
+int pahq_mx4_quantize(void* hip_stream, const void* x, int32_t dtype, int32_t rows, int32_t cols, int64_t ld, int32_t by,
+                      uint8_t* codes, uint8_t* scales);
+int pahq_mx4_dequantize(void* hip_stream, const uint8_t* codes, const uint8_t* scales, int32_t rows, int32_t cols, void* out,
+                        int32_t dtype, int64_t ld);
+int pahq_mx4_gemm(void* hip_stream, const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes,
+                  const uint8_t* w_scales, int32_t m, int32_t n, int32_t k, const float* bias, const void* residual,
+                  int64_t ld_residual, void* out, int32_t dtype, int64_t ld_out);
+
+/* Rotary positions.  The first rot_dim elements of every head form pairs (a, b): element i and i + rot_dim / 2
+ * (PAHQ_ROTARY_HALF) or elements 2 i and 2 i + 1 (PAHQ_ROTARY_INTERLEAVED), i < rot_dim / 2; the rest of the head is copied.
+ *     phi = position * f_i;   a' = magnitude * (a cos phi - b sin phi),  b' = magnitude * (a sin phi + b cos phi)
+ * inverse = 1 turns by -phi: the gradient with respect to x, given that of out.
+ * x, out: [tokens][heads][d_head] with strides of their own for tokens and heads, elements of a head contiguous.  In out either
+ * may be the outer one, and no two elements share a place; x may repeat rows (stride 0).  out may be x itself with the same
+ * strides.  positions: device int64 [tokens], any values, not checked.
+ * Arithmetic in fp32, one rounding to the type.
+ * table: device uint64 [rot_dim / 2], from pahq_rotary_table, which fills HOST memory: f_i / (2 pi) modulo 1 in units of
+ * 2^-64, so the angle of a far position is as good as that of a near one.  rot_dim even, 2 .. PAHQ_ROTARY_MAX_DIM.
+ *     PAHQ_ROTARY_PLAIN   f_i = theta^(-2 i / rot_dim)
+ *     PAHQ_ROTARY_LINEAR  f_i / factor: positions squeezed into the trained range
+ *     PAHQ_ROTARY_BASE    theta * factor^(rot_dim / (rot_dim - 2)) in place of theta: the slowest pair is stretched by factor,
+ *                         the fastest not at all (rot_dim >= 4)
+ *     PAHQ_ROTARY_BANDS   by how often a pair turns over the trained range of `original` positions, r = original f_i / (2 pi):
+ *                         f_i from turns_hi turns on, f_i / factor up to turns_lo, in between f_i (g + (1 - g) / factor) with
+ *                         g = (r - turns_lo) / (turns_hi - turns_lo)
+ * factor >= 1; arguments a form does not use are ignored. */
+enum { PAHQ_ROTARY_HALF = 0, PAHQ_ROTARY_INTERLEAVED = 1 };
+enum { PAHQ_ROTARY_PLAIN = 0, PAHQ_ROTARY_LINEAR = 1, PAHQ_ROTARY_BASE = 2, PAHQ_ROTARY_BANDS = 3 };
+enum { PAHQ_ROTARY_MAX_DIM = 1024 };
+int pahq_rotary_table(int32_t rot_dim, double theta, int32_t scaling, double factor, double original, double turns_lo,
+                      double turns_hi, uint64_t* table);
+int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32_t tokens, int32_t heads, int32_t d_head, int64_t x_token,
+                int64_t x_head, const int64_t* positions, const uint64_t* table, int32_t rot_dim, int32_t layout,
+                float magnitude, int32_t inverse, void* out, int64_t out_token, int64_t out_head);
+
 const char* pahq_strerror(int code);
 void pahq_free(pahq_model*);            /* frees host state only; the workspace stays the caller's */
 

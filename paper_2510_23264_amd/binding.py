@@ -106,6 +106,13 @@ def lib():
             "pahq_set_profiling_sample": [C.c_void_p, C.c_uint32, C.c_int32],
             "pahq_get_profile": [C.c_void_p, C.POINTER(KernelStat)],
             "pahq_quantize_rows_noalloc": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p],
+            "pahq_mx4_bytes": [C.c_int32, C.c_int32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+            "pahq_mx4_quantize": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p],
+            "pahq_mx4_dequantize": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int64],
+            "pahq_mx4_gemm": [C.c_void_p] * 5 + [C.c_int32] * 3 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int64],
+            "pahq_rotary_table": [C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4 + [C.POINTER(C.c_uint64)],
+            "pahq_rotary": [C.c_void_p, C.c_void_p] + [C.c_int32] * 4 + [C.c_int64] * 2 + [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                            C.c_float, C.c_int32, C.c_void_p, C.c_int64, C.c_int64],
             "pahq_compare_encoders": [C.c_void_p, C.c_void_p, C.POINTER(C.c_uint64), C.POINTER(C.c_uint32)],
             "pahq_measure_ceilings": [C.c_void_p, C.c_void_p, C.c_size_t, C.POINTER(C.c_double), C.POINTER(C.c_double)],
         }

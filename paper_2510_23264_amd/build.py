@@ -6,7 +6,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpahq.so")
-SOURCES = ["rows.hip", "gemm.hip", "oproj.hip", "attn_kl.hip", "engine.hip", "api.hip", "ceilings.hip", "noalloc.hip"]
+SOURCES = ["rows.hip", "gemm.hip", "oproj.hip", "attn_kl.hip", "engine.hip", "api.hip", "ceilings.hip", "noalloc.hip", "mx4.hip",
+           "rotary.hip"]
 # -ffp-contract=off: a product and a sum are rounded separately unless the source says fmaf.  The same
 # expression (a norm's x * rstd * gain + offset, a GEMM epilogue's acc * scale + bias) is compiled into
 # several kernels -- cache passes and candidate passes take different ones -- and results that must agree

@@ -1,0 +1,64 @@
+// What the operators on device tensors share: element types, loads and stores of eight neighbouring elements at any
+// alignment of the element, and the host's check of memory that two operands share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+#include "../../include/pahq.h"
+
+namespace pahq {
+
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+inline int dtype_bytes(int dtype) { return dtype == PAHQ_F32 ? 4 : dtype == PAHQ_BF16 || dtype == PAHQ_F16 ? 2 : 0; }
+inline bool overlap(const void* p, size_t pn, const void* q, size_t qn) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return a < b + qn && b < a + pn;
+}
+
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(bf16_t x) { return (float)x; }
+__device__ __forceinline__ float as_float(f16_t x) { return (float)x; }
+// round to nearest, ties to even
+template <typename T> __device__ __forceinline__ T from_float(float x) { return (T)x; }
+
+// N elements of an array that is aligned to its element only: one load or store of N * sizeof(T) bytes where the hardware
+// has one (global memory takes any alignment).
+template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Pack { T v[N]; };
+
+// elements [0, 8) of p that exist (left of them), the rest zero
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int left, float* v) {
+  constexpr int N = 16 / sizeof(T);
+  if (left >= 8) {
+#pragma unroll
+    for (int h = 0; h < 8 / N; h++) {
+      const Pack<T, N> q = *(const Pack<T, N>*)(p + h * N);
+#pragma unroll
+      for (int j = 0; j < N; j++) v[h * N + j] = as_float(q.v[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = j < left ? as_float(p[j]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int left, const float* v) {
+  constexpr int N = 16 / sizeof(T);
+  if (left >= 8) {
+#pragma unroll
+    for (int h = 0; h < 8 / N; h++) {
+      Pack<T, N> q;
+#pragma unroll
+      for (int j = 0; j < N; j++) q.v[j] = from_float<T>(v[h * N + j]);
+      *(Pack<T, N>*)(p + h * N) = q;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+      if (j < left) p[j] = from_float<T>(v[j]);
+  }
+}
+
+}  // namespace pahq

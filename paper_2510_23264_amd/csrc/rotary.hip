@@ -1,0 +1,150 @@
+// Rotary positions as an operator on device tensors: pairs of elements of every head turn by an angle that grows with the
+// token's position (the layouts, the stretched frequencies and the definition are in include/pahq.h).
+//
+// The angle.  A frequency is kept as the fraction of a turn it advances in one position, in 64 binary digits, so position *
+// frequency modulo one turn is one 64-bit integer product, exact at every position; binary32 angles are off by more
+// than a hundredth of a radian from position 2^18 on.  The quarter turns come off as the product's two top digits, so
+// that what is left, at most an eighth of a turn, loses no more than 2^-25 of that when it becomes a float.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include "../../include/pahq.h"
+#include "device_tensor.h"
+
+namespace pahq {
+
+struct RotaryArgs {
+  long long x_token, x_head, o_token, o_head;       // strides in elements
+  const long long* positions;
+  const unsigned long long* table;
+  int tokens, heads, d, rot, per_group, copy;       // per_group: tokens of a workgroup; copy: the rest of the head goes along
+  float magnitude, direction;
+};
+
+// A workgroup takes a few neighbouring tokens: first their cosines and sines into LDS, shared by all heads, then the heads,
+// V elements of a pair's two sides a thread (V = 1: any alignment and any number of pairs).
+template <typename T, int V, bool HALF>
+__global__ __launch_bounds__(256) void rotary_k(const T* x, T* out, RotaryArgs q) {
+  extern __shared__ float2 turn[];                  // [per_group][rot / 2]
+  const int half = q.rot / 2, t0 = blockIdx.x * q.per_group, nt = min(q.per_group, q.tokens - t0);
+  for (int e = threadIdx.x; e < nt * half; e += 256) {
+    const int t = e / half, i = e - t * half;
+    const unsigned long long phase = (unsigned long long)q.positions[t0 + t] * q.table[i] + (1ull << 61);
+    const int quarter = (int)(phase >> 62);
+    const int left = (int)(((long long)(phase << 2) >> 32) ^ 0x80000000ll);       // in 2^-34 turns, from -1/8 on
+    float s, c;
+    sincospif((float)left * 1.1641532182693481e-10f, &s, &c);                     // 2^-33: half turns
+    const float cq = quarter & 1 ? s : c, sq = quarter & 1 ? c : s;
+    turn[e] = make_float2((quarter == 1 || quarter == 2 ? -cq : cq) * q.magnitude, (quarter >= 2 ? -sq : sq) * q.magnitude * q.direction);
+  }
+  __syncthreads();
+  // items of a head: groups of V pairs, then the elements behind the rotated part, V at a time
+  const int pairs = half / V, rest = q.copy ? (q.d - q.rot) / V : 0, items = pairs + rest;
+  for (int e = threadIdx.x; e < nt * q.heads * items; e += 256) {
+    const int h0 = e / items, i = e - h0 * items, t = h0 / q.heads, h = h0 - t * q.heads;
+    const T* p = x + (t0 + t) * q.x_token + h * q.x_head;
+    T* o = out + (t0 + t) * q.o_token + h * q.o_head;
+    if (i >= pairs) {
+      const int at = q.rot + (i - pairs) * V;
+      *(Pack<T, V>*)(o + at) = *(const Pack<T, V>*)(p + at);
+      continue;
+    }
+    const float2* cs = turn + t * half + i * V;
+    Pack<T, V> a, b;
+    const int ia = HALF ? i * V : 2 * i * V, ib = HALF ? half + i * V : 2 * i * V + V;
+    a = *(const Pack<T, V>*)(p + ia);
+    b = *(const Pack<T, V>*)(p + ib);
+#pragma unroll
+    for (int j = 0; j < V; j++) {
+      // half: a holds the first sides of V pairs and b their second sides; interleaved: the 2 V elements of V pairs in turn
+      T& u = HALF ? a.v[j] : (2 * j < V ? a.v[2 * j % V] : b.v[2 * j % V]);
+      T& w = HALF ? b.v[j] : V == 1 ? b.v[0] : (2 * j < V ? a.v[(2 * j + 1) % V] : b.v[(2 * j + 1) % V]);
+      const float f = as_float(u), g = as_float(w);
+      u = from_float<T>(f * cs[j].x - g * cs[j].y);
+      w = from_float<T>(f * cs[j].y + g * cs[j].x);
+    }
+    *(Pack<T, V>*)(o + ia) = a;
+    *(Pack<T, V>*)(o + ib) = b;
+  }
+}
+
+namespace {
+template <typename T>
+int rotary_as(hipStream_t st, const T* x, T* out, RotaryArgs q, int layout) {
+  constexpr int V = 16 / sizeof(T);
+  // 16 bytes a thread need whole groups of pairs on either side and behind them
+  const bool wide = (q.rot / 2) % V == 0 && (q.d - q.rot) % V == 0;
+  const int half = q.rot / 2;
+  q.per_group = max(1, min(min(2048 / half, 8), q.tokens));
+  const dim3 grid((q.tokens + q.per_group - 1) / q.per_group);
+  const size_t lds = (size_t)q.per_group * half * sizeof(float2);
+#define ROT(V_, HALF_) hipLaunchKernelGGL((rotary_k<T, V_, HALF_>), grid, dim3(256), lds, st, x, out, q)
+  if (layout == PAHQ_ROTARY_HALF) { if (wide) ROT(V, true); else ROT(1, true); }
+  else { if (wide) ROT(V, false); else ROT(1, false); }
+#undef ROT
+  return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
+}
+// [tokens][heads][d] in either order of the first two, no two elements in one place; extent in elements
+bool strides_ok(long long tokens, long long heads, long long d, long long st, long long sh, long long* extent) {
+  if (st < 0 || sh < 0) return false;
+  const bool rows = (heads == 1 || sh >= d) && (tokens == 1 || st >= (heads - 1) * sh + d);
+  const bool planes = (tokens == 1 || st >= d) && (heads == 1 || sh >= (tokens - 1) * st + d);
+  *extent = (tokens - 1) * st + (heads - 1) * sh + d;
+  return rows || planes;
+}
+}  // namespace
+
+}  // namespace pahq
+
+using namespace pahq;
+
+extern "C" int pahq_rotary_table(int32_t rot_dim, double theta, int32_t scaling, double factor, double original, double turns_lo, double turns_hi,
+                                 uint64_t* table) {
+  if (rot_dim < 2 || (rot_dim & 1) || rot_dim > PAHQ_ROTARY_MAX_DIM || !table) return PAHQ_EINVAL;
+  if (!(theta > 0.0) || !isfinite(theta) || scaling < PAHQ_ROTARY_PLAIN || scaling > PAHQ_ROTARY_BANDS) return PAHQ_EINVAL;
+  if (scaling != PAHQ_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return PAHQ_EINVAL;
+  if (scaling == PAHQ_ROTARY_BASE && rot_dim < 4) return PAHQ_EINVAL;
+  if (scaling == PAHQ_ROTARY_BANDS && (!(original > 0.0) || !isfinite(original) || !(turns_lo >= 0.0) || !(turns_hi > turns_lo) || !isfinite(turns_hi))) return PAHQ_EINVAL;
+  const long double tau = 6.283185307179586476925286766559005768L;
+  long double base = theta;
+  if (scaling == PAHQ_ROTARY_BASE) base *= powl(factor, (long double)rot_dim / (rot_dim - 2));
+  for (int i = 0; i < rot_dim / 2; i++) {
+    long double f = powl(base, -2.0L * i / rot_dim) / tau;             // turns a position
+    if (scaling == PAHQ_ROTARY_LINEAR) f /= factor;
+    if (scaling == PAHQ_ROTARY_BANDS) {
+      const long double g = fminl(1.0L, fmaxl(0.0L, (f * original - turns_lo) / (turns_hi - turns_lo)));
+      f *= g + (1.0L - g) / factor;
+    }
+    if (!isfinite(f)) return PAHQ_EINVAL;
+    // whole turns drop out; 2^64 itself (a fraction that rounds up to one) is no turn
+    const long double scaled = roundl((f - floorl(f)) * 18446744073709551616.0L);
+    table[i] = scaled >= 18446744073709551616.0L ? 0ull : (uint64_t)scaled;
+  }
+  return PAHQ_OK;
+}
+
+extern "C" int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32_t tokens, int32_t heads, int32_t d_head, int64_t x_token, int64_t x_head,
+                           const int64_t* positions, const uint64_t* table, int32_t rot_dim, int32_t layout, float magnitude, int32_t inverse, void* out,
+                           int64_t out_token, int64_t out_head) {
+  const int eb = dtype_bytes(dtype);
+  if (tokens < 0 || heads < 0 || d_head < 1 || !eb || rot_dim < 2 || (rot_dim & 1) || rot_dim > d_head || rot_dim > PAHQ_ROTARY_MAX_DIM) return PAHQ_EINVAL;
+  if ((layout != PAHQ_ROTARY_HALF && layout != PAHQ_ROTARY_INTERLEAVED) || (inverse != 0 && inverse != 1)) return PAHQ_EINVAL;
+  if (tokens == 0 || heads == 0) return PAHQ_OK;
+  if (!x || !out || !positions || !table || (uintptr_t)x % eb || (uintptr_t)out % eb || (uintptr_t)positions % 8 || (uintptr_t)table % 8) return PAHQ_EINVAL;
+  // a workgroup counts the elements of its (at most eight) tokens in 32 bits
+  if ((int64_t)heads * d_head > (1 << 27)) return PAHQ_ETOOBIG;
+  long long xn, on;
+  if (x_token < 0 || x_head < 0 || !strides_ok(tokens, heads, d_head, out_token, out_head, &on)) return PAHQ_EINVAL;
+  xn = (tokens - 1ll) * x_token + (heads - 1ll) * x_head + d_head;      // only read: rows may share memory
+  const bool in_place = x == out && x_token == out_token && x_head == out_head;
+  if (!in_place && overlap(x, (size_t)xn * eb, out, (size_t)on * eb)) return PAHQ_EINVAL;
+  if (overlap(out, (size_t)on * eb, positions, (size_t)tokens * 8) || overlap(out, (size_t)on * eb, table, (size_t)rot_dim * 4)) return PAHQ_EINVAL;
+  hipStream_t st = (hipStream_t)hip_stream;
+  RotaryArgs q = {x_token, x_head, out_token, out_head, (const long long*)positions, (const unsigned long long*)table, tokens, heads, d_head, rot_dim, 1,
+                  !in_place, magnitude, inverse ? -1.f : 1.f};
+  switch (dtype) {
+    case PAHQ_F32: return rotary_as(st, (const float*)x, (float*)out, q, layout);
+    case PAHQ_BF16: return rotary_as(st, (const bf16_t*)x, (bf16_t*)out, q, layout);
+    default: return rotary_as(st, (const f16_t*)x, (f16_t*)out, q, layout);
+  }
+}

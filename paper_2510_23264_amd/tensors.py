@@ -1,0 +1,207 @@
+"""The library's operators on device tensors (include/pahq.h, the section of that name) with torch tensors: matrices
+in 4 microscaled bits and their product, and rotary positions.
+
+Every call enqueues on the current stream of its tensors' device (whichever device is current) and does not wait.  Results are
+new tensors unless `out` is given.  Strided tensors are taken as they are where the C functions can walk them and refused
+otherwise; nothing is copied behind the caller's back.  Arguments that do not fit raise ValueError, a refusal of the
+library raises PahqError."""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from .binding import lib, _chk
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_SCALING = {"none": 0, "linear": 1, "base": 2, "bands": 3}
+_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _call(name, device, *args):
+    """One library call on the current stream of `device`, with that device current."""
+    fn = getattr(lib(), name)
+    if device.index == torch.cuda.current_device():
+        _chk(fn(torch.cuda.current_stream(device).cuda_stream, *args), name)
+    else:
+        with torch.cuda.device(device):
+            _chk(fn(torch.cuda.current_stream(device).cuda_stream, *args), name)
+
+
+def _tracked(*tensors):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _row_stride(t):
+    """Elements from row to row of a matrix whose rows are contiguous; None if they are not.  Of a single row or column torch
+    reports any stride."""
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        return None
+    if rows <= 1:
+        return max(cols, 1)
+    return t.stride(0) if t.stride(0) >= cols else None
+
+
+class Mx4:
+    """A matrix [rows][cols] in 4 microscaled bits: `codes` uint8 [rows][K / 2] and `scales` uint8 [rows][K / 32], K = cols
+    rounded up to 256, both contiguous on one device (the format is described in include/pahq.h)."""
+
+    __slots__ = ("codes", "scales", "cols")
+
+    def __init__(self, codes, scales, cols):
+        k = -(-int(cols) // 256) * 256
+        _need(codes.dtype == scales.dtype == torch.uint8 and codes.is_cuda and codes.device == scales.device, "codes and scales: uint8, on one device")
+        _need(codes.dim() == 2 and cols >= 1 and tuple(codes.shape) == (codes.shape[0], k // 2)
+              and tuple(scales.shape) == (codes.shape[0], k // 32), "codes [rows][K / 2], scales [rows][K / 32], K = cols rounded up to 256")
+        _need(codes.is_contiguous() and scales.is_contiguous(), "codes and scales: contiguous")
+        self.codes, self.scales, self.cols = codes, scales, int(cols)
+
+    @classmethod
+    def empty(cls, rows, cols, device="cuda"):
+        k = -(-int(cols) // 256) * 256
+        return cls(torch.empty((rows, k // 2), dtype=torch.uint8, device=device), torch.empty((rows, k // 32), dtype=torch.uint8, device=device), cols)
+
+    @property
+    def rows(self):
+        return self.codes.shape[0]
+
+    @property
+    def device(self):
+        return self.codes.device
+
+
+def mx4_quantize(x, by="rows", out=None):
+    """x float32 / bfloat16 / float16 [rows][cols] -> Mx4 of the same shape; by="columns": the Mx4 of x transposed, its blocks
+    running down the columns of x (a weight [k][n] as mx4_gemm takes it).  Rows, or columns, of x are contiguous."""
+    _need(x.is_cuda and x.dim() == 2 and x.dtype in _DTYPES, "x: a matrix in float32, bfloat16 or float16 on the device")
+    _need(by in ("rows", "columns"), "by: 'rows' or 'columns'")
+    _need(not _tracked(x), "rounding to 4 bits has no gradient: detach x")
+    if _row_stride(x) is None and _row_stride(x.t()) is not None:     # a transposed view: the other direction of its base
+        x, down = x.t(), by == "rows"
+    else:
+        down = by == "columns"
+    ld = _row_stride(x)
+    _need(ld is not None, "x: rows or columns contiguous, not overlapping")
+    rows, cols = (x.shape[1], x.shape[0]) if down else x.shape
+    _need(cols >= 1, "rows of at least one element")
+    if out is None:
+        out = Mx4.empty(rows, cols, x.device)
+    else:
+        _need(out.rows == rows and out.cols == cols and out.device == x.device, "out: of the result's shape, on x's device")
+    if rows:
+        _call("pahq_mx4_quantize", x.device, x.data_ptr(), _DTYPES[x.dtype], rows, cols, ld, 1 if down else 0, out.codes.data_ptr(), out.scales.data_ptr())
+    return out
+
+
+def _result(out, rows, cols, dtype, device):
+    """(tensor, row stride): `out` checked, or a new one."""
+    if out is None:
+        _need(dtype in _DTYPES, "dtype: float32, bfloat16 or float16")
+        return torch.empty((rows, cols), dtype=dtype, device=device), max(cols, 1)
+    ld = _row_stride(out) if out.dim() == 2 else None
+    _need(tuple(out.shape) == (rows, cols) and out.dtype in _DTYPES and out.device == device and ld is not None and not _tracked(out),
+          "out: [%d][%d] in float32, bfloat16 or float16, rows contiguous, on the operands' device, without a gradient" % (rows, cols))
+    return out, ld
+
+
+def mx4_dequantize(q, dtype=torch.float32, out=None):
+    """The values of an Mx4, exact in float32 and bfloat16.  `out` brings its own dtype."""
+    out, ld = _result(out, q.rows, q.cols, dtype, q.device)
+    if q.rows:
+        _call("pahq_mx4_dequantize", q.device, q.codes.data_ptr(), q.scales.data_ptr(), q.rows, q.cols, out.data_ptr(), _DTYPES[out.dtype], ld)
+    return out
+
+
+def mx4_gemm(a, w, bias=None, residual=None, dtype=torch.float32, out=None):
+    """a Mx4 [m][k], w Mx4 [n][k] -> a w^T (+ bias float32 [n]) (+ residual [m][n] of the result's dtype; it may be `out`)."""
+    _need(a.cols == w.cols and a.device == w.device, "a [m][k] and w [n][k] on one device")
+    m, n = a.rows, w.rows
+    out, ld = _result(out, m, n, dtype, a.device)
+    bp = rp = None
+    ld_res = ld
+    if bias is not None:
+        _need(bias.dtype == torch.float32 and tuple(bias.shape) == (n,) and bias.device == a.device and (n <= 1 or bias.stride(0) == 1)
+              and not _tracked(bias), "bias: float32 [n], contiguous, without a gradient")
+        bp = bias.data_ptr()
+    if residual is not None:
+        ld_res = _row_stride(residual) if residual.dim() == 2 else None
+        _need(tuple(residual.shape) == (m, n) and residual.dtype == out.dtype and residual.device == a.device and ld_res is not None
+              and not _tracked(residual), "residual: [m][n] of the result's dtype, rows contiguous, without a gradient")
+        rp = residual.data_ptr()
+    if m and n:
+        _call("pahq_mx4_gemm", a.device, a.codes.data_ptr(), a.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), m, n, a.cols, bp, rp, ld_res,
+              out.data_ptr(), _DTYPES[out.dtype], ld)
+    return out
+
+
+def rotary_table(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=0.0, turns=(1.0, 32.0), device="cuda"):
+    """The table `rotary` takes, int64 [rot_dim / 2] (bit patterns): frequencies theta^(-2 i / rot_dim), as they are
+    ("none"), divided by `factor` ("linear"), of a stretched theta ("base"), or divided where a pair turns less than turns[0]
+    times over `original` positions, kept from turns[1] times on and blended in between ("bands")."""
+    _need(scaling in _SCALING, "scaling: none, linear, base or bands")
+    host = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.int64)
+    _chk(lib().pahq_rotary_table(int(rot_dim), float(theta), _SCALING[scaling], float(factor), float(original), float(turns[0]), float(turns[1]),
+                                 C.cast(host.data_ptr(), C.POINTER(C.c_uint64))), "pahq_rotary_table")
+    return host.to(device)
+
+
+def _strides(t):
+    tokens, heads, d = t.shape
+    _need(d <= 1 or t.stride(2) == 1, "the elements of a head: contiguous")
+    st, sh = t.stride(0), t.stride(1)
+    if heads <= 1:
+        sh = d
+    if tokens <= 1:
+        st = max(heads - 1, 0) * sh + d
+    return st, sh
+
+
+def _rotary(x, positions, table, layout, magnitude, inverse, out):
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _need(out.shape == x.shape and out.dtype == x.dtype and out.device == x.device, "out: of x's shape and dtype, on its device")
+    tokens, heads, d = x.shape
+    if tokens and heads:
+        st, sh = _strides(x)
+        ot, oh = (st, sh) if out.data_ptr() == x.data_ptr() and out.stride() == x.stride() else _strides(out)
+        _call("pahq_rotary", x.device, x.data_ptr(), _DTYPES[x.dtype], tokens, heads, d, st, sh, positions.data_ptr(), table.data_ptr(), 2 * table.numel(),
+              _LAYOUTS[layout], magnitude, 1 if inverse else 0, out.data_ptr(), ot, oh)
+    return out
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, positions, table, layout, magnitude, inverse):
+        ctx.save_for_backward(positions, table)
+        ctx.how = layout, magnitude, not inverse
+        return _rotary(x, positions, table, layout, magnitude, inverse, None)
+
+    @staticmethod
+    def backward(ctx, grad):
+        positions, table = ctx.saved_tensors
+        if grad.shape[2] > 1 and grad.stride(2) != 1:       # an expanded or transposed gradient
+            grad = grad.contiguous()
+        return _Rotary.apply(grad, positions, table, *ctx.how), None, None, None, None, None
+
+
+def rotary(x, positions, table, layout="half", magnitude=1.0, inverse=False, out=None):
+    """Turns the first 2 * len(table) elements of every head of x [tokens][heads][d_head] by their tokens' positions (int64
+    [tokens]); the rest of the head is copied.  layout: "half" (pairs i, i + rot / 2) or "interleaved" (pairs 2 i, 2 i + 1).
+    inverse turns back (the gradient; x gets it by itself where autograd asks).  out may be x."""
+    _need(x.is_cuda and x.dim() == 3 and x.dtype in _DTYPES, "x: [tokens][heads][d_head] in float32, bfloat16 or float16 on the device")
+    _need(positions.dtype == torch.int64 and tuple(positions.shape) == (x.shape[0],) and positions.device == x.device
+          and (x.shape[0] <= 1 or positions.stride(0) == 1), "positions: int64 [tokens], contiguous, on x's device")
+    _need(table.dtype == torch.int64 and table.dim() == 1 and table.device == x.device and (table.numel() <= 1 or table.stride(0) == 1)
+          and 2 <= 2 * table.numel() <= x.shape[2], "table: from rotary_table, on x's device, for at most d_head elements")
+    _need(layout in _LAYOUTS, "layout: 'half' or 'interleaved'")
+    if _tracked(x, out):
+        _need(out is None, "out: not where a gradient is recorded")
+        return _Rotary.apply(x, positions, table, layout, float(magnitude), bool(inverse))
+    return _rotary(x, positions, table, layout, float(magnitude), bool(inverse), out)

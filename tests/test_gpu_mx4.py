@@ -1,0 +1,305 @@
+"""Matrices in 4 microscaled bits on the device: codes and scales bit for bit against the definition written out in Fractions
+and 64 bits, values, and products against sums in 64 bits."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+VALUE = np.concatenate([GRID, -GRID])
+HALF_STEP = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}       # relative to the value
+TINY = {"float32": 2.0 ** -150, "bfloat16": 2.0 ** -134, "float16": 2.0 ** -25}         # half of the type's smallest step
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2510_23264_amd as p
+    return p
+
+
+def held(x):
+    """Codes [rows][K] and scale bytes [rows][K / 32] of float rows (as float64), by the definition."""
+    rows, cols = x.shape
+    k = -(-cols // 256) * 256
+    x = np.concatenate([x, np.zeros((rows, k - cols))], 1).reshape(rows, k // 32, 32)
+    top = np.abs(x).max(2)                                  # NaN stays NaN
+    finite = np.isfinite(top)
+    with np.errstate(all="ignore"):
+        s = np.where(top > 0, np.maximum(np.frexp(top)[1] - 3, -127), 0)
+    s = np.where(finite, s, 0)
+    y = np.where(finite[..., None], x, 0) * 2.0 ** -s[..., None].astype(np.float64)
+    a = np.abs(y)
+    code = np.zeros(a.shape, np.int64)
+    for i in range(7):                                      # nearest; on a border the even one of codes i and i + 1
+        border = (GRID[i] + GRID[i + 1]) / 2
+        code = np.where((a > border) | ((a == border) & (i % 2 == 1)), i + 1, code)
+    code = np.where(finite[..., None], code | (np.signbit(y).astype(np.int64) << 3), 0)
+    return code.reshape(rows, k).astype(np.uint8), np.where(finite, s + 127, 255).astype(np.uint8)
+
+
+def packed(code):
+    return code[:, 0::2] | code[:, 1::2] << 4
+
+
+def values(code, scale):
+    with np.errstate(invalid="ignore"):
+        return VALUE[code] * np.where(scale == 255, np.nan, 2.0 ** (scale.astype(np.float64) - 127)).repeat(32, 1)
+
+
+def special_rows(rng, rows, cols):
+    """Normal rows of very different sizes with values on every border, zeros of both signs, empty blocks and rows."""
+    x = rng.standard_normal((rows, cols)) * 2.0 ** rng.integers(-60, 60, (rows, 1))
+    borders = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, 0.5, 6.0, -0.25, -2.5, -5.0, 0.0, -0.0])
+    x[::3] = rng.choice(borders, (len(x[::3]), cols)) * 2.0 ** rng.integers(-20, 20, (len(x[::3]), 1))
+    x[min(1, rows - 1), : cols // 2] = 0
+    if rows > 5:
+        x[4] = -0.0
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("rows, cols", [(1, 1), (1, 31), (3, 32), (2, 33), (7, 255), (5, 256), (6, 257), (9, 1000), (130, 768), (1, 4096), (33, 16384), (2049, 40)])
+def test_codes_and_scales_by_rows_and_columns(P, dtype, rows, cols):
+    import torch
+    rng = np.random.default_rng(rows * 70001 + cols)
+    t = getattr(torch, dtype)
+    x = special_rows(rng, rows, cols)
+    if dtype == "float16":
+        x = np.clip(x, -60000, 60000)
+    x = torch.from_numpy(x).to(t)
+    code, scale = held(x.double().numpy())
+    for by in ("rows", "columns"):
+        xd = (x if by == "rows" else x.t().contiguous()).cuda()
+        q = P.mx4_quantize(xd, by=by)
+        assert (q.rows, q.cols) == (rows, cols)
+        assert (q.scales.cpu().numpy() == scale).all(), by
+        assert (q.codes.cpu().numpy() == packed(code)).all(), by
+    for out in ("float32", "bfloat16", "float16"):
+        got = P.mx4_dequantize(q, dtype=getattr(torch, out)).cpu()
+        want = torch.from_numpy(values(code, scale)[:, :cols]).to(getattr(torch, out))
+        assert torch.equal(got, want), out
+
+
+def test_extreme_values(P):
+    import torch
+    tiny, big = 2.0 ** -149, float(np.finfo(np.float32).max)
+    x = np.zeros((12, 96), np.float32)
+    x[0, :4] = [tiny, -tiny, 3 * tiny, 0]
+    x[1, :4] = [2.0 ** -126, 2.0 ** -127, -2.0 ** -128, 2.0 ** -129]
+    x[2, :4] = [2.0 ** -125, 1.5 * 2.0 ** -126, 2.0 ** -124, 2.0 ** -130]
+    x[3, :3] = [big, -big, 1.0]
+    x[4, 5] = np.inf
+    x[5, 33] = -np.inf
+    x[6, 95] = np.nan
+    x[7, :] = 1.0
+    x[8, :] = -6.0
+    x[9, :3] = [7.0, 6.999, 5.0]
+    x[10, 0] = 1.0
+    x[10, 1:] = 1e-38
+    x[11, 64:] = np.array([2.0 ** 127, 2.0 ** 126, 1.0] + [0.0] * 29)
+    code, scale = held(x.astype(np.float64))
+    for by in ("rows", "columns"):
+        q = P.mx4_quantize(torch.from_numpy(x if by == "rows" else x.T.copy()).cuda(), by=by)
+        assert (q.scales.cpu().numpy() == scale).all() and (q.codes.cpu().numpy() == packed(code)).all()
+    want = values(code, scale)[:, :96]
+    for t in (torch.float32, torch.bfloat16):
+        got = P.mx4_dequantize(q, dtype=t).double().cpu().numpy()
+        assert np.array_equal(got, want, equal_nan=True)
+    assert np.isnan(want[4, :32]).all() and np.isfinite(want[4, 32:]).all()
+    # foreign matrices: every scale byte with every code
+    codes = torch.arange(256, dtype=torch.uint8).repeat(256, 1)[:, :128].contiguous()
+    codes[:, 64:] = torch.arange(64, 128, dtype=torch.uint8) + 128
+    scales = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 8).contiguous()
+    got = P.mx4_dequantize(P.Mx4(codes.cuda(), scales.cuda(), 256)).double().cpu().numpy()
+    c = np.stack([codes.numpy() & 15, codes.numpy() >> 4], 2).reshape(256, 256)
+    with np.errstate(over="ignore"):
+        want = values(c, scales.numpy()).astype(np.float32).astype(np.float64)
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+def test_strided_shifted_and_transposed_operands(P):
+    """Rows at any element, row strides that are odd, views of larger tensors, transposed views; nothing written outside."""
+    import torch
+    rng = np.random.default_rng(5)
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        for rows, cols, ld, shift in ((5, 300, 301, 1), (4, 257, 1031, 3), (6, 64, 65, 5)):
+            flat = torch.from_numpy(rng.standard_normal(rows * ld + 8)).to(dtype).cuda()
+            x = flat[shift:shift + rows * ld].view(rows, ld)[:, :cols]
+            want = P.mx4_quantize(x.contiguous())
+            q = P.Mx4.empty(rows + 2, cols)
+            q.codes.fill_(0xAA), q.scales.fill_(0xAA)
+            inner = P.Mx4(q.codes[1:rows + 1], q.scales[1:rows + 1], cols)
+            P.mx4_quantize(x, out=inner)
+            assert torch.equal(inner.codes, want.codes) and torch.equal(inner.scales, want.scales)
+            for t in (q.codes, q.scales):
+                assert (t[0] == 0xAA).all() and (t[rows + 1:] == 0xAA).all()
+            down = P.mx4_quantize(x, by="columns")
+            again = P.mx4_quantize(x.t())                          # a transposed view: rows of x^T
+            plain = P.mx4_quantize(x.t().contiguous())
+            assert torch.equal(down.codes, plain.codes) and torch.equal(again.codes, plain.codes) and torch.equal(down.scales, plain.scales)
+            buf = torch.full((rows * ld + 8,), 7.0, dtype=dtype, device="cuda")
+            out = buf[shift:shift + rows * ld].view(rows, ld)[:, :cols]
+            P.mx4_dequantize(inner, out=out)
+            assert torch.equal(out, P.mx4_dequantize(want, dtype=dtype))
+            out.fill_(7.0)
+            assert (buf == 7.0).all()
+
+
+def random_matrix(rng, rows, k, low, high):
+    """Random codes and scale bytes in [low, high], padded as the format says."""
+    kp = -(-k // 256) * 256
+    code = rng.integers(0, 16, (rows, kp)).astype(np.uint8)
+    code[:, k:] = 0
+    scale = rng.integers(low, high + 1, (rows, kp // 32)).astype(np.uint8)
+    scale[:, -(-k // 32):] = 127
+    return code, scale
+
+
+def device(P, code, scale, k):
+    import torch
+    return P.Mx4(torch.from_numpy(packed(code)).cuda(), torch.from_numpy(scale).cuda(), k)
+
+
+SIZES = [(1, 1, 1), (1, 16, 32), (2, 17, 33), (1, 4096, 512), (3, 100, 257), (15, 33, 700), (16, 64, 256), (17, 65, 1024), (31, 257, 300), (33, 129, 96),
+         (50, 515, 768), (64, 64, 64), (65, 130, 2000), (100, 2304, 768), (128, 128, 128), (129, 255, 512), (255, 256, 1280), (256, 256, 1023), (257, 300, 4096),
+         (300, 1000, 130), (512, 513, 256), (640, 384, 3000), (1025, 70, 520), (1500, 1537, 600)]
+
+
+@pytest.mark.parametrize("m, n, k", SIZES)
+def test_products_whose_sums_are_exact(P, m, n, k):
+    """Scales of 1 and 1/2: every product is a multiple of 2^-4 of at most 36, so any partial sum of up to 2^24 / (36 * 16)
+    = 29127 of them is a binary32 number, and the result is the exact sum whatever the order."""
+    import torch
+    rng = np.random.default_rng(m * 1000003 + n * 1009 + k)
+    a, sa = random_matrix(rng, m, k, 126, 127)
+    w, sw = random_matrix(rng, n, k, 126, 127)
+    want = values(a, sa) @ values(w, sw).T
+    got = P.mx4_gemm(device(P, a, sa, k), device(P, w, sw, k))
+    assert torch.equal(got.cpu(), torch.from_numpy(want).float())
+    bias, res = rng.integers(-64, 64, n) / 4.0, rng.integers(-64, 64, (m, n)) / 4.0
+    for t in (torch.float32, torch.bfloat16, torch.float16):
+        got = P.mx4_gemm(device(P, a, sa, k), device(P, w, sw, k), bias=torch.from_numpy(bias).float().cuda(), residual=torch.from_numpy(res).to(t).cuda(), dtype=t)
+        assert torch.equal(got.cpu(), torch.from_numpy(want + bias + res).to(t)), t
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("m, n, k", [(1, 70, 4096), (20, 40, 1000), (70, 200, 2048), (300, 520, 768), (513, 300, 1500)])
+def test_products_of_quantised_rows(P, dtype, m, n, k):
+    """Scales of all sizes.  A sum of K binary32 additions in any order is within K 2^-24 of the sum of magnitudes (K + 8 with the
+    joining of partial sums, bias and residual); one rounding to the result's type on top."""
+    import torch
+    rng = np.random.default_rng(m + n + k)
+    t = getattr(torch, dtype)
+    x = rng.standard_normal((m, k)) * np.exp(rng.standard_normal(k))
+    x[0] = 0
+    qa = P.mx4_quantize(torch.from_numpy(x).float().cuda())
+    qw = P.mx4_quantize(torch.from_numpy(rng.standard_normal((k, n)) * 0.02).float().cuda(), by="columns")
+    a, w = P.mx4_dequantize(qa).double().cpu().numpy(), P.mx4_dequantize(qw).double().cpu().numpy()
+    bias = torch.from_numpy(rng.standard_normal(n)).float()
+    res = torch.from_numpy(rng.standard_normal((m, n))).to(t)
+    got = P.mx4_gemm(qa, qw, bias=bias.cuda(), residual=res.cuda(), dtype=t).double().cpu().numpy()
+    want = a @ w.T + bias.double().numpy() + res.double().numpy()
+    size = np.abs(a) @ np.abs(w).T + np.abs(bias.double().numpy()) + np.abs(res.double().numpy())
+    bound = (k + 8) * 2.0 ** -24 * size
+    bound = bound + HALF_STEP[dtype] * (np.abs(want) + bound) + TINY[dtype]
+    assert (np.abs(got - want) <= bound).all(), (np.abs(got - want) / bound).max()
+    # the same call, the same bits
+    again = P.mx4_gemm(qa, qw, bias=bias.cuda(), residual=res.cuda(), dtype=t).double().cpu().numpy()
+    assert np.array_equal(got, again)
+
+
+def test_blocks_that_are_not_finite_stay_in_their_rows(P):
+    import torch
+    rng = np.random.default_rng(11)
+    for m, n, k in ((5, 40, 300), (70, 90, 600), (300, 280, 1100)):
+        x, y = rng.standard_normal((m, k)).astype(np.float32), rng.standard_normal((n, k)).astype(np.float32)
+        x[3, 5], x[1, k - 1], y[7, 40] = np.nan, np.inf, -np.inf
+        got = P.mx4_gemm(P.mx4_quantize(torch.from_numpy(x).cuda()), P.mx4_quantize(torch.from_numpy(y).cuda())).cpu().numpy()
+        nan = np.zeros((m, n), bool)
+        nan[[1, 3]] = True
+        nan[:, 7] = True
+        assert np.array_equal(np.isnan(got), nan) and np.isfinite(got[~nan]).all()
+
+
+@pytest.mark.parametrize("m, n, k", [(1, 40, 300), (19, 100, 512), (130, 260, 256), (300, 513, 800)])
+def test_results_in_strided_memory_and_in_place(P, m, n, k):
+    """Results and residuals at any element and stride, a residual that is the result; nothing written beside the rows."""
+    import torch
+    rng = np.random.default_rng(k)
+    qa, qw = (P.mx4_quantize(torch.from_numpy(rng.standard_normal((r, k))).float().cuda()) for r in (m, n))
+    for t in (torch.float32, torch.bfloat16, torch.float16):
+        res = torch.from_numpy(rng.standard_normal((m, n))).to(t).cuda()
+        want = P.mx4_gemm(qa, qw, residual=res, dtype=t)
+        for ld, shift in ((n + 3, 1), (n + 8, 8), (n, 0)):
+            buf = torch.full((m * ld + 16,), 9.0, dtype=t, device="cuda")
+            out = buf[shift:shift + m * ld].view(m, ld)[:, :n]
+            wide = torch.zeros((m, n + 5), dtype=t, device="cuda")[:, 2:n + 2]
+            wide.copy_(res)
+            P.mx4_gemm(qa, qw, residual=wide, out=out)
+            assert torch.equal(out, want)
+            out.fill_(9.0)
+            assert (buf == 9.0).all()
+            out.copy_(res)
+            P.mx4_gemm(qa, qw, residual=out, out=out)
+            assert torch.equal(out, want)
+
+
+def test_wrapper_refuses(P):
+    import torch
+    q = P.mx4_quantize(torch.randn(4, 64, device="cuda"))
+    bad = [lambda: P.mx4_quantize(torch.randn(4, 64, device="cuda", dtype=torch.float64)), lambda: P.mx4_quantize(torch.randn(4, 64, 2, device="cuda")),
+           lambda: P.mx4_quantize(torch.randn(4, 64, device="cuda"), by="blocks"), lambda: P.mx4_quantize(torch.randn(8, 8, 8, device="cuda")[:, :, 0][:, ::2]),
+           lambda: P.mx4_quantize(torch.randn(4, 0, device="cuda")), lambda: P.mx4_quantize(torch.randn(1, 64, device="cuda").expand(4, 64)),
+           lambda: P.mx4_quantize(torch.randn(4, 64, device="cuda", requires_grad=True)), lambda: P.mx4_quantize(torch.randn(4, 64, device="cuda"), out=P.Mx4.empty(4, 65)),
+           lambda: P.mx4_gemm(q, P.mx4_quantize(torch.randn(4, 65, device="cuda"))), lambda: P.mx4_gemm(q, q, bias=torch.zeros(5, device="cuda")),
+           lambda: P.mx4_gemm(q, q, bias=torch.zeros(4, device="cuda", dtype=torch.bfloat16)), lambda: P.mx4_gemm(q, q, residual=torch.zeros(4, 5, device="cuda")),
+           lambda: P.mx4_gemm(q, q, residual=torch.zeros(4, 4, device="cuda"), dtype=torch.bfloat16), lambda: P.mx4_gemm(q, q, dtype=torch.float64),
+           lambda: P.mx4_gemm(q, q, out=torch.zeros(4, 4, device="cuda").t()[:, ::2]), lambda: P.mx4_gemm(q, q, bias=torch.zeros(4)),
+           lambda: P.mx4_gemm(q, q, bias=torch.zeros(4, device="cuda", requires_grad=True)), lambda: P.mx4_dequantize(q, dtype=torch.float64),
+           lambda: P.mx4_dequantize(q, out=torch.zeros(4, 64))]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    base = torch.zeros(64, device="cuda")
+    with pytest.raises(P.PahqError) as e:               # residual that overlaps the result without being it
+        P.mx4_gemm(q, q, residual=base[1:17].view(4, 4), out=base[:16].view(4, 4))
+    assert e.value.code == -1
+
+
+def test_nothing_to_do(P):
+    import torch
+    empty = P.mx4_quantize(torch.empty(0, 70, device="cuda"))
+    q = P.mx4_quantize(torch.randn(3, 70, device="cuda"))
+    assert P.mx4_gemm(empty, q).shape == (0, 3) and P.mx4_gemm(q, empty).shape == (3, 0) and P.mx4_dequantize(empty).shape == (0, 70)
+    assert P.mx4_quantize(torch.empty(70, 0, device="cuda"), by="columns").rows == 0
+
+
+def test_streams_and_replayed_graphs(P):
+    """Quantise and multiply on a stream of its own, then captured twice and replayed with new rows in between, against the
+    eager calls; two captured graphs in turn share nothing."""
+    import torch
+    torch.manual_seed(0)
+    w = P.mx4_quantize(torch.randn(700, 512, device="cuda"))
+    xs = [torch.randn(m, 512, device="cuda") for m in (3, 70, 300)]
+    side = torch.cuda.Stream()
+    for x in xs:
+        want = P.mx4_gemm(P.mx4_quantize(x), w)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = P.mx4_gemm(P.mx4_quantize(x), w)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, want)
+    graphs = []
+    for x in xs[:2]:
+        g = torch.cuda.CUDAGraph()
+        held_in = x.clone()
+        with torch.cuda.graph(g):
+            out = P.mx4_gemm(P.mx4_quantize(held_in), w, dtype=torch.bfloat16)
+        graphs.append((g, held_in, out))
+    for turn in range(4):
+        for g, held_in, out in graphs:
+            held_in.normal_()
+            want = P.mx4_gemm(P.mx4_quantize(held_in), w, dtype=torch.bfloat16)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want), turn

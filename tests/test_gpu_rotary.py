@@ -1,0 +1,247 @@
+"""Rotary positions on the device against the definition in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+HALF_STEP = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2510_23264_amd as p
+    return p
+
+
+def frequencies(rot, theta, scaling, factor, original, lo, hi):
+    r = rot
+    if scaling == "base":
+        theta = theta * factor ** (r / (r - 2))
+    f = theta ** (-2.0 * np.arange(r // 2) / r)
+    if scaling == "linear":
+        f = f / factor
+    if scaling == "bands":
+        g = np.clip((original * f / (2 * math.pi) - lo) / (hi - lo), 0, 1)
+        f = f * (g + (1 - g) / factor)
+    return f
+
+
+def turned(x, positions, f, layout, magnitude=1.0, inverse=False):
+    """x float64 [tokens][heads][d]."""
+    r = 2 * len(f)
+    phi = positions.astype(np.float64)[:, None] * f * (-1 if inverse else 1)
+    c, s = np.cos(phi)[:, None], np.sin(phi)[:, None]
+    out = x.copy()
+    ia = np.arange(r // 2) if layout == "half" else 2 * np.arange(r // 2)
+    ib = ia + r // 2 if layout == "half" else ia + 1
+    out[..., ia] = magnitude * (x[..., ia] * c - x[..., ib] * s)
+    out[..., ib] = magnitude * (x[..., ia] * s + x[..., ib] * c)
+    return out
+
+
+def bound(x, want, rot, layout, magnitude, dtype, far, f):
+    """The angle is off by 2^-25 of an eighth of a turn and by position * 2^-65 turn, the oracle's by position * f * 2^-52;
+    sine and cosine by two ulps (2^-23), the magnitude's product by 2^-24; two products and a sum round by 2^-24 each.  Of
+    |a| + |b|, all in all; then half a step of the type, and fp16's subnormals."""
+    pair = np.zeros_like(x)
+    ia = np.arange(rot // 2) if layout == "half" else 2 * np.arange(rot // 2)
+    ib = ia + rot // 2 if layout == "half" else ia + 1
+    size = np.abs(x[..., ia]) + np.abs(x[..., ib])
+    angle = 2.0 ** -25 * math.pi / 4 + far * (2.0 ** -65 * 2 * math.pi + f * 2.0 ** -52)
+    pair[..., ia] = pair[..., ib] = abs(magnitude) * size * (angle + 2.0 ** -23 + 4 * 2.0 ** -24)
+    return pair + HALF_STEP[dtype] * (np.abs(want) + pair) * (pair > 0) + (2.0 ** -25 if dtype == "float16" else 2.0 ** -134)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("tokens, heads, d, rot", [(1, 1, 2, 2), (1, 40, 128, 128), (3, 5, 64, 16), (7, 1, 80, 20), (33, 3, 96, 96), (16, 2, 66, 34), (5, 7, 33, 32),
+                                                   (1000, 4, 64, 64), (2, 1, 1024, 1024), (9, 64, 256, 128)])
+def test_layouts_parts_and_types(P, dtype, layout, tokens, heads, d, rot):
+    import torch
+    rng = np.random.default_rng(tokens * 7 + d + rot)
+    x = torch.from_numpy(rng.standard_normal((tokens, heads, d))).to(getattr(torch, dtype))
+    positions = rng.integers(0, 1 << 20, tokens)
+    positions[0] = 0
+    f = frequencies(rot, 10000.0, "none", 1, 0, 1, 2)
+    table = P.rotary_table(rot)
+    for inverse, magnitude in ((False, 1.0), (True, 1.25)):
+        want = turned(x.double().numpy(), positions, f, layout, magnitude, inverse)
+        lim = bound(x.double().numpy(), want, rot, layout, magnitude, dtype, 1 << 20, f)
+        xd = x.cuda()
+        got = P.rotary(xd, torch.from_numpy(positions).cuda(), table, layout=layout, magnitude=magnitude, inverse=inverse)
+        err = np.abs(got.double().cpu().numpy() - want)
+        assert (err <= lim).all(), (err / lim).max()
+        assert torch.equal(got[..., rot:], xd[..., rot:])
+        P.rotary(xd, torch.from_numpy(positions).cuda(), table, layout=layout, magnitude=magnitude, inverse=inverse, out=xd)
+        assert torch.equal(xd, got)
+
+
+@pytest.mark.parametrize("scaling", ["none", "linear", "base", "bands"])
+def test_far_positions_and_stretched_frequencies(P, scaling):
+    """Positions up to 2^31, negative ones too: the oracle's own doubles are the larger part of the bound there, so the angle
+    is taken from exact integers instead: position * frequency in Fractions of a turn."""
+    import torch
+    from fractions import Fraction
+    rot, theta, factor, original, lo, hi = 64, 500000.0, 8.0, 8192.0, 1.0, 4.0
+    table = P.rotary_table(rot, theta, scaling, factor, original, (lo, hi))
+    entries = [int(v) % (1 << 64) for v in table.cpu().tolist()]
+    positions = np.array([0, 1, 100, 8191, 8192, 131071, 1 << 20, (1 << 24) + 1, (1 << 31) - 1, -1, -5000])
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((len(positions), 2, 64)).astype(np.float32)
+    got = P.rotary(torch.from_numpy(x).cuda(), torch.from_numpy(positions).cuda(), table).double().cpu().numpy()
+    f = frequencies(rot, theta, scaling, factor, original, lo, hi)
+    assert all(abs(e / 2.0 ** 64 - v / (2 * math.pi)) <= 2.0 ** -48 * v + 2.0 ** -65 for e, v in zip(entries, f))
+    phi = np.array([[float(Fraction(int(p)) * e % (1 << 64) / (1 << 64)) for e in entries] for p in positions]) * 2 * math.pi
+    c, s = np.cos(phi)[:, None], np.sin(phi)[:, None]
+    a, b = x[..., :32].astype(np.float64), x[..., 32:].astype(np.float64)
+    want = np.concatenate([a * c - b * s, a * s + b * c], -1)
+    lim = bound(x.astype(np.float64), want, rot, "half", 1.0, "float32", 0, f)
+    assert (np.abs(got - want) <= lim).all(), (np.abs(got - want) / lim).max()
+
+
+def test_strides_views_and_shared_rows(P):
+    """Queries and keys inside the rows of a projection, heads outside, odd strides and starts; rows that share memory."""
+    import torch
+    torch.manual_seed(1)
+    table = P.rotary_table(32)
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        for layout in ("half", "interleaved"):
+            rows = torch.randn(9, 7 * 48 + 1, device="cuda").to(dtype)
+            x = rows[:, 1:1 + 5 * 48].view(9, 5, 48)
+            pos = torch.arange(9, device="cuda") * 1000
+            want = P.rotary(x.contiguous(), pos, table, layout=layout)
+            assert torch.equal(P.rotary(x, pos, table, layout=layout), want)
+            planes = torch.empty(5, 9, 48, dtype=dtype, device="cuda").transpose(0, 1)
+            assert torch.equal(P.rotary(x, pos, table, layout=layout, out=planes), want)
+            assert torch.equal(P.rotary(planes.copy_(x), pos, table, layout=layout, out=planes), want)
+            shared = torch.randn(9, 1, 48, device="cuda").to(dtype).expand(9, 5, 48)
+            assert torch.equal(P.rotary(shared, pos, table, layout=layout), P.rotary(shared.contiguous(), pos, table, layout=layout))
+            keep = rows.clone()
+            P.rotary(x, pos, table, layout=layout, out=x)
+            assert torch.equal(x, want)
+            keep[:, 1:1 + 5 * 48] = rows[:, 1:1 + 5 * 48]
+            assert torch.equal(rows, keep)                       # the values beside them are as they were
+
+
+def test_gradient_against_the_formula_and_differences(P):
+    import torch
+    torch.manual_seed(2)
+    table = P.rotary_table(24, 100.0, "linear", 2.0)
+    pos = torch.tensor([0, 3, 1000, 70000, 9], device="cuda")
+    f = frequencies(24, 100.0, "linear", 2.0, 0, 1, 2)
+    for layout in ("half", "interleaved"):
+        x = torch.randn(5, 3, 32, device="cuda", requires_grad=True)
+        g = torch.randn(5, 3, 32, device="cuda")
+        y = P.rotary(x, pos, table, layout=layout, magnitude=1.5)
+        (grad,) = torch.autograd.grad(y, x, g)
+        gd = g.double().cpu().numpy()
+        want = turned(gd, pos.cpu().numpy(), f, layout, 1.5, True)
+        want[..., 24:] = gd[..., 24:]
+        lim = bound(gd, want, 24, layout, 1.5, "float32", 70000, f)
+        assert (np.abs(grad.double().cpu().numpy() - want) <= lim).all()
+        # the call is linear in x: a difference over any step is the derivative, up to the roundings of the two results
+        v = torch.randn_like(x)
+        with torch.no_grad():
+            diff = ((P.rotary(x + 4 * v, pos, table, layout=layout, magnitude=1.5).double() - P.rotary(x - 4 * v, pos, table, layout=layout, magnitude=1.5).double())
+                    * g.double()).sum() / 8
+        size = (1.5 * 2 * (x.abs() + 4 * v.abs()).double() * g.abs().double()).sum() / 4
+        assert abs(diff - (grad.double() * v.double()).sum()) <= 8 * 2.0 ** -21 * size
+        # through an expanded gradient, an input shared by the heads, and twice
+        shared = torch.randn(5, 1, 32, device="cuda", requires_grad=True)
+        P.rotary(shared.expand(5, 3, 32), pos, table, layout=layout).sum().backward()
+        ones = P.rotary(torch.ones(5, 3, 32, device="cuda"), pos, table, layout=layout, inverse=True)
+        assert torch.allclose(shared.grad, ones.sum(1, keepdim=True), rtol=0, atol=3 * 2 * 2.0 ** -22)
+        w = torch.randn(5, 3, 32, device="cuda", requires_grad=True)
+        (g1,) = torch.autograd.grad(P.rotary(w, pos, table, layout=layout), w, g.clone().requires_grad_(), create_graph=True)
+        assert g1.requires_grad
+
+
+def test_refusals_and_nothing_to_do(P):
+    import torch
+    table = P.rotary_table(32)
+    x, pos = torch.randn(4, 3, 64, device="cuda"), torch.arange(4, device="cuda")
+    bad = [dict(x=x.double()), dict(x=x[0]), dict(positions=pos[:3]), dict(positions=pos.int()), dict(positions=torch.arange(8, device="cuda")[::2]),
+           dict(table=P.rotary_table(128)), dict(table=table.int()), dict(layout="quarter"), dict(x=x.transpose(1, 2).contiguous().transpose(1, 2)),
+           dict(out=torch.empty(4, 3, 65, device="cuda")), dict(out=x.bfloat16()), dict(x=x.clone().requires_grad_(), out=torch.empty_like(x)),
+           dict(positions=pos.cpu())]
+    for change in bad:
+        with pytest.raises(ValueError):
+            P.rotary(**dict(dict(x=x, positions=pos, table=table), **change))
+    flat = torch.zeros(4 * 3 * 64 + 64, device="cuda")
+    with pytest.raises(P.PahqError):                 # a result that overlaps its operand
+        P.rotary(flat[:768].view(4, 3, 64), pos, table, out=flat[64:832].view(4, 3, 64))
+    with pytest.raises(P.PahqError):                 # a result whose heads share memory
+        P.rotary(x, pos, table, out=torch.empty(4, 1, 64, device="cuda").expand(4, 3, 64))
+    assert P.rotary(x[:0], pos[:0], table).shape == (0, 3, 64) and P.rotary(x[:, :0], pos, table).shape == (4, 0, 64)
+
+
+def test_streams_and_replayed_graphs(P):
+    import torch
+    table = P.rotary_table(64)
+    x, pos = torch.randn(50, 6, 64, device="cuda"), torch.arange(50, device="cuda")
+    want = P.rotary(x, pos, table)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = P.rotary(x, pos, table)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = P.rotary(x, pos, table)
+    for _ in range(4):
+        x.normal_()
+        pos += 1000
+        want = P.rotary(x, pos, table)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_a_layers_projections_together(P):
+    """One attention layer's way as a program runs it: rows to 4 bits, queries, keys and values in one product, rotation in
+    place of the queries and keys between the values, attention, rows to 4 bits again, output product on the residual.
+    Every step against 64 bits from the tensors it was given, with its own bound."""
+    import torch
+    torch.manual_seed(4)
+    B, S, H, dh, rot, d = 3, 37, 4, 64, 32, 256
+    T = B * S
+    stream = torch.randn(T, d, device="cuda")
+    wqkv = P.mx4_quantize(0.05 * torch.randn(d, 3 * H * dh, device="cuda"), by="columns")
+    wo = P.mx4_quantize(0.05 * torch.randn(H * dh, d, device="cuda"), by="columns")
+    bias = 0.1 * torch.randn(3 * H * dh, device="cuda")
+    table, pos = P.rotary_table(rot, theta=10000.0, scaling="linear", factor=2.0), torch.arange(S, device="cuda").repeat(B)
+
+    def product_bound(a, w, want, extra, k):
+        size = a.abs() @ w.abs().t() + extra
+        b = (k + 8) * 2.0 ** -24 * size
+        return b + 2.0 ** -24 * (want.abs() + b)
+
+    x = torch.nn.functional.layer_norm(stream, (d,))
+    q = P.mx4_quantize(x)
+    qkv = P.mx4_gemm(q, wqkv, bias=bias)
+    a, w = P.mx4_dequantize(q).double(), P.mx4_dequantize(wqkv).double()
+    want = a @ w.t() + bias.double()
+    assert ((qkv.double() - want).abs() <= product_bound(a, w, want, bias.double().abs(), d)).all()
+    assert ((a - x.double()).abs() <= x.double().abs().view(T, -1, 32).amax(2).repeat_interleave(32, 1) * 0.25).all()   # 6 of up to 8: a quarter
+    rows = qkv.view(T, 3, H, dh)
+    before = rows.double().cpu().numpy()
+    qk = qkv[:, :2 * H * dh].view(T, 2 * H, dh)
+    P.rotary(qk, pos, table, out=qk)
+    f = frequencies(rot, 10000.0, "linear", 2.0, 0, 1, 2)
+    ref = before[:, :2].reshape(T, 2 * H, dh)
+    want = turned(ref, pos.cpu().numpy(), f, "half")
+    assert (np.abs(qk.double().cpu().numpy() - want) <= bound(ref, want, rot, "half", 1.0, "float32", S, f)).all()
+    assert (rows[:, 2].double().cpu().numpy() == before[:, 2]).all()
+    per_head = rows.view(B, S, 3, H, dh).permute(2, 0, 3, 1, 4).double()
+    scores = (per_head[0] @ per_head[1].transpose(-1, -2).contiguous()) / math.sqrt(dh)
+    scores = scores.masked_fill(torch.ones(S, S, dtype=torch.bool, device="cuda").triu(1), -math.inf)
+    z = (scores.softmax(-1) @ per_head[2].contiguous()).permute(0, 2, 1, 3).reshape(T, H * dh).float()
+    qz = P.mx4_quantize(z)
+    out = stream.clone()
+    P.mx4_gemm(qz, wo, residual=out, out=out)
+    a, w = P.mx4_dequantize(qz).double(), P.mx4_dequantize(wo).double()
+    want = a @ w.t() + stream.double()
+    assert ((out.double() - want).abs() <= product_bound(a, w, want, stream.double().abs(), H * dh)).all()
