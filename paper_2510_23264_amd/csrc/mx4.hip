@@ -8,6 +8,7 @@
 // additions in any order leave.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <atomic>
 #include "../../include/pahq.h"
 #include "mma_util.h"
 #include "device_tensor.h"
@@ -106,6 +107,19 @@ __global__ __launch_bounds__(256) void mx4_values_k(const uint32_t* codes, const
 }
 
 // ---------------------------------------------------------------- product
+typedef float v16f __attribute__((ext_vector_type(16)));
+template <int N> struct Int { static constexpr int value = N; };
+
+// Tile of a workgroup: the eight XCDs take neighbouring ranges of the tiles, which run down bands of eight rows of tiles, so
+// that what an XCD works on at a time shares operands in its L2.  tm >= mt: no tile (the ranges are rounded up).
+__device__ __forceinline__ void tile_of(int wg, int mt, int nt, int& tm, int& tn) {
+  const int t = xcd_tile(wg, mt * nt);
+  if (t >= mt * nt) { tm = mt; tn = 0; return; }
+  const int band = t / (8 * nt), in = t - band * 8 * nt, high = min(8, mt - band * 8);
+  tn = in / high;
+  tm = band * 8 + in - tn * high;
+}
+
 // Few rows: 16 * MT rows x 16 columns a workgroup, the sum over k split over its waves (slab s of 256 elements to wave s
 // mod WAVES) and joined in LDS in the order of the waves, so results do not depend on timing.  Operands come straight from
 // global memory: a lane reads two neighbouring blocks of its row with their scales, which are one halfword, and the four
@@ -162,6 +176,153 @@ __global__ __launch_bounds__(WAVES * 64) void mx4_gemm_few_k(const uint8_t* a, c
   }
 }
 
+// Tiles through LDS.  AF x WF products of 32 x 32 (V_MFMA_SCALE_F32_32X32X64_F8F6F4) a wave, WM x WN waves; slabs of 256
+// elements of k (128 bytes of codes a row) in two stages, requested one slab ahead straight into LDS.  In a slab a lane takes
+// four neighbouring blocks of its row, one a step, so the bytes of one word of scales serve its four steps through the
+// instruction's byte selector.  Row AF j + f of a wave's A rows (WF j + f of its W rows) is MFMA row j of fragment f:
+// a lane then holds WF neighbouring columns of a result row, and one LDS read brings the scales of all fragments.
+// LDS holds fragment f's rows next to each other (any order can be loaded) with the 16-byte chunks of a row XOR-swizzled
+// by half the row's place, so that 16 lanes cover all 64 banks.  Scales are 8 bytes of a row a slab: fetched by slabs they
+// would cost a cache line of 128 bytes each, so a thread fetches those of one row for four slabs at a time.
+template <int AF, int WF, int WM, int WN>
+struct Mx4Tile {
+  static constexpr int BM = AF * 32 * WM, BN = WF * 32 * WN, THREADS = WM * WN * 64, ROWS = BM + BN;
+  static constexpr int STAGE = ROWS * 128, SCALES = ROWS * 32;
+  static constexpr int LDS = 2 * STAGE + SCALES;
+  static_assert(ROWS == THREADS, "a thread fetches the scales of one row");
+};
+template <typename T, int AF, int WF, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void mx4_gemm_tile_k(const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n,
+                                                              int slabs, int mt, int nt, const float* bias, const T* res, long long ld_res, T* out,
+                                                              long long ld) {
+  typedef Mx4Tile<AF, WF, WM, WN> C;
+  extern __shared__ __align__(16) uint8_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 31, g = lane >> 5;
+  const int wm = wave / WN, wn = wave % WN;
+  int tm, tn;
+  tile_of(blockIdx.x, mt, nt, tm, tn);
+  if (tm >= mt) return;
+  const int m0 = tm * C::BM, n0 = tn * C::BN;
+  const long long row_bytes = (long long)slabs * 128;
+  // this lane's eight chunks of a stage: place (slot, position) of LDS, and where in the tile's rows the bytes come from
+  constexpr int L = 8;
+  uint32_t off[L];
+#pragma unroll
+  for (int i = 0; i < L; i++) {
+    const int slot = (i * (C::THREADS / 64) + wave) * 8 + (lane >> 3), c = (lane & 7) ^ ((slot >> 1) & 7);
+    int row;
+    if (slot < C::BM) row = min((slot / (AF * 32)) * (AF * 32) + (slot & 31) * AF + (slot / 32) % AF, m - 1 - m0);
+    else {
+      const int q = slot - C::BM;
+      row = min((q / (WF * 32)) * (WF * 32) + (q & 31) * WF + (q / 32) % WF, n - 1 - n0);
+    }
+    off[i] = (uint32_t)(row * row_bytes + c * 16);
+  }
+  const uint8_t* ab = a + m0 * row_bytes;
+  const uint8_t* wb = w + n0 * row_bytes;
+  const uint32_t stage0 = lds_addr_of(lds);
+  const auto request = [&](int s) {
+    const uint32_t base = stage0 + (s & 1) * C::STAGE + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < L; i++)
+      slab_load16s((i * (C::THREADS / 64) * 8 < C::BM ? ab : wb) + (long long)s * 128, off[i], base + i * C::THREADS * 16);
+  };
+  static_assert(C::BM % (C::THREADS / 8) == 0, "a request belongs to one operand");
+  // scales of row tid of the tile, four slabs: words [slab][half of the slab][row] in LDS
+  const uint8_t* sp = tid < C::BM ? as + (long long)(m0 + min(tid, m - 1 - m0)) * slabs * 8 : ws + (long long)(n0 + min(tid - C::BM, n - 1 - n0)) * slabs * 8;
+  uint2 sc[4];
+  const auto fetch_scales = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) sc[i] = s + i < slabs ? *(const uint2*)(sp + (long long)(s + i) * 8) : make_uint2(0, 0);
+  };
+  uint32_t* const scl = (uint32_t*)(lds + 2 * C::STAGE);
+  v16f acc[AF][WF];
+#pragma unroll
+  for (int x = 0; x < AF; x++)
+#pragma unroll
+    for (int y = 0; y < WF; y++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) acc[x][y][i] = 0.f;
+
+  fetch_scales(0);
+  request(0);
+  for (int s = 0; s < slabs; s++) {
+    wait_vm_barrier<0>();              // slab s is there for every wave, and none reads the stage of slab s - 1 any more
+    if ((s & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        scl[(i * 2 + 0) * C::ROWS + tid] = sc[i].x;
+        scl[(i * 2 + 1) * C::ROWS + tid] = sc[i].y;
+      }
+      wait_vm_barrier<63>();
+      if (s + 4 < slabs) fetch_scales(s + 4);
+    }
+    if (s + 1 < slabs) request(s + 1);
+    const uint8_t* const sa = lds + (s & 1) * C::STAGE + wm * (AF * 32) * 128;
+    const uint8_t* const sw = lds + (s & 1) * C::STAGE + (C::BM + wn * (WF * 32)) * 128;
+    const uint32_t* const sc_s = scl + ((s & 3) * 2 + g) * C::ROWS;
+    int asc[AF], wsc[WF];
+#pragma unroll
+    for (int x = 0; x < AF; x++) asc[x] = (int)sc_s[wm * (AF * 32) + j * AF + x];
+#pragma unroll
+    for (int y = 0; y < WF; y++) wsc[y] = (int)sc_s[C::BM + wn * (WF * 32) + j * WF + y];
+    const auto step = [&](auto sel) {
+      constexpr int S = decltype(sel)::value;
+      v8i af[AF], wf[WF];
+      const int at = j * 128 + (((4 * g + S) ^ ((j >> 1) & 7)) * 16);       // 32 rows a fragment: the swizzle is the lane's own
+#pragma unroll
+      for (int x = 0; x < AF; x++) {
+        const int4 v = *(const int4*)(sa + x * 32 * 128 + at);
+        af[x] = (v8i){v.x, v.y, v.z, v.w, 0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int y = 0; y < WF; y++) {
+        const int4 v = *(const int4*)(sw + y * 32 * 128 + at);
+        wf[y] = (v8i){v.x, v.y, v.z, v.w, 0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int x = 0; x < AF; x++)
+#pragma unroll
+        for (int y = 0; y < WF; y++)
+          acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(af[x], wf[y], acc[x][y], 4, 4, S, asc[x], S, wsc[y]);
+    };
+    step(Int<0>());
+    step(Int<1>());
+    step(Int<2>());
+    step(Int<3>());
+  }
+  const int col = n0 + wn * (WF * 32) + j * WF;
+  if (col >= n) return;
+  const bool whole = col + WF <= n;
+  float b[WF];
+#pragma unroll
+  for (int y = 0; y < WF; y++) b[y] = bias && col + y < n ? bias[col + y] : 0.f;
+#pragma unroll
+  for (int x = 0; x < AF; x++)
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      const int row = m0 + wm * (AF * 32) + (8 * (i / 4) + 4 * g + i % 4) * AF + x;
+      if (row >= m) continue;
+      T* const o = out + (long long)row * ld + col;
+      const T* const r = res + (long long)row * ld_res + col;
+      if (whole) {
+        Pack<T, WF> v, q;
+        if (res) q = *(const Pack<T, WF>*)r;
+#pragma unroll
+        for (int y = 0; y < WF; y++) {
+          float f = acc[x][y][i] + b[y];
+          if (res) f += as_float(q.v[y]);
+          v.v[y] = from_float<T>(f);
+        }
+        *(Pack<T, WF>*)o = v;
+      } else {
+#pragma unroll
+        for (int y = 0; y < WF; y++)
+          if (col + y < n) o[y] = from_float<T>(acc[x][y][i] + b[y] + (res ? as_float(r[y]) : 0.f));
+      }
+    }
+}
+
 namespace {
 template <typename T>
 int quantize_as(hipStream_t st, const T* x, int rows, int cols, long long ld, int by, uint8_t* codes, uint8_t* scales) {
@@ -181,9 +342,33 @@ int values_as(hipStream_t st, const uint8_t* codes, const uint8_t* scales, int r
   hipLaunchKernelGGL(mx4_values_k<T>, dim3(wg), dim3(256), 0, st, (const uint32_t*)codes, scales, rows, cols, groups, out, ld);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
+template <typename T, int AF, int WF, int WM, int WN>
+int launch_tile(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs, const float* bias,
+                const T* res, long long ld_res, T* out, long long ld) {
+  typedef Mx4Tile<AF, WF, WM, WN> C;
+  const int mt = (m + C::BM - 1) / C::BM, nt = (n + C::BN - 1) / C::BN;
+  const void* fn = (const void*)mx4_gemm_tile_k<T, AF, WF, WM, WN>;
+  // more LDS than a launch gets by default: an attribute of the kernel on one device, set once for each
+  static std::atomic<bool> set[64];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return PAHQ_EHIP;
+  if (!set[dev].load(std::memory_order_acquire)) {
+    if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) != hipSuccess) return PAHQ_EHIP;
+    set[dev].store(true, std::memory_order_release);
+  }
+  hipLaunchKernelGGL((mx4_gemm_tile_k<T, AF, WF, WM, WN>), dim3((mt * nt + 7) / 8 * 8), dim3(C::THREADS), C::LDS, st, a, as, w, ws, m, n, slabs, mt, nt,
+                     bias, res, ld_res, out, ld);
+  return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
+}
 template <typename T>
 int gemm_as(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs, const float* bias,
             const T* res, long long ld_res, T* out, long long ld) {
+#define TILE(AF_, WF_, WM_, WN_) return launch_tile<T, AF_, WF_, WM_, WN_>(st, a, as, w, ws, m, n, slabs, bias, res, ld_res, out, ld)
+  if (m > 64 && slabs < (1 << 16)) {
+    if ((long long)((m + 255) / 256) * ((n + 255) / 256) >= 256) TILE(2, 4, 4, 2);
+    TILE(2, 2, 2, 2);
+  }
+#undef TILE
   const unsigned nt = (unsigned)((n + 15) / 16);
 #define FEW(MT_, WAVES_) hipLaunchKernelGGL((mx4_gemm_few_k<T, MT_, WAVES_>), dim3(nt, (m + 16 * MT_ - 1) / (16 * MT_)), dim3(WAVES_ * 64), 0, st, a, as, w, \
                                             ws, m, n, slabs, bias, res, ld_res, out, ld)
