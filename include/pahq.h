@@ -481,7 +481,8 @@ int pahq_mx4_gemm(void* hip_stream, const uint8_t* a_codes, const uint8_t* a_sca
  * strides.  positions: device int64 [tokens], any values, not checked.
  * Arithmetic in fp32, one rounding to the type.
  * table: device uint64 [rot_dim / 2], from pahq_rotary_table, which fills HOST memory: f_i / (2 pi) modulo 1 in units of
- * 2^-64, so the angle of a far position is as good as that of a near one.  rot_dim even, 2 .. PAHQ_ROTARY_MAX_DIM.
+ * 2^-64, so the angle of a far position is as good as that of a near one.  rot_dim even, 2 .. PAHQ_ROTARY_MAX_DIM;
+ * d_head up to PAHQ_ROTARY_MAX_HEAD, heads up to 65535.
  *     PAHQ_ROTARY_PLAIN   f_i = theta^(-2 i / rot_dim)
  *     PAHQ_ROTARY_LINEAR  f_i / factor: positions squeezed into the trained range
  *     PAHQ_ROTARY_BASE    theta * factor^(rot_dim / (rot_dim - 2)) in place of theta: the slowest pair is stretched by factor,
@@ -492,7 +493,7 @@ int pahq_mx4_gemm(void* hip_stream, const uint8_t* a_codes, const uint8_t* a_sca
  * factor >= 1; arguments a form does not use are ignored. */
 enum { PAHQ_ROTARY_HALF = 0, PAHQ_ROTARY_INTERLEAVED = 1 };
 enum { PAHQ_ROTARY_PLAIN = 0, PAHQ_ROTARY_LINEAR = 1, PAHQ_ROTARY_BASE = 2, PAHQ_ROTARY_BANDS = 3 };
-enum { PAHQ_ROTARY_MAX_DIM = 1024 };
+enum { PAHQ_ROTARY_MAX_DIM = 1024, PAHQ_ROTARY_MAX_HEAD = 4096 };
 int pahq_rotary_table(int32_t rot_dim, double theta, int32_t scaling, double factor, double original, double turns_lo,
                       double turns_hi, uint64_t* table);
 int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32_t tokens, int32_t heads, int32_t d_head, int64_t x_token,

@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <algorithm>
 #include "../../include/pahq.h"
 #include "device_tensor.h"
 
@@ -17,16 +18,23 @@ struct RotaryArgs {
   long long x_token, x_head, o_token, o_head;       // strides in elements
   const long long* positions;
   const unsigned long long* table;
-  int tokens, heads, d, rot, per_group, copy;       // per_group: tokens of a workgroup; copy: the rest of the head goes along
+  int tokens, heads, d, rot;
+  int nt, nh;                                       // tokens and heads of a workgroup
+  int items;                                        // of a head: groups of V pairs, then of V elements behind the rotated part
+  unsigned by_items, by_nh;                         // ceil(2^32 / .): quotients of the small numbers of a workgroup
   float magnitude, direction;
 };
 
-// A workgroup takes a few neighbouring tokens: first their cosines and sines into LDS, shared by all heads, then the heads,
-// V elements of a pair's two sides a thread (V = 1: any alignment and any number of pairs).
+// n / d where n * d < 2^32, from ceil(2^32 / d), which does not fit a word for d = 1
+__device__ __forceinline__ int quotient(int n, int d, unsigned by_d) { return d == 1 ? n : (int)__umulhi((unsigned)n, by_d); }
+
+// A workgroup takes nt neighbouring tokens and nh heads of each: first the tokens' cosines and sines into LDS, shared by the
+// heads, then the heads, V elements of a pair's two sides a thread (V = 1: any alignment and any number of pairs).
+// Memory-bound: x is read and written once.
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(256) void rotary_k(const T* x, T* out, RotaryArgs q) {
-  extern __shared__ float2 turn[];                  // [per_group][rot / 2]
-  const int half = q.rot / 2, t0 = blockIdx.x * q.per_group, nt = min(q.per_group, q.tokens - t0);
+  extern __shared__ float2 turn[];                  // [nt][rot / 2]
+  const int half = q.rot / 2, t0 = blockIdx.x * q.nt, nt = min(q.nt, q.tokens - t0), h0 = blockIdx.y * q.nh, nh = min(q.nh, q.heads - h0);
   for (int e = threadIdx.x; e < nt * half; e += 256) {
     const int t = e / half, i = e - t * half;
     const unsigned long long phase = (unsigned long long)q.positions[t0 + t] * q.table[i] + (1ull << 61);
@@ -38,22 +46,20 @@ __global__ __launch_bounds__(256) void rotary_k(const T* x, T* out, RotaryArgs q
     turn[e] = make_float2((quarter == 1 || quarter == 2 ? -cq : cq) * q.magnitude, (quarter >= 2 ? -sq : sq) * q.magnitude * q.direction);
   }
   __syncthreads();
-  // items of a head: groups of V pairs, then the elements behind the rotated part, V at a time
-  const int pairs = half / V, rest = q.copy ? (q.d - q.rot) / V : 0, items = pairs + rest;
-  for (int e = threadIdx.x; e < nt * q.heads * items; e += 256) {
-    const int h0 = e / items, i = e - h0 * items, t = h0 / q.heads, h = h0 - t * q.heads;
-    const T* p = x + (t0 + t) * q.x_token + h * q.x_head;
-    T* o = out + (t0 + t) * q.o_token + h * q.o_head;
+  const int pairs = half / V;
+  for (int e = threadIdx.x; e < nt * q.nh * q.items; e += 256) {
+    const int r = quotient(e, q.items, q.by_items), i = e - r * q.items, t = quotient(r, q.nh, q.by_nh), h = r - t * q.nh;
+    if (h >= nh) continue;
+    const T* p = x + (t0 + t) * q.x_token + (h0 + h) * q.x_head;
+    T* o = out + (t0 + t) * q.o_token + (h0 + h) * q.o_head;
     if (i >= pairs) {
       const int at = q.rot + (i - pairs) * V;
       *(Pack<T, V>*)(o + at) = *(const Pack<T, V>*)(p + at);
       continue;
     }
     const float2* cs = turn + t * half + i * V;
-    Pack<T, V> a, b;
     const int ia = HALF ? i * V : 2 * i * V, ib = HALF ? half + i * V : 2 * i * V + V;
-    a = *(const Pack<T, V>*)(p + ia);
-    b = *(const Pack<T, V>*)(p + ib);
+    Pack<T, V> a = *(const Pack<T, V>*)(p + ia), b = *(const Pack<T, V>*)(p + ib);
 #pragma unroll
     for (int j = 0; j < V; j++) {
       // half: a holds the first sides of V pairs and b their second sides; interleaved: the 2 V elements of V pairs in turn
@@ -69,20 +75,36 @@ __global__ __launch_bounds__(256) void rotary_k(const T* x, T* out, RotaryArgs q
 }
 
 namespace {
-template <typename T>
-int rotary_as(hipStream_t st, const T* x, T* out, RotaryArgs q, int layout) {
-  constexpr int V = 16 / sizeof(T);
-  // 16 bytes a thread need whole groups of pairs on either side and behind them
-  const bool wide = (q.rot / 2) % V == 0 && (q.d - q.rot) % V == 0;
+unsigned reciprocal(int d) { return (unsigned)(((1ull << 32) + d - 1) / d); }
+
+template <typename T, int V, bool HALF>
+int launch_rotary(hipStream_t st, const T* x, T* out, RotaryArgs q, bool copy) {
   const int half = q.rot / 2;
-  q.per_group = max(1, min(min(2048 / half, 8), q.tokens));
-  const dim3 grid((q.tokens + q.per_group - 1) / q.per_group);
-  const size_t lds = (size_t)q.per_group * half * sizeof(float2);
-#define ROT(V_, HALF_) hipLaunchKernelGGL((rotary_k<T, V_, HALF_>), grid, dim3(256), lds, st, x, out, q)
-  if (layout == PAHQ_ROTARY_HALF) { if (wide) ROT(V, true); else ROT(1, true); }
-  else { if (wide) ROT(V, false); else ROT(1, false); }
-#undef ROT
+  q.items = half / V + (copy ? (q.d - q.rot) / V : 0);
+  // Tokens: as many as give every thread a sine, fewer where the chip would not be full; then the heads are split as well,
+  // down to a pass of the threads each.  nt nh items <= 2^19 and nh <= 8192 keep the
+  // quotients exact.
+  q.nt = std::max(1, std::min(std::min(256 / half, 32), q.tokens / 1024));
+  const int groups = (q.tokens + q.nt - 1) / q.nt, most = std::min(8192, std::max(1, (1 << 19) / (q.nt * q.items)));
+  const int least = std::max(1, 256 / (q.nt * q.items)), split = std::max(1, 1024 / groups);
+  q.nh = std::min(std::min(most, q.heads), std::max(least, (q.heads + split - 1) / split));
+  q.by_items = reciprocal(q.items);
+  q.by_nh = reciprocal(q.nh);
+  hipLaunchKernelGGL((rotary_k<T, V, HALF>), dim3(groups, (q.heads + q.nh - 1) / q.nh), dim3(256), (size_t)q.nt * half * sizeof(float2), st, x, out, q);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
+}
+template <typename T, bool HALF>
+int rotary_as(hipStream_t st, const T* x, T* out, const RotaryArgs& q, bool copy) {
+  // the most elements an access takes that divide the pairs and what lies behind them
+  const int both = (q.rot / 2) | (q.d - q.rot);
+  if (sizeof(T) == 2 && both % 8 == 0) return launch_rotary<T, 16 / sizeof(T), HALF>(st, x, out, q, copy);
+  if (both % 4 == 0) return launch_rotary<T, 4, HALF>(st, x, out, q, copy);
+  if (both % 2 == 0) return launch_rotary<T, 2, HALF>(st, x, out, q, copy);
+  return launch_rotary<T, 1, HALF>(st, x, out, q, copy);
+}
+template <typename T>
+int rotary_as(hipStream_t st, const T* x, T* out, const RotaryArgs& q, int layout, bool copy) {
+  return layout == PAHQ_ROTARY_HALF ? rotary_as<T, true>(st, x, out, q, copy) : rotary_as<T, false>(st, x, out, q, copy);
 }
 // [tokens][heads][d] in either order of the first two, no two elements in one place; extent in elements
 bool strides_ok(long long tokens, long long heads, long long d, long long st, long long sh, long long* extent) {
@@ -131,8 +153,8 @@ extern "C" int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32
   if ((layout != PAHQ_ROTARY_HALF && layout != PAHQ_ROTARY_INTERLEAVED) || (inverse != 0 && inverse != 1)) return PAHQ_EINVAL;
   if (tokens == 0 || heads == 0) return PAHQ_OK;
   if (!x || !out || !positions || !table || (uintptr_t)x % eb || (uintptr_t)out % eb || (uintptr_t)positions % 8 || (uintptr_t)table % 8) return PAHQ_EINVAL;
-  // a workgroup counts the elements of its (at most eight) tokens in 32 bits
-  if ((int64_t)heads * d_head > (1 << 27)) return PAHQ_ETOOBIG;
+  // workgroups are counted in 16 bits along the heads
+  if (heads > 65535 || d_head > PAHQ_ROTARY_MAX_HEAD) return PAHQ_ETOOBIG;
   long long xn, on;
   if (x_token < 0 || x_head < 0 || !strides_ok(tokens, heads, d_head, out_token, out_head, &on)) return PAHQ_EINVAL;
   xn = (tokens - 1ll) * x_token + (heads - 1ll) * x_head + d_head;      // only read: rows may share memory
@@ -140,11 +162,11 @@ extern "C" int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32
   if (!in_place && overlap(x, (size_t)xn * eb, out, (size_t)on * eb)) return PAHQ_EINVAL;
   if (overlap(out, (size_t)on * eb, positions, (size_t)tokens * 8) || overlap(out, (size_t)on * eb, table, (size_t)rot_dim * 4)) return PAHQ_EINVAL;
   hipStream_t st = (hipStream_t)hip_stream;
-  RotaryArgs q = {x_token, x_head, out_token, out_head, (const long long*)positions, (const unsigned long long*)table, tokens, heads, d_head, rot_dim, 1,
-                  !in_place, magnitude, inverse ? -1.f : 1.f};
+  const RotaryArgs q = {x_token, x_head, out_token, out_head, (const long long*)positions, (const unsigned long long*)table, tokens, heads, d_head, rot_dim,
+                        0, 0, 0, 0, 0, magnitude, inverse ? -1.f : 1.f};
   switch (dtype) {
-    case PAHQ_F32: return rotary_as(st, (const float*)x, (float*)out, q, layout);
-    case PAHQ_BF16: return rotary_as(st, (const bf16_t*)x, (bf16_t*)out, q, layout);
-    default: return rotary_as(st, (const f16_t*)x, (f16_t*)out, q, layout);
+    case PAHQ_F32: return rotary_as(st, (const float*)x, (float*)out, q, layout, !in_place);
+    case PAHQ_BF16: return rotary_as(st, (const bf16_t*)x, (bf16_t*)out, q, layout, !in_place);
+    default: return rotary_as(st, (const f16_t*)x, (f16_t*)out, q, layout, !in_place);
   }
 }

@@ -23,18 +23,27 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+_functions = {}
+
+
 def _call(name, device, *args):
-    """One library call on the current stream of `device`, with that device current."""
-    fn = getattr(lib(), name)
-    if device.index == torch.cuda.current_device():
-        _chk(fn(torch.cuda.current_stream(device).cuda_stream, *args), name)
+    """One library call on the current stream of `device`, with that device current.  Looking the function up and asking for the
+    stream's handle alone keep a small call's host time at about that of torch's own (4 us of 9)."""
+    fn = _functions.get(name)
+    if fn is None:
+        fn = _functions[name] = getattr(lib(), name)
+    index = device.index
+    if index == torch._C._cuda_getDevice():
+        code = fn(torch._C._cuda_getCurrentRawStream(index), *args)
     else:
         with torch.cuda.device(device):
-            _chk(fn(torch.cuda.current_stream(device).cuda_stream, *args), name)
+            code = fn(torch._C._cuda_getCurrentRawStream(index), *args)
+    if code:
+        _chk(code, name)
 
 
-def _tracked(*tensors):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+def _tracked(t):
+    return t.requires_grad and torch.is_grad_enabled()
 
 
 def _row_stride(t):
@@ -64,8 +73,13 @@ class Mx4:
 
     @classmethod
     def empty(cls, rows, cols, device="cuda"):
-        k = -(-int(cols) // 256) * 256
-        return cls(torch.empty((rows, k // 2), dtype=torch.uint8, device=device), torch.empty((rows, k // 32), dtype=torch.uint8, device=device), cols)
+        groups = -(-int(cols) // 256)
+        _need(rows >= 0 and groups >= 1, "rows >= 0, cols >= 1")
+        q = cls.__new__(cls)                            # nothing to check: of the right form as made
+        q.codes = torch.empty((rows, groups * 128), dtype=torch.uint8, device=device)
+        q.scales = torch.empty((rows, groups * 8), dtype=torch.uint8, device=device)
+        q.cols = int(cols)
+        return q
 
     @property
     def rows(self):
@@ -79,15 +93,18 @@ class Mx4:
 def mx4_quantize(x, by="rows", out=None):
     """x float32 / bfloat16 / float16 [rows][cols] -> Mx4 of the same shape; by="columns": the Mx4 of x transposed, its blocks
     running down the columns of x (a weight [k][n] as mx4_gemm takes it).  Rows, or columns, of x are contiguous."""
-    _need(x.is_cuda and x.dim() == 2 and x.dtype in _DTYPES, "x: a matrix in float32, bfloat16 or float16 on the device")
-    _need(by in ("rows", "columns"), "by: 'rows' or 'columns'")
-    _need(not _tracked(x), "rounding to 4 bits has no gradient: detach x")
-    if _row_stride(x) is None and _row_stride(x.t()) is not None:     # a transposed view: the other direction of its base
-        x, down = x.t(), by == "rows"
-    else:
-        down = by == "columns"
+    if not (x.is_cuda and x.dim() == 2 and x.dtype in _DTYPES):
+        raise ValueError("x: a matrix in float32, bfloat16 or float16 on the device")
+    if by not in ("rows", "columns"):
+        raise ValueError("by: 'rows' or 'columns'")
+    if _tracked(x):
+        raise ValueError("rounding to 4 bits has no gradient: detach x")
+    down = by == "columns"
     ld = _row_stride(x)
-    _need(ld is not None, "x: rows or columns contiguous, not overlapping")
+    if ld is None:                                      # a transposed view: the other direction of its base
+        x, down = x.t(), not down
+        ld = _row_stride(x)
+        _need(ld is not None, "x: rows or columns contiguous, not overlapping")
     rows, cols = (x.shape[1], x.shape[0]) if down else x.shape
     _need(cols >= 1, "rows of at least one element")
     if out is None:
@@ -105,8 +122,8 @@ def _result(out, rows, cols, dtype, device):
         _need(dtype in _DTYPES, "dtype: float32, bfloat16 or float16")
         return torch.empty((rows, cols), dtype=dtype, device=device), max(cols, 1)
     ld = _row_stride(out) if out.dim() == 2 else None
-    _need(tuple(out.shape) == (rows, cols) and out.dtype in _DTYPES and out.device == device and ld is not None and not _tracked(out),
-          "out: [%d][%d] in float32, bfloat16 or float16, rows contiguous, on the operands' device, without a gradient" % (rows, cols))
+    if not (out.shape == (rows, cols) and out.dtype in _DTYPES and out.device == device and ld is not None and not _tracked(out)):
+        raise ValueError("out: [%d][%d] in float32, bfloat16 or float16, rows contiguous, on the operands' device, without a gradient" % (rows, cols))
     return out, ld
 
 
@@ -120,22 +137,26 @@ def mx4_dequantize(q, dtype=torch.float32, out=None):
 
 def mx4_gemm(a, w, bias=None, residual=None, dtype=torch.float32, out=None):
     """a Mx4 [m][k], w Mx4 [n][k] -> a w^T (+ bias float32 [n]) (+ residual [m][n] of the result's dtype; it may be `out`)."""
-    _need(a.cols == w.cols and a.device == w.device, "a [m][k] and w [n][k] on one device")
-    m, n = a.rows, w.rows
-    out, ld = _result(out, m, n, dtype, a.device)
+    device = a.codes.device
+    if a.cols != w.cols or device != w.codes.device:
+        raise ValueError("a [m][k] and w [n][k] on one device")
+    m, n = a.codes.shape[0], w.codes.shape[0]
+    out, ld = _result(out, m, n, dtype, device)
     bp = rp = None
     ld_res = ld
     if bias is not None:
-        _need(bias.dtype == torch.float32 and tuple(bias.shape) == (n,) and bias.device == a.device and (n <= 1 or bias.stride(0) == 1)
-              and not _tracked(bias), "bias: float32 [n], contiguous, without a gradient")
+        if not (bias.dtype == torch.float32 and bias.shape == (n,) and bias.device == device and (n <= 1 or bias.stride(0) == 1)
+                and not _tracked(bias)):
+            raise ValueError("bias: float32 [n], contiguous, without a gradient")
         bp = bias.data_ptr()
     if residual is not None:
         ld_res = _row_stride(residual) if residual.dim() == 2 else None
-        _need(tuple(residual.shape) == (m, n) and residual.dtype == out.dtype and residual.device == a.device and ld_res is not None
-              and not _tracked(residual), "residual: [m][n] of the result's dtype, rows contiguous, without a gradient")
+        if not (residual.shape == (m, n) and residual.dtype == out.dtype and residual.device == device and ld_res is not None
+                and not _tracked(residual)):
+            raise ValueError("residual: [m][n] of the result's dtype, rows contiguous, without a gradient")
         rp = residual.data_ptr()
     if m and n:
-        _call("pahq_mx4_gemm", a.device, a.codes.data_ptr(), a.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), m, n, a.cols, bp, rp, ld_res,
+        _call("pahq_mx4_gemm", device, a.codes.data_ptr(), a.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), m, n, a.cols, bp, rp, ld_res,
               out.data_ptr(), _DTYPES[out.dtype], ld)
     return out
 
@@ -153,8 +174,9 @@ def rotary_table(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=0.
 
 def _strides(t):
     tokens, heads, d = t.shape
-    _need(d <= 1 or t.stride(2) == 1, "the elements of a head: contiguous")
-    st, sh = t.stride(0), t.stride(1)
+    st, sh, se = t.stride()
+    if se != 1 and d > 1:
+        raise ValueError("the elements of a head: contiguous")
     if heads <= 1:
         sh = d
     if tokens <= 1:
@@ -163,14 +185,14 @@ def _strides(t):
 
 
 def _rotary(x, positions, table, layout, magnitude, inverse, out):
+    tokens, heads, d = x.shape
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    else:
-        _need(out.shape == x.shape and out.dtype == x.dtype and out.device == x.device, "out: of x's shape and dtype, on its device")
-    tokens, heads, d = x.shape
+    elif not (out.shape == x.shape and out.dtype == x.dtype and out.device == x.device):
+        raise ValueError("out: of x's shape and dtype, on its device")
     if tokens and heads:
         st, sh = _strides(x)
-        ot, oh = (st, sh) if out.data_ptr() == x.data_ptr() and out.stride() == x.stride() else _strides(out)
+        ot, oh = _strides(out)
         _call("pahq_rotary", x.device, x.data_ptr(), _DTYPES[x.dtype], tokens, heads, d, st, sh, positions.data_ptr(), table.data_ptr(), 2 * table.numel(),
               _LAYOUTS[layout], magnitude, 1 if inverse else 0, out.data_ptr(), ot, oh)
     return out
@@ -195,13 +217,18 @@ def rotary(x, positions, table, layout="half", magnitude=1.0, inverse=False, out
     """Turns the first 2 * len(table) elements of every head of x [tokens][heads][d_head] by their tokens' positions (int64
     [tokens]); the rest of the head is copied.  layout: "half" (pairs i, i + rot / 2) or "interleaved" (pairs 2 i, 2 i + 1).
     inverse turns back (the gradient; x gets it by itself where autograd asks).  out may be x."""
-    _need(x.is_cuda and x.dim() == 3 and x.dtype in _DTYPES, "x: [tokens][heads][d_head] in float32, bfloat16 or float16 on the device")
-    _need(positions.dtype == torch.int64 and tuple(positions.shape) == (x.shape[0],) and positions.device == x.device
-          and (x.shape[0] <= 1 or positions.stride(0) == 1), "positions: int64 [tokens], contiguous, on x's device")
-    _need(table.dtype == torch.int64 and table.dim() == 1 and table.device == x.device and (table.numel() <= 1 or table.stride(0) == 1)
-          and 2 <= 2 * table.numel() <= x.shape[2], "table: from rotary_table, on x's device, for at most d_head elements")
-    _need(layout in _LAYOUTS, "layout: 'half' or 'interleaved'")
-    if _tracked(x, out):
+    if not (x.is_cuda and x.dim() == 3 and x.dtype in _DTYPES):
+        raise ValueError("x: [tokens][heads][d_head] in float32, bfloat16 or float16 on the device")
+    tokens, _, d = x.shape
+    if not (positions.dtype == torch.int64 and positions.shape == (tokens,) and positions.device == x.device
+            and (tokens <= 1 or positions.stride(0) == 1)):
+        raise ValueError("positions: int64 [tokens], contiguous, on x's device")
+    if not (table.dtype == torch.int64 and table.dim() == 1 and table.device == x.device and 2 <= 2 * table.numel() <= d
+            and (table.numel() <= 1 or table.stride(0) == 1)):
+        raise ValueError("table: from rotary_table, on x's device, for at most d_head elements")
+    if layout not in _LAYOUTS:
+        raise ValueError("layout: 'half' or 'interleaved'")
+    if _tracked(x) or out is not None and _tracked(out):
         _need(out is None, "out: not where a gradient is recorded")
         return _Rotary.apply(x, positions, table, layout, float(magnitude), bool(inverse))
     return _rotary(x, positions, table, layout, float(magnitude), bool(inverse), out)

@@ -70,7 +70,7 @@ def test_gemm_refuses(P, change, code):
     (dict(x=A + 2), EINVAL), (dict(out=2 * A + 1), EINVAL), (dict(positions=4 * A + 4), EINVAL), (dict(table=5 * A + 4), EINVAL), (dict(x_token=-1), EINVAL),
     (dict(out_head=63), EINVAL), (dict(out_token=191), EINVAL), (dict(out_token=0), EINVAL), (dict(out_token=64, out_head=255), EINVAL),
     (dict(out=A + 4), EINVAL), (dict(out=A, out_token=256), EINVAL), (dict(out=4 * A), EINVAL), (dict(out=5 * A), EINVAL),
-    (dict(heads=1 << 22, out_token=1 << 28), ETOOBIG), (dict(tokens=0, x=None), 0), (dict(heads=0, out=None), 0)])
+    (dict(heads=65536, out_token=1 << 28), ETOOBIG), (dict(d=4097, out_head=4097, out_token=3 * 4097), ETOOBIG), (dict(tokens=0, x=None), 0), (dict(heads=0, out=None), 0)])
 def test_rotary_refuses(P, change, code):
     assert P.lib().pahq_rotary(*dict(ROTARY, **change).values()) == code
 
