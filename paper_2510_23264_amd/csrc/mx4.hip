@@ -120,6 +120,9 @@ __device__ __forceinline__ void tile_of(int wg, int mt, int nt, int& tm, int& tn
   tm = band * 8 + in - tn * high;
 }
 
+// The instruction's operand type is wide enough for 8-bit elements; 4-bit ones are its first half.
+__device__ __forceinline__ v8i four_bits(int4 v) { return (v8i){v.x, v.y, v.z, v.w, 0, 0, 0, 0}; }
+
 // Few rows: 16 * MT rows x 16 columns a workgroup, the sum over k split over its waves (slab s of 256 elements to wave s
 // mod WAVES) and joined in LDS in the order of the waves, so results do not depend on timing.  Operands come straight from
 // global memory: a lane reads two neighbouring blocks of its row with their scales, which are one halfword, and the four
@@ -177,65 +180,83 @@ __global__ __launch_bounds__(WAVES * 64) void mx4_gemm_few_k(const uint8_t* a, c
 }
 
 // Tiles through LDS.  AF x WF products of 32 x 32 (V_MFMA_SCALE_F32_32X32X64_F8F6F4) a wave, WM x WN waves; slabs of 256
-// elements of k (128 bytes of codes a row) in two stages, requested one slab ahead straight into LDS.  In a slab a lane takes
-// four neighbouring blocks of its row, one a step, so the bytes of one word of scales serve its four steps through the
-// instruction's byte selector.  Row AF j + f of a wave's A rows (WF j + f of its W rows) is MFMA row j of fragment f:
-// a lane then holds WF neighbouring columns of a result row, and one LDS read brings the scales of all fragments.
-// LDS holds fragment f's rows next to each other (any order can be loaded) with the 16-byte chunks of a row XOR-swizzled
-// by half the row's place, so that 16 lanes cover all 64 banks.  Scales are 8 bytes of a row a slab: fetched by slabs they
-// would cost a cache line of 128 bytes each, so a thread fetches those of one row for four slabs at a time.
-template <int AF, int WF, int WM, int WN>
+// elements of k (128 bytes of codes a row) in NS stages, requested up to NS slabs ahead straight into LDS.  In a slab a lane
+// takes four neighbouring blocks of its row, one a step, so the bytes of one word of scales serve its four steps through the
+// instruction's byte selector.  LDS holds a row's 16-byte chunks XOR-swizzled by half the row's number, so that 16 lanes cover
+// all 64 banks.  Scales are 8 bytes of a row a slab; they come by pairs of slabs, 16 bytes a request.
+// The fragments of a step are read while the step before it multiplies, those of the next slab's first step too: the wait for
+// that slab and the barrier stand in front of the last step, when every fragment of this slab is in registers and its stage
+// is free for the next request.
+template <int AF, int WF, int WM, int WN, int NS>
 struct Mx4Tile {
-  static constexpr int BM = AF * 32 * WM, BN = WF * 32 * WN, THREADS = WM * WN * 64, ROWS = BM + BN;
-  static constexpr int STAGE = ROWS * 128, SCALES = ROWS * 32;
-  static constexpr int LDS = 2 * STAGE + SCALES;
-  static_assert(ROWS == THREADS, "a thread fetches the scales of one row");
+  static constexpr int BM = AF * 32 * WM, BN = WF * 32 * WN, THREADS = WM * WN * 64, WAVES = WM * WN, ROWS = BM + BN;
+  static constexpr int STAGE = ROWS * 128, PAIRS = NS > 2 ? 4 : 2, IN = NS * STAGE + PAIRS * ROWS * 16;
+  static constexpr int STRIDE = WF * 32 + 4, OUT = WAVES * 32 * STRIDE * 4;       // a fragment's 32 rows of a wave's results, in floats
+  static constexpr int LDS = IN > OUT ? IN : OUT;
+  static constexpr int REQUESTS = ROWS * 8 / THREADS;        // of a wave and slab, besides the scales
+  static_assert(ROWS == THREADS && LDS <= 160 * 1024, "a thread requests the scales of one row");
+  static_assert(BM % (THREADS / 8) == 0 && BM % 64 == 0, "a request belongs to one operand");
 };
-template <typename T, int AF, int WF, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64) void mx4_gemm_tile_k(const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n,
-                                                              int slabs, int mt, int nt, const float* bias, const T* res, long long ld_res, T* out,
-                                                              long long ld) {
-  typedef Mx4Tile<AF, WF, WM, WN> C;
+template <typename T, int AF, int WF, int WM, int WN, int NS>
+__global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void mx4_gemm_tile_k(const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws,
+                                                                            int m, int n, int slabs, int mt, int nt, const float* bias, const T* res,
+                                                                            long long ld_res, T* out, long long ld) {
+  typedef Mx4Tile<AF, WF, WM, WN, NS> C;
   extern __shared__ __align__(16) uint8_t lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 31, g = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, g = lane >> 5;
   const int wm = wave / WN, wn = wave % WN;
   int tm, tn;
   tile_of(blockIdx.x, mt, nt, tm, tn);
   if (tm >= mt) return;
-  const int m0 = tm * C::BM, n0 = tn * C::BN;
-  const long long row_bytes = (long long)slabs * 128;
-  // this lane's eight chunks of a stage: place (slot, position) of LDS, and where in the tile's rows the bytes come from
-  constexpr int L = 8;
+  const int m0 = tm * C::BM, n0 = tn * C::BN, last_m = m - 1 - m0, last_n = n - 1 - n0;
+  const uint32_t row_bytes = (uint32_t)slabs * 128u;
+  // where this lane's chunks of a stage come from, in the tile's rows (rows past the end: the last one, not stored)
+  constexpr int L = C::REQUESTS;
   uint32_t off[L];
 #pragma unroll
   for (int i = 0; i < L; i++) {
-    const int slot = (i * (C::THREADS / 64) + wave) * 8 + (lane >> 3), c = (lane & 7) ^ ((slot >> 1) & 7);
-    int row;
-    if (slot < C::BM) row = min((slot / (AF * 32)) * (AF * 32) + (slot & 31) * AF + (slot / 32) % AF, m - 1 - m0);
-    else {
-      const int q = slot - C::BM;
-      row = min((q / (WF * 32)) * (WF * 32) + (q & 31) * WF + (q / 32) % WF, n - 1 - n0);
-    }
-    off[i] = (uint32_t)(row * row_bytes + c * 16);
+    const int place = (i * C::WAVES + wave) * 8, c = (lane & 7) ^ (lane >> 4) ^ ((place >> 1) & 4);
+    const int row = place + (lane >> 3) - (i * C::WAVES * 8 < C::BM ? 0 : C::BM);
+    off[i] = (uint32_t)min(row, i * C::WAVES * 8 < C::BM ? last_m : last_n) * row_bytes + c * 16;
   }
-  const uint8_t* ab = a + m0 * row_bytes;
-  const uint8_t* wb = w + n0 * row_bytes;
-  const uint32_t stage0 = lds_addr_of(lds);
+  const uint8_t* const ab = a + (long long)m0 * row_bytes;
+  const uint8_t* const wb = w + (long long)n0 * row_bytes;
+  // and its row's scales
+  const bool of_a = wave * 64 < C::BM;
+  const uint8_t* const sb = of_a ? as + (long long)m0 * slabs * 8 : ws + (long long)n0 * slabs * 8;
+  const int srow = wave * 64 - (of_a ? 0 : C::BM), slast = of_a ? last_m : last_n;
+  const uint32_t soff = (uint32_t)min(srow + lane, slast) * (uint32_t)slabs * 8u;
+  const uint32_t stage0 = lds_addr_of(lds) + wave * 1024, scales0 = stage0 + NS * C::STAGE;
+  // a pair of slabs behind the last full one starts a slab early, so that nothing behind the row is read
+  const auto pair_start = [&](int s) { return max(0, min(s & ~1, slabs - 2)); };
+  const auto request_scales = [&](int s) {
+    slab_load16s(sb + pair_start(s) * 8ll, soff, scales0 + ((s >> 1) & (C::PAIRS - 1)) * (C::ROWS * 16));
+  };
   const auto request = [&](int s) {
-    const uint32_t base = stage0 + (s & 1) * C::STAGE + wave * 1024;
+    const uint32_t to = stage0 + (s & (NS - 1)) * C::STAGE;
 #pragma unroll
-    for (int i = 0; i < L; i++)
-      slab_load16s((i * (C::THREADS / 64) * 8 < C::BM ? ab : wb) + (long long)s * 128, off[i], base + i * C::THREADS * 16);
+    for (int i = 0; i < L; i++) slab_load16s((i * C::WAVES * 8 < C::BM ? ab : wb) + s * 128ll, off[i], to + i * C::THREADS * 16);
   };
-  static_assert(C::BM % (C::THREADS / 8) == 0, "a request belongs to one operand");
-  // scales of row tid of the tile, four slabs: words [slab][half of the slab][row] in LDS
-  const uint8_t* sp = tid < C::BM ? as + (long long)(m0 + min(tid, m - 1 - m0)) * slabs * 8 : ws + (long long)(n0 + min(tid - C::BM, n - 1 - n0)) * slabs * 8;
-  uint2 sc[4];
-  const auto fetch_scales = [&](int s) {
+  // fragments and scales of this wave
+  const uint8_t* const fa = lds + (wm * (AF * 32) + j) * 128;
+  const uint8_t* const fw = lds + (C::BM + wn * (WF * 32) + j) * 128;
+  const uint8_t* const fs = lds + NS * C::STAGE + g * 4 + j * 16;
+  int4 af[2][AF], wf[2][WF];
+  int asc[2][AF], wsc[2][WF];
+  const auto read = [&](int s, int S, int to) {
+    const int at = (s & (NS - 1)) * C::STAGE + (((4 * g + S) ^ ((j >> 1) & 7)) * 16);
 #pragma unroll
-    for (int i = 0; i < 4; i++) sc[i] = s + i < slabs ? *(const uint2*)(sp + (long long)(s + i) * 8) : make_uint2(0, 0);
+    for (int x = 0; x < AF; x++) af[to][x] = *(const int4*)(fa + at + x * 32 * 128);
+#pragma unroll
+    for (int y = 0; y < WF; y++) wf[to][y] = *(const int4*)(fw + at + y * 32 * 128);
   };
-  uint32_t* const scl = (uint32_t*)(lds + 2 * C::STAGE);
+  const auto read_scales = [&](int s, int to) {
+    const uint8_t* const p = fs + ((s >> 1) & (C::PAIRS - 1)) * (C::ROWS * 16) + ((s - pair_start(s)) & 1) * 8;
+#pragma unroll
+    for (int x = 0; x < AF; x++) asc[to][x] = *(const int*)(p + (wm * (AF * 32) + x * 32) * 16);
+#pragma unroll
+    for (int y = 0; y < WF; y++) wsc[to][y] = *(const int*)(p + (C::BM + wn * (WF * 32) + y * 32) * 16);
+  };
   v16f acc[AF][WF];
 #pragma unroll
   for (int x = 0; x < AF; x++)
@@ -243,84 +264,111 @@ __global__ __launch_bounds__(WM * WN * 64) void mx4_gemm_tile_k(const uint8_t* a
     for (int y = 0; y < WF; y++)
 #pragma unroll
       for (int i = 0; i < 16; i++) acc[x][y][i] = 0.f;
-
-  fetch_scales(0);
-  request(0);
-  for (int s = 0; s < slabs; s++) {
-    wait_vm_barrier<0>();              // slab s is there for every wave, and none reads the stage of slab s - 1 any more
-    if ((s & 3) == 0) {
+  const auto multiply = [&](auto sel, int from, int scales) {
+    constexpr int S = decltype(sel)::value;
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        scl[(i * 2 + 0) * C::ROWS + tid] = sc[i].x;
-        scl[(i * 2 + 1) * C::ROWS + tid] = sc[i].y;
-      }
-      wait_vm_barrier<63>();
-      if (s + 4 < slabs) fetch_scales(s + 4);
-    }
-    if (s + 1 < slabs) request(s + 1);
-    const uint8_t* const sa = lds + (s & 1) * C::STAGE + wm * (AF * 32) * 128;
-    const uint8_t* const sw = lds + (s & 1) * C::STAGE + (C::BM + wn * (WF * 32)) * 128;
-    const uint32_t* const sc_s = scl + ((s & 3) * 2 + g) * C::ROWS;
-    int asc[AF], wsc[WF];
-#pragma unroll
-    for (int x = 0; x < AF; x++) asc[x] = (int)sc_s[wm * (AF * 32) + j * AF + x];
-#pragma unroll
-    for (int y = 0; y < WF; y++) wsc[y] = (int)sc_s[C::BM + wn * (WF * 32) + j * WF + y];
-    const auto step = [&](auto sel) {
-      constexpr int S = decltype(sel)::value;
-      v8i af[AF], wf[WF];
-      const int at = j * 128 + (((4 * g + S) ^ ((j >> 1) & 7)) * 16);       // 32 rows a fragment: the swizzle is the lane's own
-#pragma unroll
-      for (int x = 0; x < AF; x++) {
-        const int4 v = *(const int4*)(sa + x * 32 * 128 + at);
-        af[x] = (v8i){v.x, v.y, v.z, v.w, 0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int y = 0; y < WF; y++) {
-        const int4 v = *(const int4*)(sw + y * 32 * 128 + at);
-        wf[y] = (v8i){v.x, v.y, v.z, v.w, 0, 0, 0, 0};
-      }
+    for (int y = 0; y < WF; y++)
 #pragma unroll
       for (int x = 0; x < AF; x++)
-#pragma unroll
-        for (int y = 0; y < WF; y++)
-          acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(af[x], wf[y], acc[x][y], 4, 4, S, asc[x], S, wsc[y]);
-    };
-    step(Int<0>());
-    step(Int<1>());
-    step(Int<2>());
-    step(Int<3>());
+        acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(four_bits(af[from][x]), four_bits(wf[from][y]), acc[x][y], 4, 4, S, asc[scales][x], S, wsc[scales][y]);
+  };
+
+#pragma unroll 1
+  for (int s = 0; s < min(NS, slabs); s++) {
+    if (slabs == 1) {
+#pragma unroll 1
+      for (int i = 0; i < 4; i++)          // a row has 8 bytes alone: words 0 1 0 1
+        lds_load4s((const float*)sb, (uint32_t)min(srow + i * 16 + (lane >> 2), slast) * 8u + (lane & 1) * 4, scales0 + i * 256);
+    } else if ((s & 1) == 0) request_scales(s);
+    request(s);
   }
-  const int col = n0 + wn * (WF * 32) + j * WF;
-  if (col >= n) return;
-  const bool whole = col + WF <= n;
-  float b[WF];
+  if (slabs >= NS) wait_vm_barrier<(NS - 1) * L + (NS - 2) / 2>();      // NS - 1 slabs are under way behind the first
+  else wait_vm_barrier<0>();
+  read_scales(0, 0);
+  read(0, 0, 0);
+  // One slab.  MORE: slab s + NS is there to be requested (2: with scales), and NS - 2 behind slab s + 1 are under way, half of
+  // them with scales; without it (0) everything is waited for, and behind the last slab the stage read is an old one that
+  // nothing uses.  No branch stands inside: around one the compiler moves the products away from the reads they hide
+  // (8192 x 4096 x 11008 181 us with a branch around the scales' request).
+  const auto slab = [&](int s, auto more) {
+    constexpr int MORE = decltype(more)::value;
+    read(s, 1, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(Int<0>(), 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    read(s, 2, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(Int<1>(), 1, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    read(s, 3, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(Int<2>(), 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vm_barrier<MORE ? (NS - 2) * L + (NS - 2) / 2 : 0>();
+    if (MORE == 2) request_scales(s + NS);
+    if (MORE) request(s + NS);
+    read_scales(s + 1, 1);
+    read(s + 1, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(Int<3>(), 1, 0);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int y = 0; y < WF; y++) b[y] = bias && col + y < n ? bias[col + y] : 0.f;
+    for (int x = 0; x < AF; x++) asc[0][x] = asc[1][x];
 #pragma unroll
-  for (int x = 0; x < AF; x++)
+    for (int y = 0; y < WF; y++) wsc[0][y] = wsc[1][y];
+  };
+  int s = 0;
+#pragma unroll 1
+  for (; s + NS + 1 < slabs; s += 2) {
+    slab(s, Int<2>());
+    slab(s + 1, Int<1>());
+  }
+  if (s + NS < slabs) slab(s++, Int<2>());
+#pragma unroll 1
+  for (; s < slabs; s++) slab(s, Int<0>());
+  // The results go through LDS by fragments of 32 rows, each wave its own, so that a store writes whole rows and its code, with
+  // bias, residual and the edges, stands once.
+  wait_vm_barrier<0>();
+  float* const mine = (float*)lds + wave * 32 * C::STRIDE;
+  constexpr int V = 16 / sizeof(T), ACROSS = WF * 32 / V, DOWN = 64 / ACROSS;      // V columns a lane, DOWN rows a store
+  const int cl = lane % ACROSS * V, col = n0 + wn * (WF * 32) + cl, left = n - col;
+  float b[V];
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-      const int row = m0 + wm * (AF * 32) + (8 * (i / 4) + 4 * g + i % 4) * AF + x;
-      if (row >= m) continue;
+  for (int v = 0; v < V; v++) b[v] = bias && v < left ? bias[col + v] : 0.f;
+#pragma unroll
+  for (int x = 0; x < AF; x++) {
+#pragma unroll
+    for (int y = 0; y < WF; y++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) mine[(8 * (i / 4) + 4 * g + i % 4) * C::STRIDE + y * 32 + j] = acc[x][y][i];
+    __builtin_amdgcn_wave_barrier();
+    const int row0 = m0 + wm * (AF * 32) + x * 32;
+#pragma unroll 2
+    for (int r = lane / ACROSS; r < 32; r += DOWN) {
+      const int row = row0 + r;
+      if (row >= m || left <= 0) break;
       T* const o = out + (long long)row * ld + col;
-      const T* const r = res + (long long)row * ld_res + col;
-      if (whole) {
-        Pack<T, WF> v, q;
-        if (res) q = *(const Pack<T, WF>*)r;
+      const T* const p = res + (long long)row * ld_res + col;
+      if (left >= V) {
+        Pack<T, V> q, u;
+        if (res) u = *(const Pack<T, V>*)p;
 #pragma unroll
-        for (int y = 0; y < WF; y++) {
-          float f = acc[x][y][i] + b[y];
-          if (res) f += as_float(q.v[y]);
-          v.v[y] = from_float<T>(f);
+        for (int v = 0; v < V; v++) {
+          float f = mine[r * C::STRIDE + cl + v] + b[v];
+          if (res) f += as_float(u.v[v]);
+          q.v[v] = from_float<T>(f);
         }
-        *(Pack<T, WF>*)o = v;
+        *(Pack<T, V>*)o = q;
       } else {
-#pragma unroll
-        for (int y = 0; y < WF; y++)
-          if (col + y < n) o[y] = from_float<T>(acc[x][y][i] + b[y] + (res ? as_float(r[y]) : 0.f));
+#pragma unroll 1
+        for (int v = 0; v < left; v++) {
+          const float f = mine[r * C::STRIDE + cl + v] + (bias ? bias[col + v] : 0.f);
+          o[v] = from_float<T>(res ? f + as_float(p[v]) : f);
+        }
       }
     }
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 namespace {
@@ -342,12 +390,12 @@ int values_as(hipStream_t st, const uint8_t* codes, const uint8_t* scales, int r
   hipLaunchKernelGGL(mx4_values_k<T>, dim3(wg), dim3(256), 0, st, (const uint32_t*)codes, scales, rows, cols, groups, out, ld);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
-template <typename T, int AF, int WF, int WM, int WN>
+template <typename T, int AF, int WF, int WM, int WN, int NS>
 int launch_tile(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs, const float* bias,
                 const T* res, long long ld_res, T* out, long long ld) {
-  typedef Mx4Tile<AF, WF, WM, WN> C;
+  typedef Mx4Tile<AF, WF, WM, WN, NS> C;
   const int mt = (m + C::BM - 1) / C::BM, nt = (n + C::BN - 1) / C::BN;
-  const void* fn = (const void*)mx4_gemm_tile_k<T, AF, WF, WM, WN>;
+  const void* fn = (const void*)mx4_gemm_tile_k<T, AF, WF, WM, WN, NS>;
   // more LDS than a launch gets by default: an attribute of the kernel on one device, set once for each
   static std::atomic<bool> set[64];
   int dev = 0;
@@ -356,17 +404,17 @@ int launch_tile(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8
     if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) != hipSuccess) return PAHQ_EHIP;
     set[dev].store(true, std::memory_order_release);
   }
-  hipLaunchKernelGGL((mx4_gemm_tile_k<T, AF, WF, WM, WN>), dim3((mt * nt + 7) / 8 * 8), dim3(C::THREADS), C::LDS, st, a, as, w, ws, m, n, slabs, mt, nt,
+  hipLaunchKernelGGL((mx4_gemm_tile_k<T, AF, WF, WM, WN, NS>), dim3((mt * nt + 7) / 8 * 8), dim3(C::THREADS), C::LDS, st, a, as, w, ws, m, n, slabs, mt, nt,
                      bias, res, ld_res, out, ld);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
 template <typename T>
 int gemm_as(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs, const float* bias,
             const T* res, long long ld_res, T* out, long long ld) {
-#define TILE(AF_, WF_, WM_, WN_) return launch_tile<T, AF_, WF_, WM_, WN_>(st, a, as, w, ws, m, n, slabs, bias, res, ld_res, out, ld)
+#define TILE(AF_, WF_, WM_, WN_, NS_) return launch_tile<T, AF_, WF_, WM_, WN_, NS_>(st, a, as, w, ws, m, n, slabs, bias, res, ld_res, out, ld)
   if (m > 64 && slabs < (1 << 16)) {
-    if ((long long)((m + 255) / 256) * ((n + 255) / 256) >= 256) TILE(2, 4, 4, 2);
-    TILE(2, 2, 2, 2);
+    if ((long long)((m + 255) / 256) * ((n + 255) / 256) >= 256) TILE(2, 4, 4, 2, 2);
+    TILE(2, 2, 2, 2, 4);
   }
 #undef TILE
   const unsigned nt = (unsigned)((n + 15) / 16);
