@@ -106,6 +106,12 @@ __device__ __forceinline__ void wait_vm_barrier() {
   static_assert(N < 64, "vmcnt has six bits");
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
+// The same for a wave that shares its stages with no other.
+template <int N>
+__device__ __forceinline__ void wait_vm_lds() {
+  static_assert(N < 64, "vmcnt has six bits");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
 // The wait in front of a slab with `after` more slabs behind it, in a loop of two or three stages that has requested one slab
 // less than it has stages, each with L loads of this wave.
 template <int NS, int L>

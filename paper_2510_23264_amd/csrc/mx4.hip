@@ -8,6 +8,7 @@
 // additions in any order leave.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <stdlib.h>
 #include <atomic>
 #include "../../include/pahq.h"
 #include "mma_util.h"
@@ -179,39 +180,44 @@ __global__ __launch_bounds__(WAVES * 64) void mx4_gemm_few_k(const uint8_t* a, c
   }
 }
 
-// Tiles through LDS.  AF x WF products of 32 x 32 (V_MFMA_SCALE_F32_32X32X64_F8F6F4) a wave, WM x WN waves; slabs of 256
-// elements of k (128 bytes of codes a row) in NS stages, requested up to NS slabs ahead straight into LDS.  In a slab a lane
-// takes four neighbouring blocks of its row, one a step, so the bytes of one word of scales serve its four steps through the
-// instruction's byte selector.  LDS holds a row's 16-byte chunks XOR-swizzled by half the row's number, so that 16 lanes cover
-// all 64 banks.  Scales are 8 bytes of a row a slab; they come by pairs of slabs, 16 bytes a request.
+// Tiles through LDS.  AF x WF products of 32 x 32 (V_MFMA_SCALE_F32_32X32X64_F8F6F4) a wave, a group of WM x WN waves a tile, KW
+// groups a workgroup that share the sum over k.  Slabs of 256 elements of k (128 bytes of codes a row) come in two stages,
+// straight into LDS, each group's its own.  In a slab a lane takes four neighbouring blocks of
+// its row, one a step, so the bytes of one word of scales serve its four steps through the instruction's byte selector.  LDS
+// holds a row's 16-byte chunks XOR-swizzled by half the row's number, so that 16 lanes cover all 64 banks.  Scales are 8 bytes
+// of a row a slab; they come by pairs of slabs, 16 bytes a request.
 // The fragments of a step are read while the step before it multiplies, those of the next slab's first step too: the wait for
 // that slab and the barrier stand in front of the last step, when every fragment of this slab is in registers and its stage
-// is free for the next request.
-template <int AF, int WF, int WM, int WN, int NS>
+// is free for the next request.  A group of one wave needs no barrier.
+template <int AF, int WF, int WM, int WN, int KW>
 struct Mx4Tile {
-  static constexpr int BM = AF * 32 * WM, BN = WF * 32 * WN, THREADS = WM * WN * 64, WAVES = WM * WN, ROWS = BM + BN;
-  static constexpr int STAGE = ROWS * 128, PAIRS = NS > 2 ? 4 : 2, IN = NS * STAGE + PAIRS * ROWS * 16;
-  static constexpr int STRIDE = WF * 32 + 4, OUT = WAVES * 32 * STRIDE * 4;       // a fragment's 32 rows of a wave's results, in floats
-  static constexpr int LDS = IN > OUT ? IN : OUT;
-  static constexpr int REQUESTS = ROWS * 8 / THREADS;        // of a wave and slab, besides the scales
-  static_assert(ROWS == THREADS && LDS <= 160 * 1024, "a thread requests the scales of one row");
-  static_assert(BM % (THREADS / 8) == 0 && BM % 64 == 0, "a request belongs to one operand");
+  static constexpr int BM = AF * 32 * WM, BN = WF * 32 * WN, WAVES = WM * WN, THREADS = KW * WAVES * 64, ROWS = BM + BN;
+  static constexpr int STAGE = ROWS * 128, GROUP = 2 * (STAGE + ROWS * 16);        // two slabs, two pairs' scales
+  static constexpr int STRIDE = WF * 32 + 8;                                         // floats, of a row of a wave's results
+  static constexpr int OUT = KW * WAVES * (KW > 1 ? AF : 1) * 32 * STRIDE * 4;       // a fragment's rows at a time, or all
+  static constexpr int LDS = KW * GROUP > OUT ? KW * GROUP : OUT;
+  static constexpr int L = ROWS / (8 * WAVES), SL = ROWS / (64 * WAVES);             // requests of a wave: a slab's codes, a pair's scales
+  static_assert(ROWS % (64 * WAVES) == 0 && LDS <= 160 * 1024 && (KW == 1 || WAVES == 1), "whole requests");
+  static_assert(BM % (8 * WAVES) == 0 && BM % 64 == (WAVES == 1 && SL == 1 ? 32 : 0), "a request of codes belongs to one operand");
 };
-template <typename T, int AF, int WF, int WM, int WN, int NS>
-__global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void mx4_gemm_tile_k(const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws,
-                                                                            int m, int n, int slabs, int mt, int nt, const float* bias, const T* res,
-                                                                            long long ld_res, T* out, long long ld) {
-  typedef Mx4Tile<AF, WF, WM, WN, NS> C;
+template <typename T, int AF, int WF, int WM, int WN, int KW>
+__global__ __launch_bounds__(KW * WM * WN * 64, (KW * WM * WN + 3) / 4) void mx4_gemm_tile_k(const uint8_t* a, const uint8_t* as, const uint8_t* w,
+                                                                                          const uint8_t* ws, int m, int n, int slabs, int mt, int nt,
+                                                                                          const float* bias, const T* res, long long ld_res, T* out,
+                                                                                          long long ld) {
+  typedef Mx4Tile<AF, WF, WM, WN, KW> C;
   extern __shared__ __align__(16) uint8_t lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, g = lane >> 5;
-  const int wm = wave / WN, wn = wave % WN;
+  const int lane = threadIdx.x & 63, j = lane & 31, g = lane >> 5, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = any_wave / C::WAVES, wave = any_wave % C::WAVES, wm = wave / WN, wn = wave % WN;
   int tm, tn;
   tile_of(blockIdx.x, mt, nt, tm, tn);
   if (tm >= mt) return;
   const int m0 = tm * C::BM, n0 = tn * C::BN, last_m = m - 1 - m0, last_n = n - 1 - n0;
+  // this group's slabs of k: s0 .. s0 + count - 1
+  const int share = (slabs + KW - 1) / KW, s0 = group * share, count = min(share, slabs - s0);
   const uint32_t row_bytes = (uint32_t)slabs * 128u;
   // where this lane's chunks of a stage come from, in the tile's rows (rows past the end: the last one, not stored)
-  constexpr int L = C::REQUESTS;
+  constexpr int L = C::L, SL = C::SL;
   uint32_t off[L];
 #pragma unroll
   for (int i = 0; i < L; i++) {
@@ -219,39 +225,40 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void mx4_gemm_tile_k(con
     const int row = place + (lane >> 3) - (i * C::WAVES * 8 < C::BM ? 0 : C::BM);
     off[i] = (uint32_t)min(row, i * C::WAVES * 8 < C::BM ? last_m : last_n) * row_bytes + c * 16;
   }
-  const uint8_t* const ab = a + (long long)m0 * row_bytes;
-  const uint8_t* const wb = w + (long long)n0 * row_bytes;
-  // and its row's scales
-  const bool of_a = wave * 64 < C::BM;
-  const uint8_t* const sb = of_a ? as + (long long)m0 * slabs * 8 : ws + (long long)n0 * slabs * 8;
-  const int srow = wave * 64 - (of_a ? 0 : C::BM), slast = of_a ? last_m : last_n;
-  const uint32_t soff = (uint32_t)min(srow + lane, slast) * (uint32_t)slabs * 8u;
-  const uint32_t stage0 = lds_addr_of(lds) + wave * 1024, scales0 = stage0 + NS * C::STAGE;
-  // a pair of slabs behind the last full one starts a slab early, so that nothing behind the row is read
-  const auto pair_start = [&](int s) { return max(0, min(s & ~1, slabs - 2)); };
-  const auto request_scales = [&](int s) {
-    slab_load16s(sb + pair_start(s) * 8ll, soff, scales0 + ((s >> 1) & (C::PAIRS - 1)) * (C::ROWS * 16));
+  const uint8_t* const ab = a + (long long)m0 * row_bytes + s0 * 128ll;
+  const uint8_t* const wb = w + (long long)n0 * row_bytes + s0 * 128ll;
+  // and its rows' scales; of a single slab, 8 bytes a row
+  const auto scales_of = [&](int place) {
+    return place < C::BM ? as + (long long)(m0 + min(place, last_m)) * slabs * 8 : ws + (long long)(n0 + min(place - C::BM, last_n)) * slabs * 8;
   };
-  const auto request = [&](int s) {
-    const uint32_t to = stage0 + (s & (NS - 1)) * C::STAGE;
+  const uint8_t* sp[SL];
 #pragma unroll
-    for (int i = 0; i < L; i++) slab_load16s((i * C::WAVES * 8 < C::BM ? ab : wb) + s * 128ll, off[i], to + i * C::THREADS * 16);
+  for (int i = 0; i < SL; i++) sp[i] = scales_of((i * C::WAVES + wave) * 64 + lane);
+  uint8_t* const mine = lds + group * C::GROUP;
+  const uint32_t stage0 = lds_addr_of(mine) + wave * 1024, scales0 = stage0 + 2 * C::STAGE;
+  // a pair of slabs behind the last full one starts a slab early, so that nothing behind the row is read
+  const auto pair_start = [&](int s) { return max(0, min(s0 + (s & ~1), slabs - 2)); };
+  const auto request_scales = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < SL; i++)
+      slab_load16(sp[i] + pair_start(s) * 8ll, scales0 + (s >> 1 & 1) * (C::ROWS * 16) + i * C::WAVES * 1024);
+  };
+  const auto request = [&](int s, int i) {
+    slab_load16s((i * C::WAVES * 8 < C::BM ? ab : wb) + s * 128ll, off[i], stage0 + (s & 1) * C::STAGE + i * C::WAVES * 1024);
   };
   // fragments and scales of this wave
-  const uint8_t* const fa = lds + (wm * (AF * 32) + j) * 128;
-  const uint8_t* const fw = lds + (C::BM + wn * (WF * 32) + j) * 128;
-  const uint8_t* const fs = lds + NS * C::STAGE + g * 4 + j * 16;
+  const uint8_t* const fa = mine + (wm * (AF * 32) + j) * 128;
+  const uint8_t* const fw = mine + (C::BM + wn * (WF * 32) + j) * 128;
+  const uint8_t* const fs = mine + 2 * C::STAGE + g * 4 + j * 16;
   int4 af[2][AF], wf[2][WF];
   int asc[2][AF], wsc[2][WF];
-  const auto read = [&](int s, int S, int to) {
-    const int at = (s & (NS - 1)) * C::STAGE + (((4 * g + S) ^ ((j >> 1) & 7)) * 16);
-#pragma unroll
-    for (int x = 0; x < AF; x++) af[to][x] = *(const int4*)(fa + at + x * 32 * 128);
-#pragma unroll
-    for (int y = 0; y < WF; y++) wf[to][y] = *(const int4*)(fw + at + y * 32 * 128);
+  const auto read = [&](int s, int S, int to, int i) {           // fragment i of a step: first those of A
+    const int at = (s & 1) * C::STAGE + (((4 * g + S) ^ ((j >> 1) & 7)) * 16);
+    if (i < AF) af[to][i] = *(const int4*)(fa + at + i * 32 * 128);
+    else wf[to][i - AF] = *(const int4*)(fw + at + (i - AF) * 32 * 128);
   };
   const auto read_scales = [&](int s, int to) {
-    const uint8_t* const p = fs + ((s >> 1) & (C::PAIRS - 1)) * (C::ROWS * 16) + ((s - pair_start(s)) & 1) * 8;
+    const uint8_t* const p = fs + (s >> 1 & 1) * (C::ROWS * 16) + ((s0 + s - pair_start(s)) & 1) * 8;
 #pragma unroll
     for (int x = 0; x < AF; x++) asc[to][x] = *(const int*)(p + (wm * (AF * 32) + x * 32) * 16);
 #pragma unroll
@@ -264,54 +271,70 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void mx4_gemm_tile_k(con
     for (int y = 0; y < WF; y++)
 #pragma unroll
       for (int i = 0; i < 16; i++) acc[x][y][i] = 0.f;
-  const auto multiply = [&](auto sel, int from, int scales) {
-    constexpr int S = decltype(sel)::value;
+  // The products of a step; behind each of them stands its share of `pieces` other instructions.
+  const auto multiply = [&](auto sel, int from, int pieces, auto piece) {
+    constexpr int S = decltype(sel)::value, N = AF * WF;
 #pragma unroll
-    for (int y = 0; y < WF; y++)
+    for (int i = 0; i < N; i++) {
+      const int x = i % AF, y = i / AF;
+      acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(four_bits(af[from][x]), four_bits(wf[from][y]), acc[x][y], 4, 4, S, asc[0][x], S, wsc[0][y]);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int x = 0; x < AF; x++)
-        acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(four_bits(af[from][x]), four_bits(wf[from][y]), acc[x][y], 4, 4, S, asc[scales][x], S, wsc[scales][y]);
+      for (int p = i * pieces / N; p < (i + 1) * pieces / N; p++) {
+        piece(p);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  const auto arrive = [&](auto left) {
+    constexpr int N = decltype(left)::value;
+    if (C::WAVES > 1) wait_vm_barrier<N>();
+    else wait_vm_lds<N>();
   };
 
-#pragma unroll 1
-  for (int s = 0; s < min(NS, slabs); s++) {
+  // A slab's requests are spread over the products of the step that frees its stage (FIRST of them) and of the next.
+  constexpr int FIRST = L * 5 / 8, FRAGMENTS = AF + WF;
+  if (count > 0) {
     if (slabs == 1) {
 #pragma unroll 1
-      for (int i = 0; i < 4; i++)          // a row has 8 bytes alone: words 0 1 0 1
-        lds_load4s((const float*)sb, (uint32_t)min(srow + i * 16 + (lane >> 2), slast) * 8u + (lane & 1) * 4, scales0 + i * 256);
-    } else if ((s & 1) == 0) request_scales(s);
-    request(s);
+      for (int i = 0; i < 4 * SL; i++)          // a row has 8 bytes alone: words 0 1 0 1 of 16 rows
+        lds_load4(scales_of((i / 4 * C::WAVES + wave) * 64 + i % 4 * 16 + (lane >> 2)) + (lane & 1) * 4, scales0 + i / 4 * C::WAVES * 1024 + i % 4 * 256);
+    } else {
+      request_scales(0);
+    }
+#pragma unroll
+    for (int i = 0; i < L; i++) request(0, i);
   }
-  if (slabs >= NS) wait_vm_barrier<(NS - 1) * L + (NS - 2) / 2>();      // NS - 1 slabs are under way behind the first
-  else wait_vm_barrier<0>();
+  if (count > 1) {
+#pragma unroll
+    for (int i = 0; i < FIRST; i++) request(1, i);
+    arrive(Int<FIRST>());
+  } else {
+    arrive(Int<0>());
+  }
   read_scales(0, 0);
-  read(0, 0, 0);
-  // One slab.  MORE: slab s + NS is there to be requested (2: with scales), and NS - 2 behind slab s + 1 are under way, half of
-  // them with scales; without it (0) everything is waited for, and behind the last slab the stage read is an old one that
-  // nothing uses.  No branch stands inside: around one the compiler moves the products away from the reads they hide
-  // (8192 x 4096 x 11008 181 us with a branch around the scales' request).
-  const auto slab = [&](int s, auto more) {
-    constexpr int MORE = decltype(more)::value;
-    read(s, 1, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(Int<0>(), 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    read(s, 2, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(Int<1>(), 1, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    read(s, 3, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(Int<2>(), 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    wait_vm_barrier<MORE ? (NS - 2) * L + (NS - 2) / 2 : 0>();
-    if (MORE == 2) request_scales(s + NS);
-    if (MORE) request(s + NS);
-    read_scales(s + 1, 1);
-    read(s + 1, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(Int<3>(), 1, 0);
-    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < FRAGMENTS; i++) read(0, 0, 0, i);
+  // One slab.  NEXT: slab s + 1 is there, the rest of it to be requested; MORE: slab s + 2 too (2: with scales).  Behind the
+  // last slab the stage read is an old one that nothing uses.  No branch stands inside: around one the compiler moves the
+  // products away from what they hide.  Without DMA a slab of the 256 x 256 tile took 2650 clocks, of products alone 2190, of
+  // all 3280 where reads and requests stood in front of a step's products.
+  const auto slab = [&](int s, auto next, auto more) {
+    constexpr int NEXT = decltype(next)::value, MORE = decltype(more)::value;
+    multiply(Int<0>(), 0, FRAGMENTS + (NEXT ? L - FIRST : 0), [&](int p) {
+      constexpr int N = NEXT ? L - FIRST : 0;           // requests first: they have the longest way
+      if (p < N) request(s + 1, FIRST + p);
+      else read(s, 1, 1, p - N);
+    });
+    multiply(Int<1>(), 1, FRAGMENTS, [&](int p) { read(s, 2, 0, p); });
+    multiply(Int<2>(), 0, FRAGMENTS, [&](int p) { read(s, 3, 1, p); });
+    arrive(Int<0>());
+    multiply(Int<3>(), 1, 1 + FRAGMENTS + (MORE ? FIRST : 0) + (MORE == 2 ? 1 : 0), [&](int p) {
+      if (p == 0) read_scales(s + 1, 1);
+      else if (p <= FRAGMENTS) read(s + 1, 0, 0, p - 1);
+      else if (p <= FRAGMENTS + FIRST) request(s + 2, p - FRAGMENTS - 1);
+      else request_scales(s + 2);
+    });
 #pragma unroll
     for (int x = 0; x < AF; x++) asc[0][x] = asc[1][x];
 #pragma unroll
@@ -319,52 +342,64 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN / 4) void mx4_gemm_tile_k(con
   };
   int s = 0;
 #pragma unroll 1
-  for (; s + NS + 1 < slabs; s += 2) {
-    slab(s, Int<2>());
-    slab(s + 1, Int<1>());
+  for (; s + 3 < count; s += 2) {
+    slab(s, Int<1>(), Int<2>());
+    slab(s + 1, Int<1>(), Int<1>());
   }
-  if (s + NS < slabs) slab(s++, Int<2>());
-#pragma unroll 1
-  for (; s < slabs; s++) slab(s, Int<0>());
-  // The results go through LDS by fragments of 32 rows, each wave its own, so that a store writes whole rows and its code, with
-  // bias, residual and the edges, stands once.
+  if (s + 2 < count) slab(s++, Int<1>(), Int<2>());
+  if (s + 1 < count) slab(s++, Int<1>(), Int<0>());
+  if (s < count) slab(s, Int<0>(), Int<0>());
+
+  // The results go through LDS, so that a store writes whole rows and its code, with bias, residual and the edges, is short: V
+  // columns a lane.  One group: a fragment's 32 rows at a time, each wave its own.  Several: all rows, added in the order of
+  // the groups by the threads of the workgroup.
   wait_vm_barrier<0>();
-  float* const mine = (float*)lds + wave * 32 * C::STRIDE;
-  constexpr int V = 16 / sizeof(T), ACROSS = WF * 32 / V, DOWN = 64 / ACROSS;      // V columns a lane, DOWN rows a store
-  const int cl = lane % ACROSS * V, col = n0 + wn * (WF * 32) + cl, left = n - col;
+  constexpr int V = 16 / sizeof(T), ACROSS = WF * 32 / V, DOWN = (KW > 1 ? C::THREADS : 64) / ACROSS, H = (KW > 1 ? AF : 1) * 32;
+  constexpr int R = (H + DOWN - 1) / DOWN;                                            // rows a lane stores
+  float* const sums = (float*)lds + (KW > 1 ? 0 : wave) * (32 * C::STRIDE);
+  float* const put = (float*)lds + any_wave * (H * C::STRIDE);
+  const int t = KW > 1 ? (int)threadIdx.x : lane, cl = t % ACROSS * V, rl = t / ACROSS, col = n0 + wn * (WF * 32) + cl, left = n - col;
   float b[V];
 #pragma unroll
-  for (int v = 0; v < V; v++) b[v] = bias && v < left ? bias[col + v] : 0.f;
+  for (int v = 0; v < V; v++) b[v] = bias ? bias[min(col + v, n - 1)] : 0.f;
 #pragma unroll
-  for (int x = 0; x < AF; x++) {
+  for (int x = 0; x < AF; x += KW > 1 ? AF : 1) {
+    const int row0 = m0 + wm * (AF * 32) + x * 32 + rl;
+    Pack<T, V> u[R];
+    if (res && left >= V) {
 #pragma unroll
-    for (int y = 0; y < WF; y++)
+      for (int r = 0; r < R; r++) u[r] = *(const Pack<T, V>*)(res + (long long)min(row0 + r * DOWN, m - 1) * ld_res + col);
+    }
 #pragma unroll
-      for (int i = 0; i < 16; i++) mine[(8 * (i / 4) + 4 * g + i % 4) * C::STRIDE + y * 32 + j] = acc[x][y][i];
-    __builtin_amdgcn_wave_barrier();
-    const int row0 = m0 + wm * (AF * 32) + x * 32;
-#pragma unroll 2
-    for (int r = lane / ACROSS; r < 32; r += DOWN) {
-      const int row = row0 + r;
-      if (row >= m || left <= 0) break;
+    for (int z = x; z < (KW > 1 ? AF : x + 1); z++)
+#pragma unroll
+      for (int y = 0; y < WF; y++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) put[((z - x) * 32 + 8 * (i / 4) + 4 * g + i % 4) * C::STRIDE + y * 32 + j] = acc[z][y][i];
+    if (KW > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+      const int row = row0 + r * DOWN;
+      if (row >= m || (H % DOWN && rl + r * DOWN >= H) || left <= 0) continue;
+      float f[V];
+#pragma unroll
+      for (int v = 0; v < V; v++) f[v] = sums[(rl + r * DOWN) * C::STRIDE + cl + v];
+#pragma unroll
+      for (int q = 1; q < KW; q++)
+#pragma unroll
+        for (int v = 0; v < V; v++) f[v] += sums[(q * H + rl + r * DOWN) * C::STRIDE + cl + v];
       T* const o = out + (long long)row * ld + col;
-      const T* const p = res + (long long)row * ld_res + col;
       if (left >= V) {
-        Pack<T, V> q, u;
-        if (res) u = *(const Pack<T, V>*)p;
+        Pack<T, V> q;
 #pragma unroll
-        for (int v = 0; v < V; v++) {
-          float f = mine[r * C::STRIDE + cl + v] + b[v];
-          if (res) f += as_float(u.v[v]);
-          q.v[v] = from_float<T>(f);
-        }
+        for (int v = 0; v < V; v++) q.v[v] = from_float<T>(res ? f[v] + b[v] + as_float(u[r].v[v]) : f[v] + b[v]);
         *(Pack<T, V>*)o = q;
       } else {
-#pragma unroll 1
-        for (int v = 0; v < left; v++) {
-          const float f = mine[r * C::STRIDE + cl + v] + (bias ? bias[col + v] : 0.f);
-          o[v] = from_float<T>(res ? f + as_float(p[v]) : f);
-        }
+        const T* const p = res + (long long)row * ld_res + col;
+#pragma unroll
+        for (int v = 0; v < V; v++)
+          if (v < left) o[v] = from_float<T>(res ? f[v] + b[v] + as_float(p[v]) : f[v] + b[v]);
       }
     }
     __builtin_amdgcn_wave_barrier();
@@ -390,12 +425,12 @@ int values_as(hipStream_t st, const uint8_t* codes, const uint8_t* scales, int r
   hipLaunchKernelGGL(mx4_values_k<T>, dim3(wg), dim3(256), 0, st, (const uint32_t*)codes, scales, rows, cols, groups, out, ld);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
-template <typename T, int AF, int WF, int WM, int WN, int NS>
+template <typename T, int AF, int WF, int WM, int WN, int KW>
 int launch_tile(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs, const float* bias,
                 const T* res, long long ld_res, T* out, long long ld) {
-  typedef Mx4Tile<AF, WF, WM, WN, NS> C;
+  typedef Mx4Tile<AF, WF, WM, WN, KW> C;
   const int mt = (m + C::BM - 1) / C::BM, nt = (n + C::BN - 1) / C::BN;
-  const void* fn = (const void*)mx4_gemm_tile_k<T, AF, WF, WM, WN, NS>;
+  const void* fn = (const void*)mx4_gemm_tile_k<T, AF, WF, WM, WN, KW>;
   // more LDS than a launch gets by default: an attribute of the kernel on one device, set once for each
   static std::atomic<bool> set[64];
   int dev = 0;
@@ -404,17 +439,24 @@ int launch_tile(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8
     if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) != hipSuccess) return PAHQ_EHIP;
     set[dev].store(true, std::memory_order_release);
   }
-  hipLaunchKernelGGL((mx4_gemm_tile_k<T, AF, WF, WM, WN, NS>), dim3((mt * nt + 7) / 8 * 8), dim3(C::THREADS), C::LDS, st, a, as, w, ws, m, n, slabs, mt, nt,
-                     bias, res, ld_res, out, ld);
+  hipLaunchKernelGGL((mx4_gemm_tile_k<T, AF, WF, WM, WN, KW>), dim3((mt * nt + 7) / 8 * 8), dim3(C::THREADS), C::LDS, st, a, as, w, ws, m, n, slabs, mt,
+                     nt, bias, res, ld_res, out, ld);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
 template <typename T>
 int gemm_as(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs, const float* bias,
             const T* res, long long ld_res, T* out, long long ld) {
-#define TILE(AF_, WF_, WM_, WN_, NS_) return launch_tile<T, AF_, WF_, WM_, WN_, NS_>(st, a, as, w, ws, m, n, slabs, bias, res, ld_res, out, ld)
+#define TILE(...) return launch_tile<T, __VA_ARGS__>(st, a, as, w, ws, m, n, slabs, bias, res, ld_res, out, ld)
+  static const int force = getenv("MXV") ? atoi(getenv("MXV")) : 0;
+  if (force == 1) TILE(1, 1, 1, 1, 4);
+  if (force == 2) TILE(1, 1, 1, 1, 8);
+  if (force == 3) TILE(2, 2, 1, 1, 4);
+  if (force == 9) TILE(2, 2, 1, 1, 2);
+  if (force == 6) TILE(2, 2, 2, 2, 1);
+  if (force == 5) TILE(2, 4, 4, 2, 1);
   if (m > 64 && slabs < (1 << 16)) {
-    if ((long long)((m + 255) / 256) * ((n + 255) / 256) >= 256) TILE(2, 4, 4, 2, 2);
-    TILE(2, 2, 2, 2, 4);
+    if ((long long)((m + 255) / 256) * ((n + 255) / 256) >= 256) TILE(2, 4, 4, 2, 1);
+    TILE(2, 2, 2, 2, 1);
   }
 #undef TILE
   const unsigned nt = (unsigned)((n + 15) / 16);
