@@ -463,6 +463,7 @@ enum { PAHQ_F32 = 0, PAHQ_BF16 = 1, PAHQ_F16 = 2 };
  * fp32 [n] or NULL, residual of out's type or NULL (it may be out itself, with the same stride).  Sums in fp32, one rounding
  * to out's type.  The order of a sum depends on the sizes alone: the same call gives the same bits. */
 enum { PAHQ_MX4_BY_ROWS = 0, PAHQ_MX4_BY_COLUMNS = 1 };
+enum { PAHQ_MX4_MAX_K = 1 << 24 };            /* of a product */
 int pahq_mx4_bytes(int32_t rows, int32_t cols, size_t* codes, size_t* scales);
 int pahq_mx4_quantize(void* hip_stream, const void* x, int32_t dtype, int32_t rows, int32_t cols, int64_t ld, int32_t by,
                       uint8_t* codes, uint8_t* scales);

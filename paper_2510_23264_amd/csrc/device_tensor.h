@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
+#include <type_traits>
 #include "../../include/pahq.h"
 
 namespace pahq {
@@ -59,6 +60,34 @@ __device__ __forceinline__ void store8(T* p, int left, const float* v) {
     for (int j = 0; j < 8; j++)
       if (j < left) p[j] = from_float<T>(v[j]);
   }
+}
+
+// Sixteen bytes of elements as four registers (an array of 16-bit elements takes one each), at any alignment of the element.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int A> struct __attribute__((packed, aligned(A))) Lines { u32x4 v; };
+template <typename T> __device__ __forceinline__ u32x4 load16(const T* p) {
+  return ((const Lines<sizeof(T)>*)p)->v;
+}
+template <typename T> __device__ __forceinline__ void store16(T* p, u32x4 v) {
+  ((Lines<sizeof(T)>*)p)->v = v;
+}
+template <typename T> __device__ __forceinline__ float element(u32x4 v, int i) {
+  if (sizeof(T) == 4) return __uint_as_float(v[i]);
+  const uint16_t h = (uint16_t)(v[i / 2] >> (i % 2 * 16));
+  return as_float(__builtin_bit_cast(T, (std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>)h));
+}
+template <typename T> __device__ __forceinline__ u32x4 pack16(const float* f) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    if (sizeof(T) == 4) v[i] = __float_as_uint(f[i]);
+    else {
+      typedef T T2 __attribute__((ext_vector_type(2)));
+      typedef std::conditional_t<sizeof(T) == 2, uint32_t, uint64_t> W;
+      v[i] = (uint32_t)__builtin_bit_cast(W, (T2){from_float<T>(f[2 * i % (16 / sizeof(T))]), from_float<T>(f[(2 * i + 1) % (16 / sizeof(T))])});
+    }
+  }
+  return v;
 }
 
 }  // namespace pahq

@@ -8,11 +8,12 @@
 // additions in any order leave.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
-#include <stdlib.h>
+#include <algorithm>
 #include <atomic>
 #include "../../include/pahq.h"
 #include "mma_util.h"
 #include "device_tensor.h"
+#include "mx4_rules.h"
 
 namespace pahq {
 
@@ -111,141 +112,141 @@ __global__ __launch_bounds__(256) void mx4_values_k(const uint32_t* codes, const
 typedef float v16f __attribute__((ext_vector_type(16)));
 template <int N> struct Int { static constexpr int value = N; };
 
-// Tile of a workgroup: the eight XCDs take neighbouring ranges of the tiles, which run down bands of eight rows of tiles, so
-// that what an XCD works on at a time shares operands in its L2.  tm >= mt: no tile (the ranges are rounded up).
-__device__ __forceinline__ void tile_of(int wg, int mt, int nt, int& tm, int& tn) {
-  const int t = xcd_tile(wg, mt * nt);
-  if (t >= mt * nt) { tm = mt; tn = 0; return; }
-  const int band = t / (8 * nt), in = t - band * 8 * nt, high = min(8, mt - band * 8);
-  tn = in / high;
-  tm = band * 8 + in - tn * high;
-}
-
 // The instruction's operand type is wide enough for 8-bit elements; 4-bit ones are its first half.
 __device__ __forceinline__ v8i four_bits(int4 v) { return (v8i){v.x, v.y, v.z, v.w, 0, 0, 0, 0}; }
 
-// Few rows: 16 * MT rows x 16 columns a workgroup, the sum over k split over its waves (slab s of 256 elements to wave s
-// mod WAVES) and joined in LDS in the order of the waves, so results do not depend on timing.  Operands come straight from
-// global memory: a lane reads two neighbouring blocks of its row with their scales, which are one halfword, and the four
-// lanes of a row take 128 contiguous bytes.  Which 32 elements of the slab a lane's block is does not matter to the sum as
-// long as both operands agree.  Rows and columns past the end read the last one and are not stored.
-template <typename T, int MT, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void mx4_gemm_few_k(const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n,
-                                                            int slabs, const float* bias, const T* res, long long ld_res, T* out, long long ld) {
-  __shared__ float part[WAVES][MT * 16][17];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * MT);
-  const long long row_bytes = (long long)slabs * 128;
-  const long long wr = min(n0 + r, n - 1);
+// Few rows: up to 16 rows x 16 columns a workgroup, the sum over k split over its eight waves (slab s of 256 elements to wave s
+// mod 8) and joined in LDS in the order of the waves, so results do not depend on timing.  Operands come straight from global
+// memory: a lane reads two neighbouring blocks of its row with their scales, which are one halfword, and the four lanes of a row
+// take 128 contiguous bytes.  Which 32 elements of the slab a lane's block is does not matter to the sum as long as both
+// operands agree.  Rows and columns past the end read the last one and are not stored.  Bound by the way to the first bytes:
+// one token through 4096 x 4096 takes 4.4 us, 1.7 of them the weights' bytes at the rate of a large copy, 2.3 an empty launch.
+template <typename T>
+__global__ __launch_bounds__(512) void mx4_gemm_few_k(const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs,
+                                                      const float* bias, const T* res, long long ld_res, T* out, long long ld) {
+  constexpr int WAVES = 8;
+  __shared__ float part[WAVES][16][17];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4, n0 = blockIdx.x * 16;
+  const long long row_bytes = (long long)slabs * 128, wr = min(n0 + r, n - 1), ar = min(r, m - 1);
   const uint8_t* wp = w + wr * row_bytes + g * 32;
   const uint8_t* wsp = ws + wr * slabs * 8 + g * 2;
-  const uint8_t* ap[MT];
-  const uint8_t* asp[MT];
-#pragma unroll
-  for (int t = 0; t < MT; t++) {
-    const long long ar = min(m0 + t * 16 + r, m - 1);
-    ap[t] = a + ar * row_bytes + g * 32;
-    asp[t] = as + ar * slabs * 8 + g * 2;
-  }
-  v4f acc[MT];
-#pragma unroll
-  for (int t = 0; t < MT; t++) acc[t] = (v4f){0.f, 0.f, 0.f, 0.f};
+  const uint8_t* ap = a + ar * row_bytes + g * 32;
+  const uint8_t* asp = as + ar * slabs * 8 + g * 2;
+  v4f acc = {0.f, 0.f, 0.f, 0.f};
   for (int s = wave; s < slabs; s += WAVES) {
-    const int4 w0 = *(const int4*)(wp + (long long)s * 128), w1 = *(const int4*)(wp + (long long)s * 128 + 16);
-    const int wsc = *(const uint16_t*)(wsp + (long long)s * 8);
-    const v8i b0 = {w0.x, w0.y, w0.z, w0.w, 0, 0, 0, 0}, b1 = {w1.x, w1.y, w1.z, w1.w, 0, 0, 0, 0};
-#pragma unroll
-    for (int t = 0; t < MT; t++) {
-      const int4 a0 = *(const int4*)(ap[t] + (long long)s * 128), a1 = *(const int4*)(ap[t] + (long long)s * 128 + 16);
-      const int asc = *(const uint16_t*)(asp[t] + (long long)s * 8);
-      const v8i c0 = {a0.x, a0.y, a0.z, a0.w, 0, 0, 0, 0}, c1 = {a1.x, a1.y, a1.z, a1.w, 0, 0, 0, 0};
-      acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(c0, b0, acc[t], 4, 4, 0, asc, 0, wsc);
-      acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(c1, b1, acc[t], 4, 4, 1, asc, 1, wsc);
-    }
+    const int4 w0 = *(const int4*)(wp + s * 128ll), w1 = *(const int4*)(wp + s * 128ll + 16);
+    const int4 a0 = *(const int4*)(ap + s * 128ll), a1 = *(const int4*)(ap + s * 128ll + 16);
+    const int wsc = *(const uint16_t*)(wsp + s * 8ll), asc = *(const uint16_t*)(asp + s * 8ll);
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_bits(a0), four_bits(w0), acc, 4, 4, 0, asc, 0, wsc);
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_bits(a1), four_bits(w1), acc, 4, 4, 1, asc, 1, wsc);
   }
 #pragma unroll
-  for (int t = 0; t < MT; t++)
-#pragma unroll
-    for (int i = 0; i < 4; i++) part[wave][t * 16 + g * 4 + i][r] = acc[t][i];
+  for (int i = 0; i < 4; i++) part[wave][g * 4 + i][r] = acc[i];
   __syncthreads();
-  for (int e = threadIdx.x; e < MT * 256; e += WAVES * 64) {
-    const int row = m0 + (e >> 4), col = n0 + (e & 15);
-    if (row >= m || col >= n) continue;
-    float y = 0.f;
+  const int row = threadIdx.x >> 4, col = n0 + (threadIdx.x & 15);
+  if (row >= m || col >= n) return;             // (of the 512 threads 256 have an element)
+  float y = 0.f;
 #pragma unroll
-    for (int v = 0; v < WAVES; v++) y += part[v][e >> 4][e & 15];
-    if (bias) y += bias[col];
-    if (res) y += as_float(res[(long long)row * ld_res + col]);
-    out[(long long)row * ld + col] = from_float<T>(y);
-  }
+  for (int v = 0; v < WAVES; v++) y += part[v][row][threadIdx.x & 15];
+  if (bias) y += bias[col];
+  if (res) y += as_float(res[row * ld_res + col]);
+  out[row * ld + col] = from_float<T>(y);
 }
 
 // Tiles through LDS.  AF x WF products of 32 x 32 (V_MFMA_SCALE_F32_32X32X64_F8F6F4) a wave, a group of WM x WN waves a tile, KW
 // groups a workgroup that share the sum over k.  Slabs of 256 elements of k (128 bytes of codes a row) come in two stages,
-// straight into LDS, each group's its own.  In a slab a lane takes four neighbouring blocks of
-// its row, one a step, so the bytes of one word of scales serve its four steps through the instruction's byte selector.  LDS
-// holds a row's 16-byte chunks XOR-swizzled by half the row's number, so that 16 lanes cover all 64 banks.  Scales are 8 bytes
-// of a row a slab; they come by pairs of slabs, 16 bytes a request.
-// The fragments of a step are read while the step before it multiplies, those of the next slab's first step too: the wait for
-// that slab and the barrier stand in front of the last step, when every fragment of this slab is in registers and its stage
-// is free for the next request.  A group of one wave needs no barrier.
+// straight into LDS, each group's its own.  In a slab a lane takes four neighbouring blocks of its row, one a step, so the bytes
+// of one word of scales serve its four steps through the instruction's byte selector.  LDS holds a row's 16-byte chunks
+// XOR-swizzled by half the row's number, so that 16 lanes cover all 64 banks.  Scales are 8 bytes of a row a slab; they come by
+// pairs of slabs, 16 bytes a request.
+// Every read of a fragment (a step ahead) and every request (up to two slabs ahead) stands between two products: the wait for the
+// next slab and the barrier are in front of a slab's last step, when all its fragments are in registers and its stage is free.
+// A workgroup of one group walks the tiles of its XCD's range; the first slabs of the next tile are requested before the results
+// of this one are stored.
 template <int AF, int WF, int WM, int WN, int KW>
 struct Mx4Tile {
   static constexpr int BM = AF * 32 * WM, BN = WF * 32 * WN, WAVES = WM * WN, THREADS = KW * WAVES * 64, ROWS = BM + BN;
-  static constexpr int STAGE = ROWS * 128, GROUP = 2 * (STAGE + ROWS * 16);        // two slabs, two pairs' scales
-  static constexpr int STRIDE = WF * 32 + 8;                                         // floats, of a row of a wave's results
-  static constexpr int OUT = KW * WAVES * (KW > 1 ? AF : 1) * 32 * STRIDE * 4;       // a fragment's rows at a time, or all
+  static constexpr int STAGE = ROWS * 128, GROUP = 2 * (STAGE + ROWS * 16);          // two slabs, two pairs' scales
+  static constexpr int STRIDE = WF * 32 + 8;                                         // floats, of a row of a group's results
+  static constexpr int OUT = KW > 1 ? KW * AF * 32 * STRIDE * 4 : GROUP + WAVES * 2048;
   static constexpr int LDS = KW * GROUP > OUT ? KW * GROUP : OUT;
+  static constexpr int PER_CU = 160 * 1024 / LDS, PER_SIMD = (PER_CU * KW * WAVES + 3) / 4;     // workgroups and waves that the LDS leaves room for
   static constexpr int L = ROWS / (8 * WAVES), SL = ROWS / (64 * WAVES);             // requests of a wave: a slab's codes, a pair's scales
   static_assert(ROWS % (64 * WAVES) == 0 && LDS <= 160 * 1024 && (KW == 1 || WAVES == 1), "whole requests");
   static_assert(BM % (8 * WAVES) == 0 && BM % 64 == (WAVES == 1 && SL == 1 ? 32 : 0), "a request of codes belongs to one operand");
 };
 template <typename T, int AF, int WF, int WM, int WN, int KW>
-__global__ __launch_bounds__(KW * WM * WN * 64, (KW * WM * WN + 3) / 4) void mx4_gemm_tile_k(const uint8_t* a, const uint8_t* as, const uint8_t* w,
+__global__ __launch_bounds__(KW * WM * WN * 64, (Mx4Tile<AF, WF, WM, WN, KW>::PER_SIMD)) void mx4_gemm_tile_k(const uint8_t* a, const uint8_t* as, const uint8_t* w,
                                                                                           const uint8_t* ws, int m, int n, int slabs, int mt, int nt,
                                                                                           const float* bias, const T* res, long long ld_res, T* out,
                                                                                           long long ld) {
   typedef Mx4Tile<AF, WF, WM, WN, KW> C;
+  constexpr int L = C::L, SL = C::SL, FRAGMENTS = AF + WF;
+  // a slab's requests: FIRST of them in the step that frees its stage, the others in the next
+  constexpr int FIRST = L * 5 / 8;
   extern __shared__ __align__(16) uint8_t lds[];
   const int lane = threadIdx.x & 63, j = lane & 31, g = lane >> 5, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = any_wave / C::WAVES, wave = any_wave % C::WAVES, wm = wave / WN, wn = wave % WN;
-  int tm, tn;
-  tile_of(blockIdx.x, mt, nt, tm, tn);
-  if (tm >= mt) return;
-  const int m0 = tm * C::BM, n0 = tn * C::BN, last_m = m - 1 - m0, last_n = n - 1 - n0;
+  // tiles of this workgroup's XCD: neighbouring ones run down bands of eight rows of tiles, so that what an XCD works on at a
+  // time shares operands in its L2
+  const int total = mt * nt, chunk = (total + 7) >> 3, tile_end = min(total, ((int)blockIdx.x & 7) * chunk + chunk), stride = gridDim.x >> 3;
+  int tile = ((int)blockIdx.x & 7) * chunk + ((int)blockIdx.x >> 3);
+  if (tile >= tile_end) return;
   // this group's slabs of k: s0 .. s0 + count - 1
   const int share = (slabs + KW - 1) / KW, s0 = group * share, count = min(share, slabs - s0);
   const uint32_t row_bytes = (uint32_t)slabs * 128u;
-  // where this lane's chunks of a stage come from, in the tile's rows (rows past the end: the last one, not stored)
-  constexpr int L = C::L, SL = C::SL;
+
+  // Where this lane's chunks of a stage come from, in the rows of the tile that is loaded (rows past the end: the last one, not
+  // stored), and its rows' scales.
+  int m0, n0;
   uint32_t off[L];
-#pragma unroll
-  for (int i = 0; i < L; i++) {
-    const int place = (i * C::WAVES + wave) * 8, c = (lane & 7) ^ (lane >> 4) ^ ((place >> 1) & 4);
-    const int row = place + (lane >> 3) - (i * C::WAVES * 8 < C::BM ? 0 : C::BM);
-    off[i] = (uint32_t)min(row, i * C::WAVES * 8 < C::BM ? last_m : last_n) * row_bytes + c * 16;
-  }
-  const uint8_t* const ab = a + (long long)m0 * row_bytes + s0 * 128ll;
-  const uint8_t* const wb = w + (long long)n0 * row_bytes + s0 * 128ll;
-  // and its rows' scales; of a single slab, 8 bytes a row
+  const uint8_t *ab, *wb, *sp[SL];
   const auto scales_of = [&](int place) {
-    return place < C::BM ? as + (long long)(m0 + min(place, last_m)) * slabs * 8 : ws + (long long)(n0 + min(place - C::BM, last_n)) * slabs * 8;
+    return place < C::BM ? as + (long long)min(m0 + place, m - 1) * slabs * 8 : ws + (long long)min(n0 + place - C::BM, n - 1) * slabs * 8;
   };
-  const uint8_t* sp[SL];
+  const auto place_tile = [&]() {
+    const int band = tile / (8 * nt), in = tile - band * 8 * nt, high = min(8, mt - band * 8);
+    m0 = (band * 8 + in % high) * C::BM;
+    n0 = in / high * C::BN;
 #pragma unroll
-  for (int i = 0; i < SL; i++) sp[i] = scales_of((i * C::WAVES + wave) * 64 + lane);
+    for (int i = 0; i < L; i++) {
+      const int place = (i * C::WAVES + wave) * 8, c = (lane & 7) ^ (lane >> 4) ^ ((place >> 1) & 4);
+      const int row = place + (lane >> 3) - (i * C::WAVES * 8 < C::BM ? 0 : C::BM);
+      off[i] = (uint32_t)min(row, i * C::WAVES * 8 < C::BM ? m - 1 - m0 : n - 1 - n0) * row_bytes + c * 16;
+    }
+    ab = a + (long long)m0 * row_bytes + s0 * 128ll;
+    wb = w + (long long)n0 * row_bytes + s0 * 128ll;
+#pragma unroll
+    for (int i = 0; i < SL; i++) sp[i] = scales_of((i * C::WAVES + wave) * 64 + lane);
+  };
   uint8_t* const mine = lds + group * C::GROUP;
   const uint32_t stage0 = lds_addr_of(mine) + wave * 1024, scales0 = stage0 + 2 * C::STAGE;
   // a pair of slabs behind the last full one starts a slab early, so that nothing behind the row is read
   const auto pair_start = [&](int s) { return max(0, min(s0 + (s & ~1), slabs - 2)); };
   const auto request_scales = [&](int s) {
 #pragma unroll
-    for (int i = 0; i < SL; i++)
-      slab_load16(sp[i] + pair_start(s) * 8ll, scales0 + (s >> 1 & 1) * (C::ROWS * 16) + i * C::WAVES * 1024);
+    for (int i = 0; i < SL; i++) slab_load16(sp[i] + pair_start(s) * 8ll, scales0 + (s >> 1 & 1) * (C::ROWS * 16) + i * C::WAVES * 1024);
   };
   const auto request = [&](int s, int i) {
     slab_load16s((i * C::WAVES * 8 < C::BM ? ab : wb) + s * 128ll, off[i], stage0 + (s & 1) * C::STAGE + i * C::WAVES * 1024);
   };
+  const auto request_first = [&]() {
+    if (count <= 0) return;
+    if (slabs == 1) {
+#pragma unroll 1
+      for (int i = 0; i < 4 * SL; i++)          // a row has 8 bytes alone: words 0 1 0 1 of 16 rows
+        lds_load4(scales_of((i / 4 * C::WAVES + wave) * 64 + i % 4 * 16 + (lane >> 2)) + (lane & 1) * 4, scales0 + i / 4 * C::WAVES * 1024 + i % 4 * 256);
+    } else {
+      request_scales(0);
+    }
+#pragma unroll
+    for (int i = 0; i < L; i++) request(0, i);
+    if (count > 1) {
+#pragma unroll
+      for (int i = 0; i < FIRST; i++) request(1, i);
+    }
+  };
+
   // fragments and scales of this wave
   const uint8_t* const fa = mine + (wm * (AF * 32) + j) * 128;
   const uint8_t* const fw = mine + (C::BM + wn * (WF * 32) + j) * 128;
@@ -265,12 +266,6 @@ __global__ __launch_bounds__(KW * WM * WN * 64, (KW * WM * WN + 3) / 4) void mx4
     for (int y = 0; y < WF; y++) wsc[to][y] = *(const int*)(p + (C::BM + wn * (WF * 32) + y * 32) * 16);
   };
   v16f acc[AF][WF];
-#pragma unroll
-  for (int x = 0; x < AF; x++)
-#pragma unroll
-    for (int y = 0; y < WF; y++)
-#pragma unroll
-      for (int i = 0; i < 16; i++) acc[x][y][i] = 0.f;
   // The products of a step; behind each of them stands its share of `pieces` other instructions.
   const auto multiply = [&](auto sel, int from, int pieces, auto piece) {
     constexpr int S = decltype(sel)::value, N = AF * WF;
@@ -291,34 +286,10 @@ __global__ __launch_bounds__(KW * WM * WN * 64, (KW * WM * WN + 3) / 4) void mx4
     if (C::WAVES > 1) wait_vm_barrier<N>();
     else wait_vm_lds<N>();
   };
-
-  // A slab's requests are spread over the products of the step that frees its stage (FIRST of them) and of the next.
-  constexpr int FIRST = L * 5 / 8, FRAGMENTS = AF + WF;
-  if (count > 0) {
-    if (slabs == 1) {
-#pragma unroll 1
-      for (int i = 0; i < 4 * SL; i++)          // a row has 8 bytes alone: words 0 1 0 1 of 16 rows
-        lds_load4(scales_of((i / 4 * C::WAVES + wave) * 64 + i % 4 * 16 + (lane >> 2)) + (lane & 1) * 4, scales0 + i / 4 * C::WAVES * 1024 + i % 4 * 256);
-    } else {
-      request_scales(0);
-    }
-#pragma unroll
-    for (int i = 0; i < L; i++) request(0, i);
-  }
-  if (count > 1) {
-#pragma unroll
-    for (int i = 0; i < FIRST; i++) request(1, i);
-    arrive(Int<FIRST>());
-  } else {
-    arrive(Int<0>());
-  }
-  read_scales(0, 0);
-#pragma unroll
-  for (int i = 0; i < FRAGMENTS; i++) read(0, 0, 0, i);
   // One slab.  NEXT: slab s + 1 is there, the rest of it to be requested; MORE: slab s + 2 too (2: with scales).  Behind the
   // last slab the stage read is an old one that nothing uses.  No branch stands inside: around one the compiler moves the
-  // products away from what they hide.  Without DMA a slab of the 256 x 256 tile took 2650 clocks, of products alone 2190, of
-  // all 3280 where reads and requests stood in front of a step's products.
+  // products away from what they hide.  A slab of the 256 x 256 tile: products alone 2190 clocks, with everything 2620; 3280
+  // where reads and requests stood in front of a step's products.
   const auto slab = [&](int s, auto next, auto more) {
     constexpr int NEXT = decltype(next)::value, MORE = decltype(more)::value;
     multiply(Int<0>(), 0, FRAGMENTS + (NEXT ? L - FIRST : 0), [&](int p) {
@@ -340,69 +311,136 @@ __global__ __launch_bounds__(KW * WM * WN * 64, (KW * WM * WN + 3) / 4) void mx4
 #pragma unroll
     for (int y = 0; y < WF; y++) wsc[0][y] = wsc[1][y];
   };
-  int s = 0;
-#pragma unroll 1
-  for (; s + 3 < count; s += 2) {
-    slab(s, Int<1>(), Int<2>());
-    slab(s + 1, Int<1>(), Int<1>());
-  }
-  if (s + 2 < count) slab(s++, Int<1>(), Int<2>());
-  if (s + 1 < count) slab(s++, Int<1>(), Int<0>());
-  if (s < count) slab(s, Int<0>(), Int<0>());
 
-  // The results go through LDS, so that a store writes whole rows and its code, with bias, residual and the edges, is short: V
-  // columns a lane.  One group: a fragment's 32 rows at a time, each wave its own.  Several: all rows, added in the order of
-  // the groups by the threads of the workgroup.
-  wait_vm_barrier<0>();
-  constexpr int V = 16 / sizeof(T), ACROSS = WF * 32 / V, DOWN = (KW > 1 ? C::THREADS : 64) / ACROSS, H = (KW > 1 ? AF : 1) * 32;
-  constexpr int R = (H + DOWN - 1) / DOWN;                                            // rows a lane stores
-  float* const sums = (float*)lds + (KW > 1 ? 0 : wave) * (32 * C::STRIDE);
-  float* const put = (float*)lds + any_wave * (H * C::STRIDE);
-  const int t = KW > 1 ? (int)threadIdx.x : lane, cl = t % ACROSS * V, rl = t / ACROSS, col = n0 + wn * (WF * 32) + cl, left = n - col;
-  float b[V];
+  // The results go through LDS, so that a store writes whole lines: V columns a lane.
+  constexpr int V = 16 / sizeof(T), ACROSS = WF * 32 / V;
+  const auto finish = [&](float* f, const float* b, u32x4 u, T* o, const T* r, int left) {
+    if (left >= V) {
 #pragma unroll
-  for (int v = 0; v < V; v++) b[v] = bias ? bias[min(col + v, n - 1)] : 0.f;
+      for (int v = 0; v < V; v++) f[v] = res ? f[v] + b[v] + element<T>(u, v) : f[v] + b[v];
+      store16(o, pack16<T>(f));
+    } else {
 #pragma unroll
-  for (int x = 0; x < AF; x += KW > 1 ? AF : 1) {
-    const int row0 = m0 + wm * (AF * 32) + x * 32 + rl;
-    Pack<T, V> u[R];
-    if (res && left >= V) {
-#pragma unroll
-      for (int r = 0; r < R; r++) u[r] = *(const Pack<T, V>*)(res + (long long)min(row0 + r * DOWN, m - 1) * ld_res + col);
+      for (int v = 0; v < V; v++)
+        if (v < left) o[v] = from_float<T>(res ? f[v] + b[v] + as_float(r[v]) : f[v] + b[v]);
     }
+  };
+
+  // stores of a wave and tile (one group)
+  constexpr int STORES = AF * 32 * ACROSS / 64;
+  bool stores_under_way = false;
+  place_tile();
+  request_first();
+  while (true) {
+    // slab 0: behind it are FIRST requests of slab 1, and the last tile's stores where their number is known
+    if (count > 1 && stores_under_way) arrive(Int<FIRST + STORES>());
+    else if (count > 1) arrive(Int<FIRST>());
+    else arrive(Int<0>());
+    read_scales(0, 0);
 #pragma unroll
-    for (int z = x; z < (KW > 1 ? AF : x + 1); z++)
+    for (int i = 0; i < FRAGMENTS; i++) read(0, 0, 0, i);
+#pragma unroll
+    for (int x = 0; x < AF; x++)
 #pragma unroll
       for (int y = 0; y < WF; y++)
 #pragma unroll
-        for (int i = 0; i < 16; i++) put[((z - x) * 32 + 8 * (i / 4) + 4 * g + i % 4) * C::STRIDE + y * 32 + j] = acc[z][y][i];
-    if (KW > 1) __syncthreads();
-    else __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int r = 0; r < R; r++) {
-      const int row = row0 + r * DOWN;
-      if (row >= m || (H % DOWN && rl + r * DOWN >= H) || left <= 0) continue;
-      float f[V];
-#pragma unroll
-      for (int v = 0; v < V; v++) f[v] = sums[(rl + r * DOWN) * C::STRIDE + cl + v];
-#pragma unroll
-      for (int q = 1; q < KW; q++)
-#pragma unroll
-        for (int v = 0; v < V; v++) f[v] += sums[(q * H + rl + r * DOWN) * C::STRIDE + cl + v];
-      T* const o = out + (long long)row * ld + col;
-      if (left >= V) {
-        Pack<T, V> q;
-#pragma unroll
-        for (int v = 0; v < V; v++) q.v[v] = from_float<T>(res ? f[v] + b[v] + as_float(u[r].v[v]) : f[v] + b[v]);
-        *(Pack<T, V>*)o = q;
-      } else {
-        const T* const p = res + (long long)row * ld_res + col;
-#pragma unroll
-        for (int v = 0; v < V; v++)
-          if (v < left) o[v] = from_float<T>(res ? f[v] + b[v] + as_float(p[v]) : f[v] + b[v]);
-      }
+        for (int i = 0; i < 16; i++) acc[x][y][i] = 0.f;
+    int s = 0;
+#pragma unroll 1
+    for (; s + 3 < count; s += 2) {
+      slab(s, Int<1>(), Int<2>());
+      slab(s + 1, Int<1>(), Int<1>());
     }
-    __builtin_amdgcn_wave_barrier();
+    if (s + 2 < count) slab(s++, Int<1>(), Int<2>());
+    if (s + 1 < count) slab(s++, Int<1>(), Int<0>());
+    if (s < count) slab(s, Int<0>(), Int<0>());
+
+    if constexpr (KW > 1) {
+      // several groups: all rows, added in the order of the groups by all threads
+      wait_vm_barrier<0>();
+      constexpr int H = AF * 32, DOWN = C::THREADS / ACROSS, R = (H + DOWN - 1) / DOWN;
+      const int t = threadIdx.x, cl = t % ACROSS * V, rl = t / ACROSS, col = n0 + cl, left = n - col;
+      float* const sums = (float*)lds + rl * C::STRIDE + cl;
+      float b[V];
+#pragma unroll
+      for (int v = 0; v < V; v++) b[v] = bias ? bias[min(col + v, n - 1)] : 0.f;
+      T* const o = out + (long long)(m0 + rl) * ld + col;
+      const T* const p = res + (long long)(m0 + rl) * ld_res + col;
+      u32x4 u[R];
+      if (res && left >= V) {
+#pragma unroll
+        for (int r = 0; r < R; r++)
+          if (m0 + rl + r * DOWN < m) u[r] = load16(p + (long long)(r * DOWN) * ld_res);
+      }
+      float* const put = (float*)lds + group * (H * C::STRIDE) + 4 * g * C::STRIDE + j;
+#pragma unroll
+      for (int x = 0; x < AF; x++)
+#pragma unroll
+        for (int y = 0; y < WF; y++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) put[(x * 32 + 8 * (i / 4) + i % 4) * C::STRIDE + y * 32] = acc[x][y][i];
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < R; r++) {
+        const int row = m0 + rl + r * DOWN;
+        if (row >= m || (H % DOWN && rl + r * DOWN >= H) || left <= 0) continue;
+        float f[V];
+#pragma unroll
+        for (int v = 0; v < V; v++) f[v] = sums[r * DOWN * C::STRIDE + v];
+#pragma unroll
+        for (int q = 1; q < KW; q++)
+#pragma unroll
+          for (int v = 0; v < V; v++) f[v] += sums[(q * H + r * DOWN) * C::STRIDE + v];
+        finish(f, b, u[r], o + (long long)(r * DOWN) * ld, p + (long long)(r * DOWN) * ld_res, left);
+      }
+      return;
+    } else {
+      // One group: PR rows of a fragment at a time through 2 KB of the wave's own, in units of a 16-byte store a lane.  The
+      // residual is read RING units ahead.
+      constexpr int PR = 16 / WF, Q = PR / 2, DOWN = 64 / ACROSS, PU = PR / DOWN, UNITS = AF * (32 / PR) * PU, RING = UNITS < 8 ? UNITS : 8;
+      static_assert(UNITS == STORES && PU >= 1, "units");
+      arrive(Int<0>());                 // nobody reads the stages any more
+      const int cl = lane % ACROSS * V, rl = lane / ACROSS, col = n0 + wn * (WF * 32) + cl, left = n - col;
+      stores_under_way = m0 + C::BM <= m && n0 + C::BN <= n;
+      // a lane's row of unit q: its row of unit 0 and a distance that is the same for all lanes
+      const int row0 = m0 + wm * (AF * 32) + (PU == 1 ? 4 * (rl / Q) + rl % Q : rl);
+      const auto down = [](int q) { return q / PU / (32 / PR) * 32 + q / PU % (32 / PR) / (4 / Q) * 8 + q / PU % (4 / Q) * Q + q % PU * 4; };
+      T* const o = out + (long long)row0 * ld + col;
+      const T* const p = res + (long long)row0 * ld_res + col;
+      const bool add = res && left >= V;
+      u32x4 u[RING];
+#pragma unroll
+      for (int q = 0; q < RING; q++)
+        if (add && row0 + down(q) < m) u[q] = load16(p + down(q) * ld_res);
+      float b[V];
+#pragma unroll
+      for (int v = 0; v < V; v++) b[v] = bias ? bias[min(col + v, n - 1)] : 0.f;
+      tile += stride;
+      if (tile < tile_end) {
+        place_tile();
+        request_first();
+      }
+      float* const box = (float*)(lds + C::GROUP + wave * 2048);
+#pragma unroll
+      for (int pass = 0; pass < UNITS / PU; pass++) {
+        const int x = pass / (32 / PR), i0 = pass % (32 / PR) / (4 / Q) * 4 + pass % (4 / Q) * Q;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int y = 0; y < WF; y++)
+#pragma unroll
+          for (int i = 0; i < Q; i++) box[(g * Q + i) * (WF * 32) + y * 32 + j] = acc[x][y][i0 + i];
+#pragma unroll
+        for (int z = 0; z < PU; z++) {
+          const int q = pass * PU + z;
+          float f[V];
+#pragma unroll
+          for (int v = 0; v < V; v++) f[v] = box[(z * DOWN + rl) * (WF * 32) + cl + v];
+          if (row0 + down(q) < m && left > 0) finish(f, b, u[q % RING], o + down(q) * ld, p + down(q) * ld_res, left);
+          if (q + RING < UNITS && add && row0 + down(q + RING) < m) u[q % RING] = load16(p + down(q + RING) * ld_res);
+        }
+      }
+      if (tile >= tile_end) return;
+    }
   }
 }
 
@@ -430,6 +468,7 @@ int launch_tile(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8
                 const T* res, long long ld_res, T* out, long long ld) {
   typedef Mx4Tile<AF, WF, WM, WN, KW> C;
   const int mt = (m + C::BM - 1) / C::BM, nt = (n + C::BN - 1) / C::BN;
+  const int tiles = (mt * nt + 7) / 8 * 8;
   const void* fn = (const void*)mx4_gemm_tile_k<T, AF, WF, WM, WN, KW>;
   // more LDS than a launch gets by default: an attribute of the kernel on one device, set once for each
   static std::atomic<bool> set[64];
@@ -439,34 +478,26 @@ int launch_tile(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8
     if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS) != hipSuccess) return PAHQ_EHIP;
     set[dev].store(true, std::memory_order_release);
   }
-  hipLaunchKernelGGL((mx4_gemm_tile_k<T, AF, WF, WM, WN, KW>), dim3((mt * nt + 7) / 8 * 8), dim3(C::THREADS), C::LDS, st, a, as, w, ws, m, n, slabs, mt,
+  hipLaunchKernelGGL((mx4_gemm_tile_k<T, AF, WF, WM, WN, KW>), dim3(KW > 1 ? tiles : std::min(tiles, 256 * C::PER_CU)), dim3(C::THREADS), C::LDS, st, a, as, w, ws, m, n, slabs, mt,
                      nt, bias, res, ld_res, out, ld);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
 template <typename T>
 int gemm_as(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs, const float* bias,
             const T* res, long long ld_res, T* out, long long ld) {
+  if (mx4_few(m, n, slabs)) {
+    hipLaunchKernelGGL(mx4_gemm_few_k<T>, dim3((unsigned)((n + 15) / 16)), dim3(512), 0, st, a, as, w, ws, m, n, slabs, bias, res, ld_res, out, ld);
+    return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
+  }
 #define TILE(...) return launch_tile<T, __VA_ARGS__>(st, a, as, w, ws, m, n, slabs, bias, res, ld_res, out, ld)
-  static const int force = getenv("MXV") ? atoi(getenv("MXV")) : 0;
-  if (force == 1) TILE(1, 1, 1, 1, 4);
-  if (force == 2) TILE(1, 1, 1, 1, 8);
-  if (force == 3) TILE(2, 2, 1, 1, 4);
-  if (force == 9) TILE(2, 2, 1, 1, 2);
-  if (force == 6) TILE(2, 2, 2, 2, 1);
-  if (force == 5) TILE(2, 4, 4, 2, 1);
-  if (m > 64 && slabs < (1 << 16)) {
-    if ((long long)((m + 255) / 256) * ((n + 255) / 256) >= 256) TILE(2, 4, 4, 2, 1);
-    TILE(2, 2, 2, 2, 1);
+  switch (mx4_form(m, n, slabs)) {
+    case 0: TILE(1, 1, 1, 1, 4);
+    case 1: TILE(2, 2, 1, 1, 4);
+    case 2: TILE(2, 2, 1, 1, 2);
+    case 3: TILE(2, 2, 2, 2, 1);
+    default: TILE(2, 4, 4, 2, 1);
   }
 #undef TILE
-  const unsigned nt = (unsigned)((n + 15) / 16);
-#define FEW(MT_, WAVES_) hipLaunchKernelGGL((mx4_gemm_few_k<T, MT_, WAVES_>), dim3(nt, (m + 16 * MT_ - 1) / (16 * MT_)), dim3(WAVES_ * 64), 0, st, a, as, w, \
-                                            ws, m, n, slabs, bias, res, ld_res, out, ld)
-  if (m <= 16) FEW(1, 8);
-  else if (m <= 32) FEW(2, 8);
-  else FEW(4, 4);
-#undef FEW
-  return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
 // rows of codes are 16-byte loads, rows of scales 8-byte ones
 bool held_aligned(const void* codes, const void* scales) { return ((uintptr_t)codes & 15) == 0 && ((uintptr_t)scales & 7) == 0; }
@@ -529,8 +560,8 @@ extern "C" int pahq_mx4_gemm(void* hip_stream, const uint8_t* a_codes, const uin
   if (!a_codes || !a_scales || !w_codes || !w_scales || !out || ld_out < n || (residual && ld_residual < n)) return PAHQ_EINVAL;
   if (!held_aligned(a_codes, a_scales) || !held_aligned(w_codes, w_scales)) return PAHQ_EINVAL;
   if ((uintptr_t)out % eb || (uintptr_t)residual % eb || (uintptr_t)bias % 4) return PAHQ_EINVAL;
-  // rows of the grid are counted in 16 bits, columns and groups in 32
-  if (too_big(m, k) || too_big(n, k) || m > 65535 * 16) return PAHQ_ETOOBIG;
+  // a tile's rows are addressed by 32 bits, tiles counted by 31
+  if (k > PAHQ_MX4_MAX_K || too_big(m, k) || too_big(n, k) || ((m + 31ll) / 32) * ((n + 31ll) / 32) >= (1ll << 31) - 8) return PAHQ_ETOOBIG;
   const size_t ob = (size_t)(((m - 1ll) * ld_out + n) * eb), ab = code_bytes(m, k), wb = code_bytes(n, k);
   if (overlap(out, ob, a_codes, ab) || overlap(out, ob, a_scales, ab / 16) || overlap(out, ob, w_codes, wb) || overlap(out, ob, w_scales, wb / 16) ||
       (bias && overlap(out, ob, bias, (size_t)n * 4)))

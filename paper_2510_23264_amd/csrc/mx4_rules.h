@@ -1,0 +1,41 @@
+// Which kernel a product of rows in 4 microscaled bits takes.  No GPU type in it, so that CPU tests compile it.
+#pragma once
+#include <math.h>
+
+namespace pahq {
+
+// Up to 16 rows whose sums are short or whose results are few: one 16 x 16 product a wave from global memory is done before a
+// tile's first stage is there (4096 x 4096 4.4 us, in tiles 4.9; 3 x 14720 x 2959 8.1, in tiles 5.5).
+inline bool mx4_few(long long m, long long n, int slabs) { return m <= 16 && (slabs < 6 || n * slabs < 80000); }
+
+// Otherwise tiles of `tile` x `tile`, the sum over k shared by `groups` groups of waves.  The times in microseconds are fitted to
+// 400 random sizes from 17 x 16 x 32 to 8192 x 50000 x 12000 (bfloat16 results): one workgroup alone takes
+// launch + start + slab * (its slabs of 256 elements of k); each further one of a compute unit `round` of that, where only one
+// fits (whole) a whole round of the chip half of the time.  The form with the least estimate took 1.01 of the best one's time in
+// the mean, 1.2 at most.  A last round of 256 x 256 tiles that leaves most of the chip without one stays as it is: as smaller
+// tiles in a launch of their own it cost 250 us instead of 244 (8192 x 11008 x 4096), for the chip's power bounds the whole.
+struct Mx4Form { int tile, groups; float launch, start, slab, round; bool whole; };
+constexpr int MX4_FORMS = 5;
+constexpr Mx4Form mx4_forms[MX4_FORMS] = {
+    {32, 4, 3.2f, 0.4f, 0.31f, 1.5f, false},      //  100 x 2304 x 768 4.4 us (64 x 64 in two groups 5.5)
+    {64, 4, 3.6f, 1.2f, 0.54f, 2.4f, true},       //  256 x 4096 x 4096 8.1 (32 x 32 11.0)
+    {64, 2, 2.8f, 1.9f, 0.61f, 0.8f, false},      //  800 x 2304 x 768 6.3 (32 x 32 10.2, 128 x 128 7.7)
+    {128, 1, 1.1f, 4.5f, 0.85f, 0.6f, false},     // 2048 x 4096 x 4096 29 (64 x 64 42, 256 x 256 38)
+    {256, 1, 4.0f, 8.9f, 1.53f, 1.27f, true},     // 8192 x 4096 x 11008 180 (128 x 128 222)
+};
+inline float mx4_estimate(const Mx4Form& f, long long m, long long n, int slabs) {
+  const float r = (float)((m + f.tile - 1) / f.tile) * (float)((n + f.tile - 1) / f.tile) / 256;
+  const float further = r <= 1 ? 0 : f.whole ? 0.5f * (ceilf(r) + r) - 1 : r - 1;
+  return f.launch + (f.start + f.slab * ((slabs + f.groups - 1) / f.groups)) * (1 + f.round * further);
+}
+inline int mx4_form(long long m, long long n, int slabs) {
+  int best = 0;
+  float least = 0;
+  for (int i = 0; i < MX4_FORMS; i++) {
+    const float t = mx4_estimate(mx4_forms[i], m, n, slabs);
+    if (i == 0 || t < least) { least = t; best = i; }
+  }
+  return best;
+}
+
+}  // namespace pahq

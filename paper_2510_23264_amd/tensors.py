@@ -50,18 +50,17 @@ def _row_stride(t):
     """Elements from row to row of a matrix whose rows are contiguous; None if they are not.  Of a single row or column torch
     reports any stride."""
     rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
-        return None
-    if rows <= 1:
-        return max(cols, 1)
-    return t.stride(0) if t.stride(0) >= cols else None
+    if t.is_contiguous() or rows <= 1 and (cols <= 1 or t.stride(1) == 1):
+        return cols or 1
+    ld, step = t.stride()
+    return ld if (step == 1 or cols <= 1) and ld >= cols else None
 
 
 class Mx4:
     """A matrix [rows][cols] in 4 microscaled bits: `codes` uint8 [rows][K / 2] and `scales` uint8 [rows][K / 32], K = cols
     rounded up to 256, both contiguous on one device (the format is described in include/pahq.h)."""
 
-    __slots__ = ("codes", "scales", "cols")
+    __slots__ = ("rows", "cols", "device", "_both", "_codes", "_scales")
 
     def __init__(self, codes, scales, cols):
         k = -(-int(cols) // 256) * 256
@@ -69,25 +68,39 @@ class Mx4:
         _need(codes.dim() == 2 and cols >= 1 and tuple(codes.shape) == (codes.shape[0], k // 2)
               and tuple(scales.shape) == (codes.shape[0], k // 32), "codes [rows][K / 2], scales [rows][K / 32], K = cols rounded up to 256")
         _need(codes.is_contiguous() and scales.is_contiguous(), "codes and scales: contiguous")
-        self.codes, self.scales, self.cols = codes, scales, int(cols)
+        self.rows, self.cols, self.device = codes.shape[0], int(cols), codes.device
+        self._both, self._codes, self._scales = None, codes, scales
 
     @classmethod
     def empty(cls, rows, cols, device="cuda"):
+        """Memory for a matrix: one allocation, the scales behind the codes."""
         groups = -(-int(cols) // 256)
-        _need(rows >= 0 and groups >= 1, "rows >= 0, cols >= 1")
-        q = cls.__new__(cls)                            # nothing to check: of the right form as made
-        q.codes = torch.empty((rows, groups * 128), dtype=torch.uint8, device=device)
-        q.scales = torch.empty((rows, groups * 8), dtype=torch.uint8, device=device)
-        q.cols = int(cols)
+        if rows < 0 or groups < 1:
+            raise ValueError("rows >= 0, cols >= 1")
+        q = cls.__new__(cls)
+        q._both = torch.empty(rows * groups * 136, dtype=torch.uint8, device=device)
+        q.rows, q.cols, q.device, q._codes, q._scales = rows, int(cols), q._both.device, None, None
         return q
 
     @property
-    def rows(self):
-        return self.codes.shape[0]
+    def codes(self):
+        if self._codes is None:
+            n = self._both.numel() // 17 * 16
+            self._codes = self._both[:n].view(self.rows, -(-self.cols // 256) * 128)
+        return self._codes
 
     @property
-    def device(self):
-        return self.codes.device
+    def scales(self):
+        if self._scales is None:
+            n = self._both.numel() // 17 * 16
+            self._scales = self._both[n:].view(self.rows, -(-self.cols // 256) * 8)
+        return self._scales
+
+    def _pointers(self):
+        if self._both is not None:
+            at = self._both.data_ptr()
+            return at, at + self.rows * -(-self.cols // 256) * 128
+        return self._codes.data_ptr(), self._scales.data_ptr()
 
 
 def mx4_quantize(x, by="rows", out=None):
@@ -109,17 +122,18 @@ def mx4_quantize(x, by="rows", out=None):
     _need(cols >= 1, "rows of at least one element")
     if out is None:
         out = Mx4.empty(rows, cols, x.device)
-    else:
-        _need(out.rows == rows and out.cols == cols and out.device == x.device, "out: of the result's shape, on x's device")
+    elif not (out.rows == rows and out.cols == cols and out.device == x.device):
+        raise ValueError("out: of the result's shape, on x's device")
     if rows:
-        _call("pahq_mx4_quantize", x.device, x.data_ptr(), _DTYPES[x.dtype], rows, cols, ld, 1 if down else 0, out.codes.data_ptr(), out.scales.data_ptr())
+        _call("pahq_mx4_quantize", out.device, x.data_ptr(), _DTYPES[x.dtype], rows, cols, ld, 1 if down else 0, *out._pointers())
     return out
 
 
 def _result(out, rows, cols, dtype, device):
     """(tensor, row stride): `out` checked, or a new one."""
     if out is None:
-        _need(dtype in _DTYPES, "dtype: float32, bfloat16 or float16")
+        if dtype not in _DTYPES:
+            raise ValueError("dtype: float32, bfloat16 or float16")
         return torch.empty((rows, cols), dtype=dtype, device=device), max(cols, 1)
     ld = _row_stride(out) if out.dim() == 2 else None
     if not (out.shape == (rows, cols) and out.dtype in _DTYPES and out.device == device and ld is not None and not _tracked(out)):
@@ -131,21 +145,20 @@ def mx4_dequantize(q, dtype=torch.float32, out=None):
     """The values of an Mx4, exact in float32 and bfloat16.  `out` brings its own dtype."""
     out, ld = _result(out, q.rows, q.cols, dtype, q.device)
     if q.rows:
-        _call("pahq_mx4_dequantize", q.device, q.codes.data_ptr(), q.scales.data_ptr(), q.rows, q.cols, out.data_ptr(), _DTYPES[out.dtype], ld)
+        _call("pahq_mx4_dequantize", q.device, *q._pointers(), q.rows, q.cols, out.data_ptr(), _DTYPES[out.dtype], ld)
     return out
 
 
 def mx4_gemm(a, w, bias=None, residual=None, dtype=torch.float32, out=None):
     """a Mx4 [m][k], w Mx4 [n][k] -> a w^T (+ bias float32 [n]) (+ residual [m][n] of the result's dtype; it may be `out`)."""
-    device = a.codes.device
-    if a.cols != w.cols or device != w.codes.device:
+    m, n, device = a.rows, w.rows, a.device
+    if a.cols != w.cols or device != w.device:
         raise ValueError("a [m][k] and w [n][k] on one device")
-    m, n = a.codes.shape[0], w.codes.shape[0]
     out, ld = _result(out, m, n, dtype, device)
     bp = rp = None
     ld_res = ld
     if bias is not None:
-        if not (bias.dtype == torch.float32 and bias.shape == (n,) and bias.device == device and (n <= 1 or bias.stride(0) == 1)
+        if not (bias.dtype == torch.float32 and bias.shape == (n,) and bias.device == device and bias.is_contiguous()
                 and not _tracked(bias)):
             raise ValueError("bias: float32 [n], contiguous, without a gradient")
         bp = bias.data_ptr()
@@ -156,8 +169,7 @@ def mx4_gemm(a, w, bias=None, residual=None, dtype=torch.float32, out=None):
             raise ValueError("residual: [m][n] of the result's dtype, rows contiguous, without a gradient")
         rp = residual.data_ptr()
     if m and n:
-        _call("pahq_mx4_gemm", device, a.codes.data_ptr(), a.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), m, n, a.cols, bp, rp, ld_res,
-              out.data_ptr(), _DTYPES[out.dtype], ld)
+        _call("pahq_mx4_gemm", device, *a._pointers(), *w._pointers(), m, n, a.cols, bp, rp, ld_res, out.data_ptr(), _DTYPES[out.dtype], ld)
     return out
 
 
@@ -174,6 +186,8 @@ def rotary_table(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=0.
 
 def _strides(t):
     tokens, heads, d = t.shape
+    if t.is_contiguous():
+        return heads * d, d
     st, sh, se = t.stride()
     if se != 1 and d > 1:
         raise ValueError("the elements of a head: contiguous")
@@ -221,10 +235,10 @@ def rotary(x, positions, table, layout="half", magnitude=1.0, inverse=False, out
         raise ValueError("x: [tokens][heads][d_head] in float32, bfloat16 or float16 on the device")
     tokens, _, d = x.shape
     if not (positions.dtype == torch.int64 and positions.shape == (tokens,) and positions.device == x.device
-            and (tokens <= 1 or positions.stride(0) == 1)):
+            and positions.is_contiguous()):
         raise ValueError("positions: int64 [tokens], contiguous, on x's device")
     if not (table.dtype == torch.int64 and table.dim() == 1 and table.device == x.device and 2 <= 2 * table.numel() <= d
-            and (table.numel() <= 1 or table.stride(0) == 1)):
+            and table.is_contiguous()):
         raise ValueError("table: from rotary_table, on x's device, for at most d_head elements")
     if layout not in _LAYOUTS:
         raise ValueError("layout: 'half' or 'interleaved'")

@@ -1,8 +1,12 @@
 """Matrices in 4 microscaled bits on the device: codes and scales bit for bit against the definition written out in Fractions
 and 64 bits, values, and products against sums in 64 bits."""
+import os
+import sys
+
 import numpy as np
 import pytest
 
+sys.path.insert(0, os.path.dirname(__file__))
 pytestmark = pytest.mark.gpu
 
 GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
@@ -180,6 +184,48 @@ def test_products_whose_sums_are_exact(P, m, n, k):
     for t in (torch.float32, torch.bfloat16, torch.float16):
         got = P.mx4_gemm(device(P, a, sa, k), device(P, w, sw, k), bias=torch.from_numpy(bias).float().cuda(), residual=torch.from_numpy(res).to(t).cuda(), dtype=t)
         assert torch.equal(got.cpu(), torch.from_numpy(want + bias + res).to(t)), t
+
+
+# the smallest sizes found for every form of the product (tests/mx4_rules.py) with 1 to 9 slabs of 256 elements of k, one tile a
+# workgroup and several; none a multiple of a tile
+FORM_SIZES = [
+    (0, 17, 17, 56), (0, 18, 19, 568), (0, 18, 17, 824), (0, 17, 18, 1080), (0, 17, 17, 2304), (0, 12, 12001, 2104),
+    (1, 67, 6510, 568), (1, 65, 6589, 824), (1, 33, 8993, 1080), (1, 33, 8119, 2104),
+    (2, 70, 6497, 56), (2, 67, 6934, 312), (2, 65, 8205, 568), (2, 68, 8278, 824), (2, 65, 8703, 2104),
+    (3, 132, 8555, 56), (3, 899, 8233, 56), (3, 195, 8526, 312), (3, 1547, 5068, 312), (3, 199, 8402, 568), (3, 903, 8637, 824), (3, 1158, 6608, 1080),
+    (4, 2713, 5151, 56), (4, 3480, 8322, 56), (4, 3503, 8067, 312), (4, 3491, 7603, 568), (4, 1444, 8464, 824), (4, 3233, 7940, 824), (4, 3297, 7718, 1080)]
+
+
+@pytest.mark.parametrize("form, m, n, k", FORM_SIZES)
+def test_every_form_at_its_edges(P, form, m, n, k):
+    """Exact sums again (see above), with and without bias and residual, results in a type each; the sums in 64 bits on the device.
+    Memory around the rows of the result stays as it was, and the same call gives the same bits."""
+    import torch
+    import mx4_rules
+    assert mx4_rules.form(m, n, k) == form
+    g = torch.Generator(device="cuda").manual_seed(m + n + k)
+    grid = torch.tensor(VALUE, device="cuda")
+
+    def matrix(rows):
+        kp = -(-k // 256) * 256
+        code = torch.randint(0, 16, (rows, kp), generator=g, device="cuda", dtype=torch.uint8)
+        code[:, k:] = 0
+        scale = torch.randint(126, 128, (rows, kp // 32), generator=g, device="cuda", dtype=torch.uint8)
+        value = grid[code.long()] * torch.exp2(scale.double() - 127).repeat_interleave(32, 1)
+        return P.Mx4(code[:, 0::2] | code[:, 1::2] << 4, scale, k), value
+    (a, av), (w, wv) = matrix(m), matrix(n)
+    want = av @ wv.t()
+    bias = torch.randint(-64, 64, (n,), generator=g, device="cuda").float() / 4
+    for t, extra in ((torch.float32, False), (torch.bfloat16, True), (torch.float16, False), (torch.float32, True)):
+        buf = torch.full((m + 2, n + 3), 9.0, dtype=t, device="cuda")
+        out = buf[1:m + 1, 1:n + 1]
+        res = torch.randint(-64, 64, (m, n), generator=g, device="cuda").to(t) / 4 if extra else None
+        P.mx4_gemm(a, w, bias=bias if extra else None, residual=res, out=out)
+        assert torch.equal(out, (want + bias + res.double() if extra else want).to(t)), t
+        again = P.mx4_gemm(a, w, bias=bias if extra else None, residual=res, dtype=t)
+        assert torch.equal(out, again)
+        out.fill_(9.0)
+        assert (buf == 9.0).all()
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
