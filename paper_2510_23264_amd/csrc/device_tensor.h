@@ -64,13 +64,10 @@ __device__ __forceinline__ void store8(T* p, int left, const float* v) {
 
 // Sixteen bytes of elements as four registers (an array of 16-bit elements takes one each), at any alignment of the element.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-template <int A> struct __attribute__((packed, aligned(A))) Lines { u32x4 v; };
-template <typename T> __device__ __forceinline__ u32x4 load16(const T* p) {
-  return ((const Lines<sizeof(T)>*)p)->v;
-}
-template <typename T> __device__ __forceinline__ void store16(T* p, u32x4 v) {
-  ((Lines<sizeof(T)>*)p)->v = v;
-}
+typedef uint32_t u32x4_at_2 __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T> __device__ __forceinline__ u32x4 load16(const T* p) { return *(const u32x4_at_2*)p; }
+// A store that does not stay in the caches (non-temporal)
+template <typename T> __device__ __forceinline__ void store16_nt(T* p, u32x4 v) { __builtin_nontemporal_store((u32x4_at_2)v, (u32x4_at_2*)p); }
 template <typename T> __device__ __forceinline__ float element(u32x4 v, int i) {
   if (sizeof(T) == 4) return __uint_as_float(v[i]);
   const uint16_t h = (uint16_t)(v[i / 2] >> (i % 2 * 16));
