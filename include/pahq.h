@@ -211,6 +211,14 @@ int pahq_clean_cache(pahq_model*, const int32_t* clean_tok, const int32_t* corru
 enum { PAHQ_METRIC_KL = 0, PAHQ_METRIC_LOGIT_DIFF = 1 };
 int pahq_set_metric(pahq_model*, int32_t metric, const int32_t* answer_ids, const int32_t* distractor_ids);
 
+/* The rotary positions of a model with PAHQ_POS_ROPE, in place of the plain ones over the whole head: queries and keys turn in
+ * the pairs (i, i + d_head / 2), i < rot_dim / 2, by position * table[i] (a fraction of a turn in 64 binary digits, from
+ * pahq_rotary_table; HOST, rot_dim / 2 entries) and are multiplied by `magnitude`; the other pairs stay as they are.  A model
+ * whose pairs lie otherwise -- neighbouring elements, or the first rot_dim elements of a head -- is given with the columns
+ * of W_Q, W_K, b_Q and b_K in this order (a head's scores do not depend on it).  PAHQ_ESTATE without PAHQ_POS_ROPE.  Call before
+ * pahq_clean_cache: like pahq_set_metric it drops the caches. */
+int pahq_set_rotary(pahq_model*, const uint64_t* table, int32_t rot_dim, float magnitude);
+
 /* Evaluates n candidate edges (sender_ids[i] -> receiver) INDEPENDENTLY: the
  * i-th result is the batch-mean KL(P_ref || P_i) at the last position, where
  * P_i is the clean run with the current removed set plus that one edge

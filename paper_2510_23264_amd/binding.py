@@ -90,6 +90,7 @@ def lib():
             "pahq_acdc_sweep_grid": [C.c_void_p, f32p, C.c_int32, i32p, C.c_int32, u8p, i64p],
             "pahq_eval_circuit": [C.c_void_p, u8p, u8p, f32p, f32p],
             "pahq_set_metric": [C.c_void_p, C.c_int32, i32p, i32p],
+            "pahq_set_rotary": [C.c_void_p, C.POINTER(C.c_uint64), C.c_int32, C.c_float],
             "pahq_set_removed": [C.c_void_p, u8p], "pahq_get_removed": [C.c_void_p, u8p],
             "pahq_set_dead_node_skipping": [C.c_void_p, C.c_int32],
             "pahq_prefetch_heads": [C.c_void_p, C.c_int32, C.c_uint64],
@@ -189,12 +190,38 @@ def quantize_rows_noalloc(x, codes, scales, stream=None):
          "pahq_quantize_rows_noalloc")
 
 
+ROTARY_SCALING = {"none": 0, "linear": 1, "base": 2, "bands": 3}
+
+
+def rotary_entries(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=0.0, turns=(1.0, 32.0)):
+    """uint64 [rot_dim / 2]: how far each pair turns in one position, in units of 2^-64 turn (pahq_rotary_table)."""
+    if scaling not in ROTARY_SCALING:
+        raise ValueError("scaling: none, linear, base or bands")
+    out = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.uint64)
+    _chk(lib().pahq_rotary_table(int(rot_dim), float(theta), ROTARY_SCALING[scaling], float(factor), float(original), float(turns[0]),
+                                 float(turns[1]), _ptr(out, C.c_uint64)), "pahq_rotary_table")
+    return out
+
+
+def rotary_columns(d_head, rot_dim, layout):
+    """Which column of a head's W_Q / W_K stands where pahq_set_rotary expects the pairs: pair i in columns i and i + d_head / 2."""
+    if layout not in ("half", "interleaved") or rot_dim < 2 or rot_dim % 2 or rot_dim > d_head:
+        raise ValueError("layout: half or interleaved; rot_dim: even, 2 .. d_head")
+    pairs, rest = rot_dim // 2, (d_head - rot_dim) // 2
+    a, b = (np.arange(pairs), np.arange(pairs) + pairs) if layout == "half" else (2 * np.arange(pairs), 2 * np.arange(pairs) + 1)
+    still = rot_dim + np.arange(rest)
+    return np.concatenate([a, still, b, still + rest])
+
+
 class Model:
     """pahq_init_model + the calls on the handle.  `weights`: dict of float32 numpy arrays
-    (layouts as in include/pahq.h)."""
+    (layouts as in include/pahq.h).  `rotary` (models with rotary positions): a dict of rot_dim, layout ("half", the default,
+    or "interleaved"), magnitude and the arguments of rotary_entries, where the positions are not the plain ones over the
+    whole head; theta defaults to the shape's."""
 
     def __init__(self, shape, weights, B, S, precision=PAHQ, max_batch_edges=32, mma=MMA_F16_EXACT, device="cuda:0",
-                 workspace_bytes_override=None, low_bits=8, nonattn_bf16=False, split_qkv=True, fp32_on_host=False):
+                 workspace_bytes_override=None, low_bits=8, nonattn_bf16=False, split_qkv=True, fp32_on_host=False,
+                 rotary=None):
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("no HIP device: libpahq has no CPU path")
@@ -210,6 +237,13 @@ class Model:
         self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         base = (self.workspace.data_ptr() + 255) // 256 * 256
         self.stream = torch.cuda.current_stream(self.device)
+        self._columns = None
+        if rotary is not None:
+            r = dict(rotary)
+            layout, magnitude, rot_dim = r.pop("layout", "half"), r.pop("magnitude", 1.0), int(r.pop("rot_dim"))
+            table = rotary_entries(rot_dim, **dict({"theta": shape.rope_theta}, **r))
+            self._columns = rotary_columns(shape.d_head, rot_dim, layout)
+            weights = dict(weights, **{n: weights[n][..., self._columns] for n in ("W_Q", "W_K", "b_Q", "b_K") if weights.get(n) is not None})
         w = Weights()
         self._keep = []
         for n in _W_NAMES:
@@ -227,6 +261,16 @@ class Model:
         self.h = h
         self._keep = []
         self.workspace_bytes = nbytes
+        if rotary is not None:
+            _chk(lib().pahq_set_rotary(self.h, _ptr(table, C.c_uint64), rot_dim, C.c_float(magnitude)), "pahq_set_rotary")
+
+    def _in_given_order(self, which, a):
+        """Columns of a head's query or key weights as the caller gave them."""
+        if self._columns is None or which not in (W_Q, W_K):
+            return a
+        out = np.empty_like(a)
+        out[..., self._columns] = a
+        return out
 
     def close(self):
         if getattr(self, "h", None):
@@ -377,7 +421,7 @@ class Model:
         scale = C.c_float()
         _chk(lib().pahq_get_weight_q(self.h, which, layer, head, _ptr(codes, C.c_uint8), C.byref(scale)),
              "pahq_get_weight_q")
-        return codes, np.float32(scale.value)
+        return self._in_given_order(which, codes), np.float32(scale.value)
 
     def quantize_rows(self, x, site=None):
         """site None: pahq_quantize_rows; 0 / 1 / 2: pahq_quantize_rows_site (hidden, norm, attention quantiser)."""
@@ -398,7 +442,7 @@ class Model:
         projection (low_bits = 16)."""
         out = np.empty(shape, dtype=np.uint16)
         _chk(lib().pahq_get_weight_bf16(self.h, int(which), int(layer), int(head), _ptr(out, C.c_uint16)), "pahq_get_weight_bf16")
-        return out
+        return self._in_given_order(which, out)
 
     def round_rows_bf16(self, x, site):
         x = np.ascontiguousarray(x, dtype=np.float32)

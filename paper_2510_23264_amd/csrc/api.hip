@@ -621,6 +621,28 @@ int pahq_set_metric(pahq_model* M, int32_t metric, const int32_t* answer_ids, co
   return PAHQ_OK;
 }
 
+int pahq_set_rotary(pahq_model* M, const uint64_t* table, int32_t rot_dim, float magnitude) {
+  if (!M || !table || rot_dim < 2 || (rot_dim & 1) || rot_dim > M->dh || !std::isfinite(magnitude)) return PAHQ_EINVAL;
+  if (!M->rope_tab) return PAHQ_ESTATE;
+  // the attention kernels' table: (cos, sin) of every position and pair, angles exact to 2^-64 turn, rounded once
+  constexpr int POSITIONS = 128, MAX_PAIRS = 64;
+  float tab[POSITIONS * MAX_PAIRS * 2];
+  const int pairs = (int)M->dh / 2;
+  for (int pos = 0; pos < POSITIONS; pos++)
+    for (int i = 0; i < pairs; i++) {
+      float* t = tab + (pos * pairs + i) * 2;
+      const bool turns = i < rot_dim / 2;
+      const double phi = turns ? (double)(int64_t)(table[i] * (uint64_t)pos) * (6.283185307179586476925 / 18446744073709551616.0) : 0.0;
+      t[0] = turns ? (float)(magnitude * std::cos(phi)) : 1.f;
+      t[1] = turns ? (float)(magnitude * std::sin(phi)) : 0.f;
+    }
+  HIPCHK(hipMemcpyAsync(M->rope_tab, tab, sizeof(float) * POSITIONS * pairs * 2, hipMemcpyHostToDevice, M->stream));
+  HIPCHK(hipStreamSynchronize(M->stream));
+  M->has_cache = false;          // every cached activation behind the first layer's queries and keys depends on it
+  M->pi_l = M->pi_h = -2; M->ref_layer = -1;
+  return PAHQ_OK;
+}
+
 // Independent candidates (sender_ids[i] -> receiver) for one receiver, or -- recv3 -- for the query, key and value
 // inputs of one head side by side: cnt[c] candidates of channel c, senders and results in channel order.  The device
 // batches of a call are queued back to back and the host waits once per ncap candidates: batch b reads its senders

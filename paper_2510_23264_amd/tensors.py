@@ -7,14 +7,12 @@ otherwise; nothing is copied behind the caller's back.  Arguments that do not fi
 library raises PahqError."""
 from __future__ import annotations
 
-import ctypes as C
-
+import numpy as np
 import torch
 
-from .binding import lib, _chk
+from .binding import lib, _chk, rotary_entries
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-_SCALING = {"none": 0, "linear": 1, "base": 2, "bands": 3}
 _LAYOUTS = {"half": 0, "interleaved": 1}
 
 
@@ -177,11 +175,7 @@ def rotary_table(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=0.
     """The table `rotary` takes, int64 [rot_dim / 2] (bit patterns): frequencies theta^(-2 i / rot_dim), as they are
     ("none"), divided by `factor` ("linear"), of a stretched theta ("base"), or divided where a pair turns less than turns[0]
     times over `original` positions, kept from turns[1] times on and blended in between ("bands")."""
-    _need(scaling in _SCALING, "scaling: none, linear, base or bands")
-    host = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.int64)
-    _chk(lib().pahq_rotary_table(int(rot_dim), float(theta), _SCALING[scaling], float(factor), float(original), float(turns[0]), float(turns[1]),
-                                 C.cast(host.data_ptr(), C.POINTER(C.c_uint64))), "pahq_rotary_table")
-    return host.to(device)
+    return torch.from_numpy(rotary_entries(rot_dim, theta, scaling, factor, original, turns).view(np.int64)).to(device)
 
 
 def _strides(t):
