@@ -61,28 +61,54 @@ __global__ __launch_bounds__(256) void mx4_rows_quant_k(const T* x, long long ld
   if ((l & 3) == 0) scales[(long long)u * 8 + (l >> 2)] = (uint8_t)s;
 }
 
-// x [cols][rows] (the masters' layout [k][n]): one thread holds a block of 32 down a column, neighbouring threads
-// neighbouring columns.  Workgroup: 64 columns, 128 elements of each.
+// x [cols][rows] (the masters' layout [k][n]): one thread holds blocks of 32 down the columns of one word of a row, neighbouring
+// threads neighbouring words.  Workgroup: 64 words, 256 elements down, a block a wave; the codes go through LDS so that a row's
+// 128 bytes leave together (as 16 bytes from each thread 4096 x 4096 in bfloat16 took 17 us, 4096 x 11008 in fp32 34).
 template <typename T>
-__global__ __launch_bounds__(256) void mx4_cols_quant_k(const T* x, long long ld, int rows, int cols, int blocks, uint8_t* codes, uint8_t* scales) {
-  const int row = blockIdx.x * 64 + (threadIdx.x & 63), b = blockIdx.y * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  float v[32];
-  uint32_t top = 0;
+__global__ __launch_bounds__(512) void mx4_cols_quant_k(const T* x, long long ld, int rows, int cols, int groups, uint8_t* codes, uint8_t* scales) {
+  constexpr int N = 4 / sizeof(T), ROWS = 64 * N;
+  __shared__ uint4 held[ROWS * 8];                      // [row][block], blocks XOR-swizzled by the row
+  __shared__ __align__(8) uint8_t held_scales[ROWS * 8];
+  const int lane = threadIdx.x & 63, b = threadIdx.x >> 6, row0 = blockIdx.x * ROWS, row = row0 + lane * N, here = min(N, rows - row);
+  {
+    const int k0 = blockIdx.y * 256 + b * 32;
+    float v[N][32];
+    uint32_t top[N] = {};
 #pragma unroll
-  for (int j = 0; j < 32; j++) {
-    const int k = b * 32 + j;
-    v[j] = k < cols ? as_float(x[(long long)k * ld + row]) : 0.f;
-    top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+    for (int j = 0; j < 32; j++) {
+      const T* const p = x + (long long)(k0 + j) * ld + row;
+      Pack<T, N> q = {};
+      if (k0 + j < cols) {
+        if (here == N) q = *(const Pack<T, N>*)p;
+        else if (here > 0) q.v[0] = p[0];
+      }
+#pragma unroll
+      for (int c = 0; c < N; c++) {
+        v[c][j] = as_float(q.v[c]);
+        top[c] = max(top[c], __float_as_uint(v[c][j]) & 0x7FFFFFFFu);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < N; c++) {
+      const int r = lane * N + c;
+      const uint32_t s = mx4_scale_of(top[c]);
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (s != 255u) {
+        const float inv = mx4_inverse(s);
+        w = make_uint4(mx4_encode8(v[c], inv), mx4_encode8(v[c] + 8, inv), mx4_encode8(v[c] + 16, inv), mx4_encode8(v[c] + 24, inv));
+      }
+      held[r * 8 + (b ^ (r & 7))] = w;
+      held_scales[r * 8 + b] = (uint8_t)s;
+    }
   }
-  const uint32_t s = mx4_scale_of(top);
-  uint4 w = make_uint4(0, 0, 0, 0);
-  if (s != 255u) {
-    const float inv = mx4_inverse(s);
-    w = make_uint4(mx4_encode8(v, inv), mx4_encode8(v + 8, inv), mx4_encode8(v + 16, inv), mx4_encode8(v + 24, inv));
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < ROWS / 64; i++) {
+    const int r = i * 64 + (threadIdx.x >> 3), c = threadIdx.x & 7;
+    if (row0 + r < rows) *(uint4*)(codes + ((long long)(row0 + r) * groups + blockIdx.y) * 128 + c * 16) = held[r * 8 + (c ^ (r & 7))];
   }
-  *(uint4*)(codes + ((long long)row * blocks + b) * 16) = w;
-  scales[(long long)row * blocks + b] = (uint8_t)s;
+  if (threadIdx.x < ROWS && row0 + threadIdx.x < rows)
+    *(uint2*)(scales + ((long long)(row0 + threadIdx.x) * groups + blockIdx.y) * 8) = *(const uint2*)(held_scales + threadIdx.x * 8);
 }
 
 // ---------------------------------------------------------------- values
@@ -454,7 +480,8 @@ int quantize_as(hipStream_t st, const T* x, int rows, int cols, long long ld, in
     const unsigned wg = (unsigned)(((long long)rows * groups + 7) / 8);
     hipLaunchKernelGGL(mx4_rows_quant_k<T>, dim3(wg), dim3(256), 0, st, x, ld, rows, cols, groups, (uint32_t*)codes, scales);
   } else {
-    hipLaunchKernelGGL(mx4_cols_quant_k<T>, dim3((rows + 63) / 64, groups * 2), dim3(256), 0, st, x, ld, rows, cols, groups * 8, codes, scales);
+    constexpr int per = 64 * 4 / (int)sizeof(T);
+    hipLaunchKernelGGL(mx4_cols_quant_k<T>, dim3((unsigned)((rows + per - 1ll) / per), groups), dim3(512), 0, st, x, ld, rows, cols, groups, codes, scales);
   }
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
@@ -526,8 +553,8 @@ extern "C" int pahq_mx4_quantize(void* hip_stream, const void* x, int32_t dtype,
   const bool down = by == PAHQ_MX4_BY_COLUMNS;
   if (!x || !codes || !scales || ld < (down ? rows : cols)) return PAHQ_EINVAL;
   if (!held_aligned(codes, scales) || (uintptr_t)x % dtype_bytes(dtype)) return PAHQ_EINVAL;
-  // grid.y counts 128 elements down the columns
-  if (too_big(rows, cols) || (down && cols > 65535 * 128)) return PAHQ_ETOOBIG;
+  // grid.y counts 256 elements down the columns
+  if (too_big(rows, cols) || (down && cols > 65535 * 256)) return PAHQ_ETOOBIG;
   const size_t xb = (size_t)((down ? (cols - 1ll) * ld + rows : (rows - 1ll) * ld + cols) * dtype_bytes(dtype)), cb = code_bytes(rows, cols);
   if (overlap(x, xb, codes, cb) || overlap(x, xb, scales, cb / 16) || overlap(codes, cb, scales, cb / 16)) return PAHQ_EINVAL;
   hipStream_t st = (hipStream_t)hip_stream;

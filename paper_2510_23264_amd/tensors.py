@@ -195,7 +195,7 @@ def _strides(t):
 def _rotary(x, positions, table, layout, magnitude, inverse, out):
     tokens, heads, d = x.shape
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
     elif not (out.shape == x.shape and out.dtype == x.dtype and out.device == x.device):
         raise ValueError("out: of x's shape and dtype, on its device")
     if tokens and heads:

@@ -38,7 +38,7 @@ ROTARY = dict(stream=None, x=A, dtype=0, tokens=4, heads=3, d=64, x_token=192, x
     (dict(rows=-1), EINVAL), (dict(cols=0), EINVAL), (dict(dtype=3), EINVAL), (dict(dtype=-1), EINVAL), (dict(by=2), EINVAL), (dict(ld=299), EINVAL),
     (dict(by=1, ld=3), EINVAL), (dict(x=None), EINVAL), (dict(codes=None), EINVAL), (dict(scales=None), EINVAL), (dict(codes=2 * A + 8), EINVAL),
     (dict(scales=3 * A + 4), EINVAL), (dict(x=A + 2), EINVAL), (dict(x=A + 1, dtype=1), EINVAL), (dict(codes=A + 16), EINVAL), (dict(scales=A + 16), EINVAL),
-    (dict(scales=2 * A + 16), EINVAL), (dict(rows=HUGE, cols=513, ld=513), ETOOBIG), (dict(by=1, cols=65535 * 128 + 1), ETOOBIG),
+    (dict(scales=2 * A + 16), EINVAL), (dict(rows=HUGE, cols=513, ld=513), ETOOBIG), (dict(by=1, cols=65535 * 256 + 1), ETOOBIG),
     (dict(rows=0, x=None), 0)])
 def test_quantize_refuses(P, change, code):
     assert P.lib().pahq_mx4_quantize(*dict(QUANTIZE, **change).values()) == code
