@@ -349,3 +349,43 @@ def test_streams_and_replayed_graphs(P):
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(out, want), turn
+
+
+def test_two_streams_at_once(P):
+    """Calls that overlap share nothing: fifty rounds on two streams without waiting, every result that of a call alone."""
+    import torch
+    torch.manual_seed(1)
+    x = [torch.randn(500, 2048, device="cuda") for _ in range(2)]
+    w = P.mx4_quantize(torch.randn(3000, 2048, device="cuda"))
+    want = [P.mx4_gemm(P.mx4_quantize(t), w) for t in x]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(50):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(P.mx4_gemm(P.mx4_quantize(x[i]), w))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[i]) for i in range(2) for o in got[i])
+
+
+def test_more_than_2_to_the_31_elements(P):
+    """Operands and results whose offsets pass 32 bits: the last rows against calls on them alone."""
+    import torch
+    torch.manual_seed(3)
+    x = torch.zeros(2800000, 800, device="cuda", dtype=torch.bfloat16)
+    x[-40:] = torch.randn(40, 800, device="cuda")
+    q = P.mx4_quantize(x)
+    last = P.mx4_quantize(x[-40:])
+    assert x.numel() > 2 ** 31 and torch.equal(q.codes[-40:], last.codes) and torch.equal(q.scales[-40:], last.scales)
+    out = P.mx4_dequantize(q, dtype=torch.bfloat16)
+    assert torch.equal(out[-40:], P.mx4_dequantize(last, dtype=torch.bfloat16)) and not out[:-40].any()
+    del x, q, out
+    m, n = 70001, 40003                              # scales of 1: exact sums, whatever the form
+    a = P.Mx4(torch.randint(0, 256, (m, 128), device="cuda", dtype=torch.uint8), torch.full((m, 8), 127, device="cuda", dtype=torch.uint8), 256)
+    w = P.Mx4(torch.randint(0, 256, (n, 128), device="cuda", dtype=torch.uint8), torch.full((n, 8), 127, device="cuda", dtype=torch.uint8), 256)
+    out = P.mx4_gemm(a, w, dtype=torch.bfloat16)
+    tail = P.mx4_gemm(P.Mx4(a.codes[-30:], a.scales[-30:], 256), w, dtype=torch.bfloat16)
+    assert out.numel() > 2 ** 31 and torch.equal(out[-30:], tail)
+    side = P.mx4_gemm(a, P.Mx4(w.codes[-30:], w.scales[-30:], 256), dtype=torch.bfloat16)
+    assert torch.equal(out[:, -30:], side)

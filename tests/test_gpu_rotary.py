@@ -245,3 +245,12 @@ def test_a_layers_projections_together(P):
     a, w = P.mx4_dequantize(qz).double(), P.mx4_dequantize(wo).double()
     want = a @ w.t() + stream.double()
     assert ((out.double() - want).abs() <= product_bound(a, w, want, stream.double().abs(), H * dh)).all()
+
+
+def test_more_than_2_to_the_31_elements(P):
+    import torch
+    x = torch.zeros(70000, 40, 1024, device="cuda", dtype=torch.bfloat16)
+    x[-2:] = torch.randn(2, 40, 1024, device="cuda")
+    pos, table = torch.arange(70000, device="cuda"), P.rotary_table(1024)
+    got = P.rotary(x, pos, table)
+    assert x.numel() > 2 ** 31 and torch.equal(got[-2:], P.rotary(x[-2:], pos[-2:], table)) and not got[:-2].any()
