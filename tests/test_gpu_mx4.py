@@ -351,6 +351,20 @@ def test_streams_and_replayed_graphs(P):
             assert torch.equal(out, want), turn
 
 
+def test_copies_have_memory_of_their_own(P):
+    import copy
+    import pickle
+    import torch
+    x, y = torch.randn(5, 300, device="cuda"), torch.randn(7, 300, device="cuda")
+    q, w = P.mx4_quantize(x), P.mx4_quantize(y)
+    want = P.mx4_gemm(q, w)
+    copies = [copy.deepcopy(q), pickle.loads(pickle.dumps(q))]
+    P.mx4_quantize(torch.zeros_like(x), out=q)
+    assert not P.mx4_gemm(q, w).any()
+    for c in copies:
+        assert torch.equal(P.mx4_gemm(c, w), want) and c.codes.data_ptr() != q.codes.data_ptr()
+
+
 def test_two_streams_at_once(P):
     """Calls that overlap share nothing: fifty rounds on two streams without waiting, every result that of a call alone."""
     import torch
