@@ -449,7 +449,8 @@ int pahq_quantize_rows_noalloc(void* hip_stream, const float* x, int32_t rows, i
  * recorded into a HIP graph, and any number of calls may be in flight, on one stream or several, as long as one does not
  * write what another uses.  The device that owns the pointers and the stream must be the current one.  Arguments the host
  * can see are checked before anything is enqueued: PAHQ_EINVAL (null or misaligned pointer, size or stride out of range, a
- * result that shares memory with an operand unless said otherwise), PAHQ_ETOOBIG (more than a launch counts).  A size
+ * result that shares memory with an operand unless said otherwise; other columns of the same rows are no shared memory where
+ * the strides are equal), PAHQ_ETOOBIG (more than a launch counts).  A size
  * of zero rows (columns, tokens, heads) does nothing and looks at no pointer.  Strides (ld) count elements; tensors need the
  * alignment of their element only. */
 enum { PAHQ_F32 = 0, PAHQ_BF16 = 1, PAHQ_F16 = 2 };
@@ -463,7 +464,7 @@ enum { PAHQ_F32 = 0, PAHQ_BF16 = 1, PAHQ_F16 = 2 };
  * byte 127):
  *     codes   [rows][K / 2] bytes, element 2 i of a row in the low half of byte i; 16-byte aligned
  *     scales  [rows][K / 32] bytes; 8-byte aligned
- * pahq_mx4_bytes gives the sizes of the two.
+ * The product reads the padding.  pahq_mx4_bytes gives the sizes of the two; a call takes up to 2^27 - 8 groups of 256 elements.
  * pahq_mx4_quantize: by = PAHQ_MX4_BY_ROWS: x [rows][cols], row stride ld >= cols.  PAHQ_MX4_BY_COLUMNS: x [cols][rows], row
  * stride ld >= rows, so that the blocks run down the columns of x: a weight master [k][n] becomes the [n][k] the product takes.
  * pahq_mx4_dequantize: the values; exact in PAHQ_F32 and PAHQ_BF16, rounded once in PAHQ_F16.
@@ -491,7 +492,7 @@ int pahq_mx4_gemm(void* hip_stream, const uint8_t* a_codes, const uint8_t* a_sca
  * Arithmetic in fp32, one rounding to the type.
  * table: device uint64 [rot_dim / 2], from pahq_rotary_table, which fills HOST memory: f_i / (2 pi) modulo 1 in units of
  * 2^-64, so the angle of a far position is as good as that of a near one.  rot_dim even, 2 .. PAHQ_ROTARY_MAX_DIM;
- * d_head up to PAHQ_ROTARY_MAX_HEAD, heads up to 65535.
+ * d_head up to PAHQ_ROTARY_MAX_HEAD, heads up to 65535, tokens up to PAHQ_ROTARY_MAX_TOKENS.
  *     PAHQ_ROTARY_PLAIN   f_i = theta^(-2 i / rot_dim)
  *     PAHQ_ROTARY_LINEAR  f_i / factor: positions squeezed into the trained range
  *     PAHQ_ROTARY_BASE    theta * factor^(rot_dim / (rot_dim - 2)) in place of theta: the slowest pair is stretched by factor,
@@ -502,7 +503,7 @@ int pahq_mx4_gemm(void* hip_stream, const uint8_t* a_codes, const uint8_t* a_sca
  * factor >= 1; arguments a form does not use are ignored. */
 enum { PAHQ_ROTARY_HALF = 0, PAHQ_ROTARY_INTERLEAVED = 1 };
 enum { PAHQ_ROTARY_PLAIN = 0, PAHQ_ROTARY_LINEAR = 1, PAHQ_ROTARY_BASE = 2, PAHQ_ROTARY_BANDS = 3 };
-enum { PAHQ_ROTARY_MAX_DIM = 1024, PAHQ_ROTARY_MAX_HEAD = 4096 };
+enum { PAHQ_ROTARY_MAX_DIM = 1024, PAHQ_ROTARY_MAX_HEAD = 4096, PAHQ_ROTARY_MAX_TOKENS = (1 << 24) - 1 };
 int pahq_rotary_table(int32_t rot_dim, double theta, int32_t scaling, double factor, double original, double turns_lo,
                       double turns_hi, uint64_t* table);
 int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32_t tokens, int32_t heads, int32_t d_head, int64_t x_token,

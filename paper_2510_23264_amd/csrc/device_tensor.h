@@ -18,6 +18,15 @@ inline bool overlap(const void* p, size_t pn, const void* q, size_t qn) {
   return a < b + qn && b < a + pn;
 }
 
+// Two matrices of rows of pn and qn bytes whose rows lie `stride` bytes apart in both (0: not the same), as columns of one: no row
+// of one touches a row of the other.
+inline bool side_by_side(const void* p, size_t pn, const void* q, size_t qn, size_t stride) {
+  if (stride == 0) return false;
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  const size_t d = b >= a ? (b - a) % stride : (stride - (a - b) % stride) % stride;      // where q's row starts in p's row
+  return d >= pn && d + qn <= stride;
+}
+
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(bf16_t x) { return (float)x; }
 __device__ __forceinline__ float as_float(f16_t x) { return (float)x; }

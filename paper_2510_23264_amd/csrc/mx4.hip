@@ -498,6 +498,7 @@ int launch_tile(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8
   typedef Mx4Tile<AF, WF, WM, WN, KW> C;
   const int mt = (m + C::BM - 1) / C::BM, nt = (n + C::BN - 1) / C::BN;
   const int tiles = (mt * nt + 7) / 8 * 8;
+  if (KW > 1 && tiles >= 1ll << 24) return PAHQ_ETOOBIG;       // fewer than 2^32 threads; the estimate takes larger tiles long before
   const void* fn = (const void*)mx4_gemm_tile_k<T, AF, WF, WM, WN, KW>;
   // more LDS than a launch gets by default: an attribute of the kernel on one device, set once for each
   static std::atomic<bool> set[64];
@@ -531,8 +532,8 @@ int gemm_as(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8_t* 
 // rows of codes are 16-byte loads, rows of scales 8-byte ones
 bool held_aligned(const void* codes, const void* scales) { return ((uintptr_t)codes & 15) == 0 && ((uintptr_t)scales & 7) == 0; }
 size_t code_bytes(long long rows, long long cols) { return (size_t)(rows * ((cols + 255) / 256) * 128); }
-// most groups of 256 elements of one matrix: workgroups are counted in 32 bits (5e11 elements do not fit the card)
-bool too_big(long long rows, long long cols) { return rows * ((cols + 255) / 256) >= (1ll << 31); }
+// Most groups of 256 elements of one matrix: a launch has fewer than 2^32 threads, of them 32 for a group.
+bool too_big(long long rows, long long cols) { return rows * ((cols + 255) / 256) > (1ll << 27) - 8; }
 }  // namespace
 
 }  // namespace pahq
@@ -589,14 +590,16 @@ extern "C" int pahq_mx4_gemm(void* hip_stream, const uint8_t* a_codes, const uin
   if (!a_codes || !a_scales || !w_codes || !w_scales || !out || ld_out < n || (residual && ld_residual < n)) return PAHQ_EINVAL;
   if (!held_aligned(a_codes, a_scales) || !held_aligned(w_codes, w_scales)) return PAHQ_EINVAL;
   if ((uintptr_t)out % eb || (uintptr_t)residual % eb || (uintptr_t)bias % 4) return PAHQ_EINVAL;
-  // a tile's rows are addressed by 32 bits, tiles counted by 31
+  // a tile's rows are addressed by 32 bits, tiles counted by 31; 512 threads take 16 columns of few rows
   if (k > PAHQ_MX4_MAX_K || too_big(m, k) || too_big(n, k) || ((m + 31ll) / 32) * ((n + 31ll) / 32) >= (1ll << 31) - 8) return PAHQ_ETOOBIG;
   const size_t ob = (size_t)(((m - 1ll) * ld_out + n) * eb), ab = code_bytes(m, k), wb = code_bytes(n, k);
   if (overlap(out, ob, a_codes, ab) || overlap(out, ob, a_scales, ab / 16) || overlap(out, ob, w_codes, wb) || overlap(out, ob, w_scales, wb / 16) ||
       (bias && overlap(out, ob, bias, (size_t)n * 4)))
     return PAHQ_EINVAL;
   // the residual may be the result's own rows: every element is read by the thread that writes it
-  if (residual && !(residual == out && ld_residual == ld_out) && overlap(out, ob, residual, (size_t)(((m - 1ll) * ld_residual + n) * eb))) return PAHQ_EINVAL;
+  if (residual && !(residual == out && ld_residual == ld_out) && overlap(out, ob, residual, (size_t)(((m - 1ll) * ld_residual + n) * eb)) &&
+      !side_by_side(out, (size_t)n * eb, residual, (size_t)n * eb, ld_out == ld_residual ? (size_t)ld_out * eb : 0))
+    return PAHQ_EINVAL;
   hipStream_t st = (hipStream_t)hip_stream;
   const int slabs = (k + 255) / 256;
   switch (dtype) {

@@ -153,13 +153,15 @@ extern "C" int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32
   if ((layout != PAHQ_ROTARY_HALF && layout != PAHQ_ROTARY_INTERLEAVED) || (inverse != 0 && inverse != 1)) return PAHQ_EINVAL;
   if (tokens == 0 || heads == 0) return PAHQ_OK;
   if (!x || !out || !positions || !table || (uintptr_t)x % eb || (uintptr_t)out % eb || (uintptr_t)positions % 8 || (uintptr_t)table % 8) return PAHQ_EINVAL;
-  // workgroups are counted in 16 bits along the heads
-  if (heads > 65535 || d_head > PAHQ_ROTARY_MAX_HEAD) return PAHQ_ETOOBIG;
+  // workgroups are counted in 16 bits along the heads, threads in 32 along the tokens
+  if (heads > 65535 || d_head > PAHQ_ROTARY_MAX_HEAD || tokens > PAHQ_ROTARY_MAX_TOKENS) return PAHQ_ETOOBIG;
   long long xn, on;
   if (x_token < 0 || x_head < 0 || !strides_ok(tokens, heads, d_head, out_token, out_head, &on)) return PAHQ_EINVAL;
   xn = (tokens - 1ll) * x_token + (heads - 1ll) * x_head + d_head;      // only read: rows may share memory
   const bool in_place = x == out && x_token == out_token && x_head == out_head;
-  if (!in_place && overlap(x, (size_t)xn * eb, out, (size_t)on * eb)) return PAHQ_EINVAL;
+  const size_t xw = (size_t)((heads - 1ll) * x_head + d_head) * eb, ow = (size_t)((heads - 1ll) * out_head + d_head) * eb;      // of a token
+  if (!in_place && overlap(x, (size_t)xn * eb, out, (size_t)on * eb) && !side_by_side(x, xw, out, ow, x_token == out_token ? (size_t)x_token * eb : 0))
+    return PAHQ_EINVAL;
   if (overlap(out, (size_t)on * eb, positions, (size_t)tokens * 8) || overlap(out, (size_t)on * eb, table, (size_t)rot_dim * 4)) return PAHQ_EINVAL;
   hipStream_t st = (hipStream_t)hip_stream;
   const RotaryArgs q = {x_token, x_head, out_token, out_head, (const long long*)positions, (const unsigned long long*)table, tokens, heads, d_head, rot_dim,

@@ -288,6 +288,10 @@ def test_results_in_strided_memory_and_in_place(P, m, n, k):
             out.copy_(res)
             P.mx4_gemm(qa, qw, residual=out, out=out)
             assert torch.equal(out, want)
+        both = torch.empty((m, 2 * n + 1), dtype=t, device="cuda")         # result and residual as columns of the same rows
+        both[:, n + 1:] = res
+        P.mx4_gemm(qa, qw, residual=both[:, n + 1:], out=both[:, :n])
+        assert torch.equal(both[:, :n], want) and torch.equal(both[:, n + 1:], res)
 
 
 def test_wrapper_refuses(P):

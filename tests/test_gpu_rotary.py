@@ -118,6 +118,10 @@ def test_strides_views_and_shared_rows(P):
             assert torch.equal(P.rotary(planes.copy_(x), pos, table, layout=layout, out=planes), want)
             shared = torch.randn(9, 1, 48, device="cuda").to(dtype).expand(9, 5, 48)
             assert torch.equal(P.rotary(shared, pos, table, layout=layout), P.rotary(shared.contiguous(), pos, table, layout=layout))
+            both = torch.randn(9, 11, 48, device="cuda").to(dtype)       # heads of the same rows, some read and others written
+            beside = P.rotary(both[:, :5].contiguous(), pos, table, layout=layout)
+            P.rotary(both[:, :5], pos, table, layout=layout, out=both[:, 6:])
+            assert torch.equal(both[:, 6:], beside)
             keep = rows.clone()
             P.rotary(x, pos, table, layout=layout, out=x)
             assert torch.equal(x, want)

@@ -38,7 +38,7 @@ ROTARY = dict(stream=None, x=A, dtype=0, tokens=4, heads=3, d=64, x_token=192, x
     (dict(rows=-1), EINVAL), (dict(cols=0), EINVAL), (dict(dtype=3), EINVAL), (dict(dtype=-1), EINVAL), (dict(by=2), EINVAL), (dict(ld=299), EINVAL),
     (dict(by=1, ld=3), EINVAL), (dict(x=None), EINVAL), (dict(codes=None), EINVAL), (dict(scales=None), EINVAL), (dict(codes=2 * A + 8), EINVAL),
     (dict(scales=3 * A + 4), EINVAL), (dict(x=A + 2), EINVAL), (dict(x=A + 1, dtype=1), EINVAL), (dict(codes=A + 16), EINVAL), (dict(scales=A + 16), EINVAL),
-    (dict(scales=2 * A + 16), EINVAL), (dict(rows=HUGE, cols=513, ld=513), ETOOBIG), (dict(by=1, cols=65535 * 256 + 1), ETOOBIG),
+    (dict(scales=2 * A + 16), EINVAL), (dict(rows=HUGE, cols=513, ld=513), ETOOBIG), (dict(rows=1 << 27), ETOOBIG), (dict(by=1, cols=65535 * 256 + 1), ETOOBIG),
     (dict(rows=0, x=None), 0)])
 def test_quantize_refuses(P, change, code):
     assert P.lib().pahq_mx4_quantize(*dict(QUANTIZE, **change).values()) == code
@@ -57,7 +57,8 @@ def test_dequantize_refuses(P, change, code):
     (dict(a=None), EINVAL), (dict(a_scales=None), EINVAL), (dict(w=None), EINVAL), (dict(w_scales=None), EINVAL), (dict(out=None), EINVAL),
     (dict(a=A + 4), EINVAL), (dict(w_scales=4 * A + 2), EINVAL), (dict(out=7 * A + 2), EINVAL), (dict(residual=6 * A + 1), EINVAL), (dict(bias=5 * A + 2), EINVAL),
     (dict(out=A), EINVAL), (dict(out=2 * A), EINVAL), (dict(out=3 * A), EINVAL), (dict(out=4 * A), EINVAL), (dict(out=5 * A), EINVAL),
-    (dict(residual=7 * A + 4), EINVAL), (dict(residual=7 * A, ld_res=9), EINVAL), (dict(n=HUGE, k=513, ld=HUGE, ld_res=HUGE), ETOOBIG),
+    (dict(residual=7 * A + 4), EINVAL), (dict(residual=7 * A, ld_res=9), EINVAL), (dict(n=HUGE, k=513, ld=HUGE, ld_res=HUGE), ETOOBIG), (dict(k=(1 << 24) + 1), ETOOBIG),
+    (dict(n=1 << 27, k=64, ld=1 << 27, ld_res=1 << 27), ETOOBIG), (dict(residual=7 * A + 16, ld=14, ld_res=14), EINVAL), (dict(residual=7 * A + 64, ld=16, ld_res=17), EINVAL),
     (dict(m=0, a=None, out=None), 0), (dict(n=0, w=None, ld=0), 0)])
 def test_gemm_refuses(P, change, code):
     assert P.lib().pahq_mx4_gemm(*dict(GEMM, **change).values()) == code
@@ -70,7 +71,7 @@ def test_gemm_refuses(P, change, code):
     (dict(x=A + 2), EINVAL), (dict(out=2 * A + 1), EINVAL), (dict(positions=4 * A + 4), EINVAL), (dict(table=5 * A + 4), EINVAL), (dict(x_token=-1), EINVAL),
     (dict(out_head=63), EINVAL), (dict(out_token=191), EINVAL), (dict(out_token=0), EINVAL), (dict(out_token=64, out_head=255), EINVAL),
     (dict(out=A + 4), EINVAL), (dict(out=A, out_token=256), EINVAL), (dict(out=4 * A), EINVAL), (dict(out=5 * A), EINVAL),
-    (dict(heads=65536, out_token=1 << 28), ETOOBIG), (dict(d=4097, out_head=4097, out_token=3 * 4097), ETOOBIG), (dict(tokens=0, x=None), 0), (dict(heads=0, out=None), 0)])
+    (dict(heads=65536, out_token=1 << 28), ETOOBIG), (dict(tokens=1 << 24), ETOOBIG), (dict(d=4097, out_head=4097, out_token=3 * 4097), ETOOBIG), (dict(tokens=0, x=None), 0), (dict(heads=0, out=None), 0)])
 def test_rotary_refuses(P, change, code):
     assert P.lib().pahq_rotary(*dict(ROTARY, **change).values()) == code
 
