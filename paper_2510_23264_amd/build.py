@@ -1,11 +1,14 @@
-"""Builds libpahq.so (HIP, gfx950 only) in-tree with hipcc."""
+"""Builds libpahq.so (HIP, gfx950 only) in-tree with hipcc, and _tensors.so, the torch side of its operators on device tensors."""
+import importlib.util
 import os
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpahq.so")
+EXTENSION = os.path.join(HERE, "_tensors.so")
 SOURCES = ["rows.hip", "gemm.hip", "oproj.hip", "attn_kl.hip", "engine.hip", "api.hip", "ceilings.hip", "noalloc.hip", "mx4.hip",
            "rotary.hip"]
 # -ffp-contract=off: a product and a sum are rounded separately unless the source says fmaf.  The same
@@ -23,12 +26,23 @@ def _compile(src):
     return obj
 
 
+def _extension():
+    """csrc/tensors_ext.cpp against torch's and Python's headers; torch's libraries are there when tensors.py loads it."""
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I" + os.path.join(torch, "include"),
+                    "-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include"), "-I/opt/rocm/include", "-I" + sysconfig.get_paths()["include"],
+                    os.path.join(CSRC, "tensors_ext.cpp"), "-o", EXTENSION, "-L" + HERE, "-l:libpahq.so", "-L" + os.path.join(torch, "lib"),
+                    "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-L/opt/rocm/lib", "-lamdhip64", "-Wl,-rpath,$ORIGIN"],
+                   check=True, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+
+
 def build(verbose=False):
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
     with ThreadPoolExecutor(max_workers=6) as ex:
         objs = list(ex.map(_compile, SOURCES))
     subprocess.run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs], check=True,
                    stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    _extension()
     if verbose:
         print("built", LIB)
     return LIB
