@@ -32,7 +32,9 @@ struct PythonError {};           // an exception is set already
 
 const Tensor& tensor(PyObject* o, const char* text) {
   need(THPVariable_Check(o), text);
-  return THPVariable_Unpack(o);
+  const Tensor& t = THPVariable_Unpack(o);
+  need(t.layout() == at::kStrided && !t.is_neg(), "tensors: strided, their values as they lie in memory");
+  return t;
 }
 long long number(PyObject* o) {
   const long long v = PyLong_AsLongLong(o);
