@@ -4,9 +4,11 @@
 
 namespace pahq {
 
-// Up to 16 rows whose sums are short or whose results are few: one 16 x 16 product a wave from global memory is done before a
-// tile's first stage is there (4096 x 4096 4.4 us, in tiles 4.9; 3 x 14720 x 2959 8.1, in tiles 5.5).
-inline bool mx4_few(long long m, long long n, int slabs) { return m <= 16 && (slabs < 6 || n * slabs < 80000); }
+// Up to 16 rows: one 16 x 16 product a wave from global memory, except for 5 rows and more whose results and sums are both long.
+// Chosen with the weights in HBM, as a program of many layers finds them: 1 x 4096 x 4096 4.3 us (in tiles 6.2), 1 x 1024 x 16000
+// 7.8 (14.7), 1 x 11008 x 4096 8.3 (8.7), but 16 x 11008 x 4096 10.9 (8.9) and 11 x 31513 x 9086 47 (34).  Over 70 sizes
+// 1.002 of the better one's time in the mean and 1.11 at most; where the last call left the weights in the caches, 1.015 and 1.49.
+inline bool mx4_few(long long m, long long n, int slabs) { return m <= 16 && (m <= 4 || n < 4000 || slabs < 10); }
 
 // Otherwise tiles of `tile` x `tile`, the sum over k shared by `groups` groups of waves.  The times in microseconds are fitted to
 // 400 random sizes from 17 x 16 x 32 to 8192 x 50000 x 12000 (bfloat16 results): one workgroup alone takes

@@ -17,6 +17,6 @@ def estimate(form, m, n, slabs):
 
 def form(m, n, k):
     slabs = -(-k // 256)
-    if m <= 16 and (slabs < 6 or n * slabs < 80000):
+    if m <= 16 and (m <= 4 or n < 4000 or slabs < 10):
         return FEW
     return min(range(5), key=lambda i: estimate(FORMS[i], m, n, slabs))

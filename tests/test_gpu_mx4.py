@@ -189,7 +189,7 @@ def test_products_whose_sums_are_exact(P, m, n, k):
 # the smallest sizes found for every form of the product (tests/mx4_rules.py) with 1 to 9 slabs of 256 elements of k, one tile a
 # workgroup and several; none a multiple of a tile
 FORM_SIZES = [
-    (0, 17, 17, 56), (0, 18, 19, 568), (0, 18, 17, 824), (0, 17, 18, 1080), (0, 17, 17, 2304), (0, 12, 12001, 2104),
+    (0, 17, 17, 56), (0, 18, 19, 568), (0, 18, 17, 824), (0, 17, 18, 1080), (0, 17, 17, 2304), (0, 12, 12001, 2360), (-1, 12, 12001, 2104), (-1, 4, 12001, 2360), (-1, 16, 3999, 2360),
     (1, 67, 6510, 568), (1, 65, 6589, 824), (1, 33, 8993, 1080), (1, 33, 8119, 2104),
     (2, 70, 6497, 56), (2, 67, 6934, 312), (2, 65, 8205, 568), (2, 68, 8278, 824), (2, 65, 8703, 2104),
     (3, 132, 8555, 56), (3, 899, 8233, 56), (3, 195, 8526, 312), (3, 1547, 5068, 312), (3, 199, 8402, 568), (3, 903, 8637, 824), (3, 1158, 6608, 1080),

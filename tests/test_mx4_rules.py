@@ -43,5 +43,6 @@ def test_the_copy_agrees(pick):
 
 
 def test_the_sizes_its_comments_name(pick):
-    assert pick([(1, 4096, 4096), (3, 14720, 2959), (100, 2304, 768), (256, 4096, 4096), (800, 2304, 768), (2048, 4096, 4096), (8192, 4096, 11008)]) == \
-        [R.FEW, R.T32, R.T32, R.T64_FOUR, R.T64_TWO, R.T128, R.T256]
+    assert pick([(1, 4096, 4096), (1, 1024, 16000), (1, 11008, 4096), (16, 11008, 4096), (11, 31513, 9086), (100, 2304, 768), (256, 4096, 4096), (800, 2304, 768),
+                 (2048, 4096, 4096), (8192, 4096, 11008)]) == \
+        [R.FEW, R.FEW, R.FEW, R.T32, R.T32, R.T32, R.T64_FOUR, R.T64_TWO, R.T128, R.T256]
