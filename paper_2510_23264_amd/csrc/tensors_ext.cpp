@@ -1,7 +1,8 @@
 // The torch side of the operators on device tensors: what a call has to check, allocate and look up before it enters the C ABI,
-// in C++ because small calls are all host time (turning four tokens took the host
-// 8.3 us through ctypes and torch's Python calls and takes it 4.2 here, of which the launch is 2; a product 6.6 and 4.4).  Python functions in the module `_tensors`; tensors.py documents and wraps them.  A function returns its
-// result, or the library's code as an int where that is not 0, and raises ValueError for arguments that do not fit.
+// in C++ because small calls are all host time (turning four tokens took the host 8.3 us through ctypes and torch's Python calls and
+// takes it 4.2 here, of which the launch is 2; a product 6.6 and 4.4).  Python functions in the module `_tensors`; tensors.py
+// documents and wraps them.  A function returns its result, or the library's code as an int where that is not 0, and raises
+// ValueError for arguments that do not fit.
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
@@ -91,6 +92,10 @@ struct Held {
     device = (at::DeviceIndex)number(PyTuple_GET_ITEM(o, 4));
   }
 };
+// `t` was written: a backward pass that kept its former values has to notice
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 bool on(const Tensor& t, at::DeviceIndex device) { return t.is_cuda() && t.get_device() == device; }
 
 // `o` checked as the result [rows][cols], or a new tensor of TYPES[dtype] where it is None
@@ -159,6 +164,7 @@ PyObject* mx4_dequantize(PyObject* const* a) {
     const On current(q.device);
     const int rc = pahq_mx4_dequantize(current.stream, q.codes, q.scales, size32(q.rows), size32(q.cols), out.data_ptr(), dtype_of(out.scalar_type()), ld);
     if (rc) return PyLong_FromLong(rc);
+    written(out);
   }
   return THPVariable_Wrap(out);
 }
@@ -189,6 +195,7 @@ PyObject* mx4_gemm(PyObject* const* a) {
     const int rc = pahq_mx4_gemm(current.stream, x.codes, x.scales, w.codes, w.scales, size32(x.rows), size32(w.rows), size32(x.cols), bias, residual, ld_res,
                                  out.data_ptr(), dtype_of(out.scalar_type()), ld);
     if (rc) return PyLong_FromLong(rc);
+    written(out);
   }
   return THPVariable_Wrap(out);
 }
@@ -230,6 +237,7 @@ PyObject* rotary(PyObject* const* a) {
                                (const int64_t*)positions.data_ptr(), (const uint64_t*)table.data_ptr(), (int32_t)(2 * table.numel()), (int32_t)number(a[3]),
                                (float)magnitude, a[5] == Py_True, out.data_ptr(), ot, oh);
     if (rc) return PyLong_FromLong(rc);
+    written(out);
   }
   return THPVariable_Wrap(out);
 }

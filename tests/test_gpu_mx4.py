@@ -407,3 +407,17 @@ def test_more_than_2_to_the_31_elements(P):
     assert out.numel() > 2 ** 31 and torch.equal(out[-30:], tail)
     side = P.mx4_gemm(a, P.Mx4(w.codes[-30:], w.scales[-30:], 256), dtype=torch.bfloat16)
     assert torch.equal(out[:, -30:], side)
+
+
+def test_few_rows_of_weights_behind_the_32nd_bit(P):
+    """Codes of 4.6 GB: the last weights against a call on them alone, which adds in the same order."""
+    import torch
+    torch.manual_seed(6)
+    m, n, k = 3, 40003, 900 * 256
+    a = P.Mx4(torch.randint(0, 256, (m, k // 2), device="cuda", dtype=torch.uint8), torch.randint(120, 130, (m, k // 32), device="cuda", dtype=torch.uint8), k)
+    w = P.Mx4(torch.randint(0, 256, (n, k // 2), device="cuda", dtype=torch.uint8), torch.randint(120, 130, (n, k // 32), device="cuda", dtype=torch.uint8), k)
+    assert w.codes.numel() > 2 ** 32
+    out = P.mx4_gemm(a, w)
+    for lo in (0, 37282, 39970):                     # the first rows, those around byte 2^32 (row 37282), the last
+        part = P.Mx4(w.codes[lo:lo + 33], w.scales[lo:lo + 33], k)
+        assert torch.equal(out[:, lo:lo + 33], P.mx4_gemm(a, part))

@@ -162,6 +162,28 @@ def test_gradient_against_the_formula_and_differences(P):
         assert g1.requires_grad
 
 
+def test_a_backward_pass_notices_what_a_call_wrote(P):
+    """Values that autograd kept are gone once a call has written to their memory: the backward pass refuses, as behind torch's own
+    operations in place, and is right where nothing was written."""
+    import torch
+    x, pos, table = torch.randn(4, 3, 64, device="cuda"), torch.arange(4, device="cuda"), P.rotary_table(64)
+    q, res = P.mx4_quantize(torch.randn(4, 64, device="cuda")), torch.randn(4, 4, device="cuda")
+    values = torch.randn(4, 64, device="cuda")
+    for kept, call in ((x, lambda: P.rotary(x, pos, table, out=x)), (res, lambda: P.mx4_gemm(q, q, residual=res, out=res)),
+                       (values, lambda: P.mx4_dequantize(q, out=values))):
+        w = torch.randn_like(kept).requires_grad_()
+        (w * kept).sum().backward()
+        assert torch.equal(w.grad, kept)
+        y = (w * kept).sum()
+        call()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    with torch.inference_mode():
+        z = torch.randn(4, 3, 64, device="cuda")
+        want = P.rotary(z, pos, table)
+        assert torch.equal(P.rotary(z, pos, table, out=z), want)
+
+
 def test_refusals_and_nothing_to_do(P):
     import torch
     table = P.rotary_table(32)
