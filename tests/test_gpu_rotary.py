@@ -226,6 +226,34 @@ def test_streams_and_replayed_graphs(P):
         assert torch.equal(out, want)
 
 
+def test_a_captured_forward_and_backward(P):
+    """A step with its gradient in one graph, replayed with new values between eager steps."""
+    import torch
+    table, pos = P.rotary_table(32, 500.0), torch.arange(20, device="cuda")
+    x, g = torch.randn(20, 4, 48, device="cuda", requires_grad=True), torch.randn(20, 4, 48, device="cuda")
+
+    def step():
+        y = P.rotary(x * 2.0, pos, table, layout="interleaved", magnitude=1.25)
+        return y.detach(), torch.autograd.grad(y, x, g)[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for _ in range(4):
+        with torch.no_grad():
+            x.normal_()
+            g.normal_()
+            pos += 77777
+        want = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held[0], want[0]) and torch.equal(held[1], want[1])
+
+
 def test_a_layers_projections_together(P):
     """One attention layer's way as a program runs it: rows to 4 bits, queries, keys and values in one product, rotation in
     place of the queries and keys between the values, attention, rows to 4 bits again, output product on the residual.
