@@ -399,7 +399,7 @@ __global__ __launch_bounds__(KW * WM * WN * 64, (Mx4Tile<AF, WF, WM, WN, KW>::PE
       if (res && left >= V) {
 #pragma unroll
         for (int r = 0; r < R; r++)
-          if (m0 + rl + r * DOWN < m) u[r] = load16(p + (long long)(r * DOWN) * ld_res);
+          if (mx4_in_tile(rl + r * DOWN, H, m - m0)) u[r] = load16(p + (long long)(r * DOWN) * ld_res);
       }
       float* const put = (float*)lds + group * (H * C::STRIDE) + 4 * g * C::STRIDE + j;
 #pragma unroll
@@ -411,8 +411,7 @@ __global__ __launch_bounds__(KW * WM * WN * 64, (Mx4Tile<AF, WF, WM, WN, KW>::PE
       __syncthreads();
 #pragma unroll
       for (int r = 0; r < R; r++) {
-        const int row = m0 + rl + r * DOWN;
-        if (row >= m || (H % DOWN && rl + r * DOWN >= H) || left <= 0) continue;
+        if (!mx4_in_tile(rl + r * DOWN, H, m - m0) || left <= 0) continue;
         float f[V];
 #pragma unroll
         for (int v = 0; v < V; v++) f[v] = sums[r * DOWN * C::STRIDE + v];

@@ -30,6 +30,9 @@ inline float mx4_estimate(const Mx4Form& f, long long m, long long n, int slabs)
   const float further = r <= 1 ? 0 : f.whole ? 0.5f * (ceilf(r) + r) - 1 : r - 1;
   return f.launch + (f.start + f.slab * ((slabs + f.groups - 1) / f.groups)) * (1 + f.round * further);
 }
+// Whether a workgroup that joins partial sums has row `at` of its tile of `high` rows, `left` of them in the matrix: its threads may
+// reach past the tile, into rows of another workgroup's.
+constexpr bool mx4_in_tile(int at, int high, int left) { return at < high && at < left; }
 inline int mx4_form(long long m, long long n, int slabs) {
   int best = 0;
   float least = 0;
