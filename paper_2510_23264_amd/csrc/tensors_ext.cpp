@@ -10,6 +10,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <ATen/ops/empty_strided.h>
+#include <c10/core/AutogradState.h>
 #include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <exception>
@@ -31,10 +32,15 @@ inline void need(bool ok, const char* text) {
 }
 struct PythonError {};           // an exception is set already
 
+// `t` has a forward-mode derivative that its next operation is expected to carry on
+bool has_tangent(const Tensor& t) { return t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode(); }
+
 const Tensor& tensor(PyObject* o, const char* text) {
   need(THPVariable_Check(o), text);
   const Tensor& t = THPVariable_Unpack(o);
   need(t.layout() == at::kStrided && !t.is_neg(), "tensors: strided, their values as they lie in memory");
+  // read or written as plain memory it would lose the tangent, or keep one that is no longer its own
+  need(!has_tangent(t), "a tangent (forward-mode derivative): not carried here");
   return t;
 }
 long long number(PyObject* o) {

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from .binding import lib, _chk, rotary_entries
 
@@ -132,6 +133,11 @@ def rotary_table(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=0.
     return torch.from_numpy(rotary_entries(rot_dim, theta, scaling, factor, original, turns).view(np.int64)).to(device)
 
 
+def _tangent(x):
+    """Whether x has a forward-mode derivative to carry on (outside of forward_ad.dual_level nothing has)."""
+    return forward_ad._current_level >= 0 and torch._C._is_fwd_grad_enabled() and forward_ad.unpack_dual(x).tangent is not None
+
+
 def _rotary(x, positions, table, layout, magnitude, inverse, out):
     got = _ext.rotary(x, positions, table, layout, magnitude, inverse, out)
     if type(got) is int:
@@ -143,6 +149,7 @@ class _Rotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, positions, table, layout, magnitude, inverse):
         ctx.save_for_backward(positions, table)
+        ctx.save_for_forward(positions, table)
         ctx.how = layout, magnitude, not inverse
         return _rotary(x, positions, table, layout, magnitude, inverse, None)
 
@@ -153,14 +160,23 @@ class _Rotary(torch.autograd.Function):
             grad = grad.contiguous()
         return _Rotary.apply(grad, positions, table, *ctx.how), None, None, None, None, None
 
+    @staticmethod
+    def jvp(ctx, tangent, *_):                              # linear in x
+        positions, table = ctx.saved_tensors
+        layout, magnitude, back = ctx.how
+        if tangent.shape[2] > 1 and tangent.stride(2) != 1:
+            tangent = tangent.contiguous()
+        return _Rotary.apply(tangent, positions, table, layout, magnitude, not back)
+
 
 def rotary(x, positions, table, layout="half", magnitude=1.0, inverse=False, out=None):
     """Turns the first 2 * len(table) elements of every head of x [tokens][heads][d_head] by their tokens' positions (int64
     [tokens]); the rest of the head is copied.  layout: "half" (pairs i, i + rot / 2) or "interleaved" (pairs 2 i, 2 i + 1).
-    inverse turns back (the gradient; x gets it by itself where autograd asks).  out may be x."""
+    inverse turns back (the gradient; x gets it by itself where autograd asks, and a tangent of x in forward mode is carried).  out
+    may be x, except where a derivative is recorded."""
     if layout not in _LAYOUTS:
         raise ValueError("layout: 'half' or 'interleaved'")
-    if torch.is_grad_enabled() and (x.requires_grad or out is not None and out.requires_grad):
+    if torch.is_grad_enabled() and (x.requires_grad or out is not None and out.requires_grad) or _tangent(x):
         _need(out is None, "out: not where a gradient is recorded")
         return _Rotary.apply(x, positions, table, _LAYOUTS[layout], float(magnitude), bool(inverse))
     return _rotary(x, positions, table, _LAYOUTS[layout], magnitude, bool(inverse), out)
