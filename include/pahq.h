@@ -464,7 +464,8 @@ enum { PAHQ_F32 = 0, PAHQ_BF16 = 1, PAHQ_F16 = 2 };
  * byte 127):
  *     codes   [rows][K / 2] bytes, element 2 i of a row in the low half of byte i; 16-byte aligned
  *     scales  [rows][K / 32] bytes; 8-byte aligned
- * The product reads the padding.  pahq_mx4_bytes gives the sizes of the two; a call takes up to 2^27 - 8 groups of 256 elements.
+ * The product reads the padding.  pahq_mx4_bytes gives the sizes of the two; a call takes up to 2^27 - 8 groups of 256 elements
+ * a matrix (PAHQ_MX4_BY_COLUMNS: of them up to 65535 a row).
  * pahq_mx4_quantize: by = PAHQ_MX4_BY_ROWS: x [rows][cols], row stride ld >= cols.  PAHQ_MX4_BY_COLUMNS: x [cols][rows], row
  * stride ld >= rows, so that the blocks run down the columns of x: a weight master [k][n] becomes the [n][k] the product takes.
  * pahq_mx4_dequantize: the values; exact in PAHQ_F32 and PAHQ_BF16, rounded once in PAHQ_F16.

@@ -515,7 +515,7 @@ int launch_tile(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8
 template <typename T>
 int gemm_as(hipStream_t st, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs, const float* bias,
             const T* res, long long ld_res, T* out, long long ld) {
-  if (mx4_few(m, n, slabs)) {
+  if (mx4_few(m, n, slabs) && mx4_few_fits(n)) {
     hipLaunchKernelGGL(mx4_gemm_few_k<T>, dim3((unsigned)((n + 15) / 16)), dim3(512), 0, st, a, as, w, ws, m, n, slabs, bias, res, ld_res, out, ld);
     return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
   }

@@ -9,6 +9,8 @@ namespace pahq {
 // 7.8 (14.7), 1 x 11008 x 4096 8.3 (8.7), but 16 x 11008 x 4096 10.9 (8.9) and 11 x 31513 x 9086 47 (34).  Over 70 sizes
 // 1.002 of the better one's time in the mean and 1.11 at most; where the last call left the weights in the caches, 1.015 and 1.49.
 inline bool mx4_few(long long m, long long n, int slabs) { return m <= 16 && (m <= 4 || n < 4000 || slabs < 10); }
+// Whether a launch can count that: 512 threads for 16 columns, fewer than 2^32 in all.  Beyond, tiles take few rows too.
+inline bool mx4_few_fits(long long n) { return (n + 15) / 16 * 512 < 1ll << 32; }
 
 // Otherwise tiles of `tile` x `tile`, the sum over k shared by `groups` groups of waves.  The times in microseconds are fitted to
 // 400 random sizes from 17 x 16 x 32 to 8192 x 50000 x 12000 (bfloat16 results): one workgroup alone takes
