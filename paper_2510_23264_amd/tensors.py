@@ -72,7 +72,11 @@ class Mx4:
         at = both.data_ptr()
         return cls._of(both, (at, at + rows * groups * 128, int(rows), int(cols), both.device.index))
 
-    def __reduce__(self):                                   # a copy, or a pickle, is a matrix of its own memory
+    # a copy, shallow or deep, or a pickle, is a matrix of its own memory
+    def __copy__(self):
+        return Mx4(self.codes.clone(), self.scales.clone(), self.cols)
+
+    def __reduce__(self):
         return Mx4, (self.codes, self.scales, self.cols)
 
     @property
