@@ -41,3 +41,10 @@ def test_all_its_names():
         "import paper_2510_23264_amd.tensors as t\n"
         "assert all(globals()[n] is getattr(t, n) for n in %r) and Model and lib\n"
         "from paper_2510_23264_amd import rotary, Mx4\n" % (NAMES,))
+
+
+def test_the_build_check_loads_the_extension():
+    run("import __graft_entry__ as g\n"
+        "from paper_2510_23264_amd import build\n"
+        "build.build = lambda **how: None\n"
+        "g.build()\n")
