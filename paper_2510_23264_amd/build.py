@@ -1,8 +1,10 @@
 """Builds libpahq.so (HIP, gfx950 only) in-tree with hipcc, and _tensors.so, the torch side of its operators on device tensors."""
 import importlib.util
 import os
+import shutil
 import subprocess
 import sysconfig
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -27,8 +29,18 @@ def _compile(src):
 
 
 def _extension():
-    """csrc/tensors_ext.cpp against torch's and Python's headers; torch's libraries are there when tensors.py loads it."""
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    """csrc/tensors_ext.cpp against torch's and Python's headers; torch's libraries are there when tensors.py loads it.  libpahq.so
+    needs none of them: where one is missing it is left without the extension, and tensors.py says so when it is used."""
+    spec = importlib.util.find_spec("torch")
+    torch = os.path.dirname(spec.origin) if spec else ""
+    missing = [what for what, there in (("torch", spec), ("torch's headers", spec and os.path.isdir(os.path.join(torch, "include", "ATen"))),
+                                        ("Python's headers", os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h"))),
+                                        ("g++", shutil.which("g++"))) if not there]
+    if missing:
+        if os.path.exists(EXTENSION):                       # one that was built for another libpahq.so
+            os.remove(EXTENSION)
+        warnings.warn("no operators on device tensors (_tensors.so): without " + ", ".join(missing))
+        return
     subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-I" + os.path.join(torch, "include"),
                     "-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include"), "-I/opt/rocm/include", "-I" + sysconfig.get_paths()["include"],
                     os.path.join(CSRC, "tensors_ext.cpp"), "-o", EXTENSION, "-L" + HERE, "-l:libpahq.so", "-L" + os.path.join(torch, "lib"),
