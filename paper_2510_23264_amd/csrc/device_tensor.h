@@ -17,6 +17,17 @@ inline bool overlap(const void* p, size_t pn, const void* q, size_t qn) {
   const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
   return a < b + qn && b < a + pn;
 }
+// Bytes from the first to the last element of [outer][inner][row], strides in elements; false where no memory is as large (or the
+// count passes 64 bits).
+inline bool extent(long long outer, long long outer_stride, long long inner, long long inner_stride, long long row, int eb, size_t* bytes) {
+  long long a, b;
+  if (__builtin_mul_overflow(outer - 1, outer_stride, &a) || __builtin_mul_overflow(inner - 1, inner_stride, &b) || __builtin_add_overflow(a, b, &a) ||
+      __builtin_add_overflow(a, row, &a) || a > 1ll << 53)
+    return false;
+  *bytes = (size_t)a * eb;
+  return true;
+}
+inline bool extent(long long rows, long long stride, long long row, int eb, size_t* bytes) { return extent(rows, stride, 1, 0, row, eb, bytes); }
 
 // Two matrices of rows of pn and qn bytes whose rows lie `stride` bytes apart in both (0: not the same), as columns of one: no row
 // of one touches a row of the other.

@@ -556,7 +556,9 @@ extern "C" int pahq_mx4_quantize(void* hip_stream, const void* x, int32_t dtype,
   if (!held_aligned(codes, scales) || (uintptr_t)x % dtype_bytes(dtype)) return PAHQ_EINVAL;
   // grid.y counts 256 elements down the columns
   if (too_big(rows, cols) || (down && cols > 65535 * 256)) return PAHQ_ETOOBIG;
-  const size_t xb = (size_t)((down ? (cols - 1ll) * ld + rows : (rows - 1ll) * ld + cols) * dtype_bytes(dtype)), cb = code_bytes(rows, cols);
+  const size_t cb = code_bytes(rows, cols);
+  size_t xb;
+  if (!extent(down ? cols : rows, ld, down ? rows : cols, dtype_bytes(dtype), &xb)) return PAHQ_EINVAL;
   if (overlap(x, xb, codes, cb) || overlap(x, xb, scales, cb / 16) || overlap(codes, cb, scales, cb / 16)) return PAHQ_EINVAL;
   hipStream_t st = (hipStream_t)hip_stream;
   switch (dtype) {
@@ -572,7 +574,9 @@ extern "C" int pahq_mx4_dequantize(void* hip_stream, const uint8_t* codes, const
   if (rows == 0) return PAHQ_OK;
   if (!out || !codes || !scales || ld < cols || !held_aligned(codes, scales) || (uintptr_t)out % dtype_bytes(dtype)) return PAHQ_EINVAL;
   if (too_big(rows, cols)) return PAHQ_ETOOBIG;
-  const size_t ob = (size_t)(((rows - 1ll) * ld + cols) * dtype_bytes(dtype)), cb = code_bytes(rows, cols);
+  const size_t cb = code_bytes(rows, cols);
+  size_t ob;
+  if (!extent(rows, ld, cols, dtype_bytes(dtype), &ob)) return PAHQ_EINVAL;
   if (overlap(out, ob, codes, cb) || overlap(out, ob, scales, cb / 16)) return PAHQ_EINVAL;
   hipStream_t st = (hipStream_t)hip_stream;
   switch (dtype) {
@@ -592,12 +596,14 @@ extern "C" int pahq_mx4_gemm(void* hip_stream, const uint8_t* a_codes, const uin
   if ((uintptr_t)out % eb || (uintptr_t)residual % eb || (uintptr_t)bias % 4) return PAHQ_EINVAL;
   // a tile's rows are addressed by 32 bits, tiles counted by 31; 512 threads take 16 columns of few rows
   if (k > PAHQ_MX4_MAX_K || too_big(m, k) || too_big(n, k) || ((m + 31ll) / 32) * ((n + 31ll) / 32) >= (1ll << 31) - 8) return PAHQ_ETOOBIG;
-  const size_t ob = (size_t)(((m - 1ll) * ld_out + n) * eb), ab = code_bytes(m, k), wb = code_bytes(n, k);
+  const size_t ab = code_bytes(m, k), wb = code_bytes(n, k);
+  size_t ob, rb = 0;
+  if (!extent(m, ld_out, n, eb, &ob) || (residual && !extent(m, ld_residual, n, eb, &rb))) return PAHQ_EINVAL;
   if (overlap(out, ob, a_codes, ab) || overlap(out, ob, a_scales, ab / 16) || overlap(out, ob, w_codes, wb) || overlap(out, ob, w_scales, wb / 16) ||
       (bias && overlap(out, ob, bias, (size_t)n * 4)))
     return PAHQ_EINVAL;
   // the residual may be the result's own rows: every element is read by the thread that writes it
-  if (residual && !(residual == out && ld_residual == ld_out) && overlap(out, ob, residual, (size_t)(((m - 1ll) * ld_residual + n) * eb)) &&
+  if (residual && !(residual == out && ld_residual == ld_out) && overlap(out, ob, residual, rb) &&
       !side_by_side(out, (size_t)n * eb, residual, (size_t)n * eb, ld_out == ld_residual ? (size_t)ld_out * eb : 0))
     return PAHQ_EINVAL;
   hipStream_t st = (hipStream_t)hip_stream;

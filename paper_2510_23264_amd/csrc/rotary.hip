@@ -106,12 +106,10 @@ template <typename T>
 int rotary_as(hipStream_t st, const T* x, T* out, const RotaryArgs& q, int layout, bool copy) {
   return layout == PAHQ_ROTARY_HALF ? rotary_as<T, true>(st, x, out, q, copy) : rotary_as<T, false>(st, x, out, q, copy);
 }
-// [tokens][heads][d] in either order of the first two, no two elements in one place; extent in elements
-bool strides_ok(long long tokens, long long heads, long long d, long long st, long long sh, long long* extent) {
-  if (st < 0 || sh < 0) return false;
+// [tokens][heads][d] in either order of the first two, no two elements in one place; the strides' products fit (extent was asked)
+bool strides_ok(long long tokens, long long heads, long long d, long long st, long long sh) {
   const bool rows = (heads == 1 || sh >= d) && (tokens == 1 || st >= (heads - 1) * sh + d);
   const bool planes = (tokens == 1 || st >= d) && (heads == 1 || sh >= (tokens - 1) * st + d);
-  *extent = (tokens - 1) * st + (heads - 1) * sh + d;
   return rows || planes;
 }
 }  // namespace
@@ -155,14 +153,15 @@ extern "C" int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32
   if (!x || !out || !positions || !table || (uintptr_t)x % eb || (uintptr_t)out % eb || (uintptr_t)positions % 8 || (uintptr_t)table % 8) return PAHQ_EINVAL;
   // workgroups are counted in 16 bits along the heads, threads in 32 along the tokens
   if (heads > 65535 || d_head > PAHQ_ROTARY_MAX_HEAD || tokens > PAHQ_ROTARY_MAX_TOKENS) return PAHQ_ETOOBIG;
-  long long xn, on;
-  if (x_token < 0 || x_head < 0 || !strides_ok(tokens, heads, d_head, out_token, out_head, &on)) return PAHQ_EINVAL;
-  xn = (tokens - 1ll) * x_token + (heads - 1ll) * x_head + d_head;      // only read: rows may share memory
+  size_t xb, ob;                                                        // x is only read: its rows may share memory
+  if (x_token < 0 || x_head < 0 || out_token < 0 || out_head < 0 || !extent(tokens, x_token, heads, x_head, d_head, eb, &xb) ||
+      !extent(tokens, out_token, heads, out_head, d_head, eb, &ob) || !strides_ok(tokens, heads, d_head, out_token, out_head))
+    return PAHQ_EINVAL;
   const bool in_place = x == out && x_token == out_token && x_head == out_head;
   const size_t xw = (size_t)((heads - 1ll) * x_head + d_head) * eb, ow = (size_t)((heads - 1ll) * out_head + d_head) * eb;      // of a token
-  if (!in_place && overlap(x, (size_t)xn * eb, out, (size_t)on * eb) && !side_by_side(x, xw, out, ow, x_token == out_token ? (size_t)x_token * eb : 0))
+  if (!in_place && overlap(x, xb, out, ob) && !side_by_side(x, xw, out, ow, x_token == out_token ? (size_t)x_token * eb : 0))
     return PAHQ_EINVAL;
-  if (overlap(out, (size_t)on * eb, positions, (size_t)tokens * 8) || overlap(out, (size_t)on * eb, table, (size_t)rot_dim * 4)) return PAHQ_EINVAL;
+  if (overlap(out, ob, positions, (size_t)tokens * 8) || overlap(out, ob, table, (size_t)rot_dim * 4)) return PAHQ_EINVAL;
   hipStream_t st = (hipStream_t)hip_stream;
   const RotaryArgs q = {x_token, x_head, out_token, out_head, (const long long*)positions, (const unsigned long long*)table, tokens, heads, d_head, rot_dim,
                         0, 0, 0, 0, 0, magnitude, inverse ? -1.f : 1.f};
