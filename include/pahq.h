@@ -470,8 +470,9 @@ enum { PAHQ_F32 = 0, PAHQ_BF16 = 1, PAHQ_F16 = 2 };
  * stride ld >= rows, so that the blocks run down the columns of x: a weight master [k][n] becomes the [n][k] the product takes.
  * pahq_mx4_dequantize: the values; exact in PAHQ_F32 and PAHQ_BF16, rounded once in PAHQ_F16.
  * pahq_mx4_gemm: out[i][j] = sum_k a[i][k] w[j][k] (+ bias[j]) (+ residual[i][j]); a [m][k], w [n][k] in this format, bias
- * fp32 [n] or NULL, residual of out's type or NULL (it may be out itself, with the same stride).  Sums in fp32, one rounding
- * to out's type.  The order of a sum depends on the sizes alone: the same call gives the same bits. */
+ * fp32 [n] or NULL, residual of out's type or NULL (it may be out itself, with the same stride).  Sums in fp32 (the 32 products
+ * of a block exactly, blocks with a rounding each), one rounding to out's type.  The order of a sum depends on the sizes alone:
+ * the same call gives the same bits. */
 enum { PAHQ_MX4_BY_ROWS = 0, PAHQ_MX4_BY_COLUMNS = 1 };
 enum { PAHQ_MX4_MAX_K = 1 << 24 };            /* of a product */
 int pahq_mx4_bytes(int32_t rows, int32_t cols, size_t* codes, size_t* scales);
