@@ -248,6 +248,14 @@ PyObject* rotary(PyObject* const* a) {
   return THPVariable_Wrap(out);
 }
 
+void set_error_of_torch(const char* name, const char* text) {
+  PyObject* const torch = PyImport_ImportModule("torch");
+  PyObject* const error = torch ? PyObject_GetAttrString(torch, name) : nullptr;
+  if (error) PyErr_SetString(error, text);
+  Py_XDECREF(error);
+  Py_XDECREF(torch);
+}
+
 // Arguments counted, C++ exceptions turned into Python's
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -260,6 +268,10 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   } catch (const PythonError&) {
   } catch (const Refused& e) {
     PyErr_SetString(PyExc_ValueError, e.what());
+  } catch (const c10::OutOfMemoryError& e) {          // under torch's own name, for programs that make room and try again
+    set_error_of_torch("OutOfMemoryError", e.what_without_backtrace());
+  } catch (const c10::Error& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
   } catch (...) {
