@@ -138,8 +138,8 @@ def rotary_table(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=0.
 
 
 def _tangent(x):
-    """Whether x has a forward-mode derivative to carry on (outside of forward_ad.dual_level nothing has)."""
-    return forward_ad._current_level >= 0 and torch._C._is_fwd_grad_enabled() and forward_ad.unpack_dual(x).tangent is not None
+    """Whether x has a forward-mode derivative to carry on, inside of a forward_ad.dual_level."""
+    return torch._C._is_fwd_grad_enabled() and forward_ad.unpack_dual(x).tangent is not None
 
 
 def _rotary(x, positions, table, layout, magnitude, inverse, out):
@@ -180,7 +180,8 @@ def rotary(x, positions, table, layout="half", magnitude=1.0, inverse=False, out
     may be x, except where a derivative is recorded."""
     if layout not in _LAYOUTS:
         raise ValueError("layout: 'half' or 'interleaved'")
-    if torch.is_grad_enabled() and (x.requires_grad or out is not None and out.requires_grad) or _tangent(x):
+    if torch.is_grad_enabled() and (x.requires_grad or out is not None and out.requires_grad) \
+            or forward_ad._current_level >= 0 and _tangent(x):             # outside of a dual_level nothing has a tangent
         _need(out is None, "out: not where a gradient is recorded")
         return _Rotary.apply(x, positions, table, _LAYOUTS[layout], float(magnitude), bool(inverse))
     return _rotary(x, positions, table, _LAYOUTS[layout], magnitude, bool(inverse), out)
