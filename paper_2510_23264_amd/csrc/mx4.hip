@@ -4,7 +4,7 @@
 //
 // Why the instructions may be used directly, where the E4M3 products of the engine go through fp16: a block of 32 products under
 // one pair of scales, multiples of 1/4 of up to 36 each, is summed exactly, and blocks are added like binary32 numbers, each addition
-// rounded to nearest, subnormal numbers included.  Measured through every form of the product: nothing lost where all partial sums
+// rounded to nearest, subnormal numbers included.  Measured through both instructions: nothing lost where all partial sums
 // are binary32 numbers (one product 2^16 times as large as 224 others, a slab 2^8 times as large as those behind it); otherwise within
 // one unit of 2^-24 of sum |a w| a block (at most 6 units over 256 elements, 18 over 4096, with scales up to 2^34 apart) and
 // without a bias (all products positive, scales 2^24 apart: 0.01 units in the mean).
@@ -65,7 +65,9 @@ __global__ __launch_bounds__(256) void mx4_rows_quant_k(const T* x, long long ld
 
 // x [cols][rows] (the masters' layout [k][n]): one thread holds blocks of 32 down the columns of one word of a row, neighbouring
 // threads neighbouring words.  Workgroup: 64 words, 256 elements down, a block a wave; the codes go through LDS so that a row's
-// 128 bytes leave together (as 16 bytes from each thread 4096 x 4096 in bfloat16 took 17 us, 4096 x 11008 in fp32 34).
+// 128 bytes leave together.  Back to back into the same memory, as 16 bytes from each thread and so: in bfloat16 4096 x 4096 16.8 and
+// 14.9 us, 4096 x 11008 44.4 and 31.7; in fp32 14.5 and 12.9, 32.8 and 32.0.  All workgroups of a round load first and then store: with x
+// from HBM these take 28 and 59, 31 and 74 us (profiles/operators_counters.txt), the same values by rows 15 and 35, 25 and 64.
 template <typename T>
 __global__ __launch_bounds__(512) void mx4_cols_quant_k(const T* x, long long ld, int rows, int cols, int groups, uint8_t* codes, uint8_t* scales) {
   constexpr int N = 4 / sizeof(T), ROWS = 64 * N;
@@ -147,8 +149,10 @@ __device__ __forceinline__ v8i four_bits(int4 v) { return (v8i){v.x, v.y, v.z, v
 // mod 8) and joined in LDS in the order of the waves, so results do not depend on timing.  Operands come straight from global
 // memory: a lane reads two neighbouring blocks of its row with their scales, which are one halfword, and the four lanes of a row
 // take 128 contiguous bytes.  Which 32 elements of the slab a lane's block is does not matter to the sum as long as both
-// operands agree.  Rows and columns past the end read the last one and are not stored.  Bound by the way to the first bytes:
-// one token through 4096 x 4096 takes 4.3 us, 1.7 of them the weights' bytes at the rate of a large copy, 2.3 an empty launch.
+// operands agree.  Rows and columns past the end read the last one and are not stored.  Bound by waits for memory one after the other: a
+// wave has one slab in flight, so k = 4096 is two waits and k = 11008 six, and behind the join bias and residual are two more.  In a trace
+// with the weights in HBM 1 x 4096 x 4096 with both takes 5.9 us (1.7 for the bytes at the rate of a large copy, 2.3 an empty
+// launch), 1 x 4096 x 11008 10.6 (4.7), 1 x 1024 x 16000 9.0 (1.7), where 64 workgroups read alone.
 template <typename T>
 __global__ __launch_bounds__(512) void mx4_gemm_few_k(const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, int m, int n, int slabs,
                                                       const float* bias, const T* res, long long ld_res, T* out, long long ld) {
@@ -342,8 +346,8 @@ __global__ __launch_bounds__(KW * WM * WN * 64, (Mx4Tile<AF, WF, WM, WN, KW>::PE
 
   // The results go through LDS, so that a store writes whole lines: V columns a lane.  Non-temporal: what the results would push
   // out of the caches, operands and residual, is worth more there (8192 x 11008 x 4096 248 -> 220 us, 2048 x 8192 x 1024 with a
-  // residual in fp32 40 -> 30; without LDS, 8 bytes a lane, 211 and 30, but 50 x 50257 x 768 in fp32 13.5 instead of 10.8).  What
-  // reads the results next pays some of it back: with mx4_quantize behind them 286 and 285 us, 2048 x 4096 x 1024 18 and 19.
+  // residual in fp32 40 -> 30; without LDS, 8 bytes a lane, 211 and 30, but 50 x 50257 x 768 in fp32 13.5 instead of 10.8).  Where
+  // the results are read next nothing is left of it: with mx4_quantize behind them 286 and 285 us, 2048 x 4096 x 1024 18 and 19.
   constexpr int V = 16 / sizeof(T), ACROSS = WF * 32 / V;
   const auto finish = [&](float* f, const float* b, u32x4 u, T* o, const T* r, int left) {
     if (left >= V) {

@@ -13,11 +13,12 @@ inline bool mx4_few(long long m, long long n, int slabs) { return m <= 16 && (m 
 inline bool mx4_few_fits(long long n) { return (n + 15) / 16 * 512 < 1ll << 32; }
 
 // Otherwise tiles of `tile` x `tile`, the sum over k shared by `groups` groups of waves.  The times in microseconds are fitted to
-// 400 random sizes from 17 x 16 x 32 to 8192 x 50000 x 12000 (bfloat16 results): one workgroup alone takes
+// 400 random sizes from 17 x 16 x 32 to 8192 x 50000 x 12000, all with bfloat16 results and without a residual, which the estimate
+// therefore knows nothing of: one workgroup alone takes
 // launch + start + slab * (its slabs of 256 elements of k); each further one of a compute unit `round` of that, where only one
 // fits (whole) a whole round of the chip half of the time.  The form with the least estimate took 1.01 of the best one's time in
 // the mean, 1.2 at most.  A last round of 256 x 256 tiles that leaves most of the chip without one stays as it is: as smaller
-// tiles in a launch of their own it cost 250 us instead of 244 (8192 x 11008 x 4096), for the chip's power bounds the whole.
+// tiles in a launch of their own it cost 250 us instead of 244 (8192 x 11008 x 4096).
 struct Mx4Form { int tile, groups; float launch, start, slab, round; bool whole; };
 constexpr int MX4_FORMS = 5;
 constexpr Mx4Form mx4_forms[MX4_FORMS] = {
