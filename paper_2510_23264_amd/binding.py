@@ -4,6 +4,7 @@ device workspace and to provide the stream."""
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 import numpy as np
 
@@ -61,12 +62,22 @@ KERNEL_CLASSES = ("gather_norm_quant", "edge_patch", "gemm_fp8", "gemm_f32", "at
 _lib = None
 
 
+def _runtime_of_torch():
+    """A torch that brings a HIP runtime of its own (the same soname as the system's) has to have it loaded before libpahq.so asks for
+    one, whether or not torch is imported yet: two runtimes in a process do not know each other's streams and memory."""
+    spec = importlib.util.find_spec("torch")
+    own = os.path.join(os.path.dirname(spec.origin), "lib", "libamdhip64.so") if spec and spec.origin else ""
+    if os.path.exists(own):
+        C.CDLL(own)
+
+
 def lib():
     """Loads libpahq.so (built in-tree by paper_2510_23264_amd.build).  There is no fallback."""
     global _lib
     if _lib is None:
         if not os.path.exists(_LIB_PATH):
             raise RuntimeError(f"{_LIB_PATH} is missing: run `python -m paper_2510_23264_amd.build` first")
+        _runtime_of_torch()
         L = C.CDLL(_LIB_PATH)
         cfgp, i32p, i64p, u8p, f32p = C.POINTER(Config), C.POINTER(C.c_int32), C.POINTER(C.c_int64), \
             C.POINTER(C.c_uint8), C.POINTER(C.c_float)

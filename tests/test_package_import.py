@@ -4,6 +4,8 @@ import os
 import subprocess
 import sys
 
+import pytest
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 NAMES = ("Mx4", "mx4_quantize", "mx4_dequantize", "mx4_gemm", "rotary_table", "rotary")
 
@@ -48,3 +50,17 @@ def test_the_build_check_loads_the_extension():
         "from paper_2510_23264_amd import build\n"
         "build.build = lambda **how: None\n"
         "g.build()\n")
+
+
+@pytest.mark.parametrize("first", ["P.lib()", "import torch", "P.n_senders", "P.mx4_gemm"])
+def test_one_hip_runtime_whatever_is_loaded_first(first):
+    run("import re, paper_2510_23264_amd as P\n"
+        "%s\n"
+        "P.lib()\n"
+        "import torch\n"
+        "from paper_2510_23264_amd import _tensors\n"
+        "maps = open('/proc/self/maps').read()\n"
+        "assert 'libpahq.so' in maps and '_tensors.so' in maps\n"
+        "for name in ('libamdhip64', 'libhsa-runtime64'):\n"
+        "    found = set(re.findall(r'/\\S*/' + name + r'\\S*', maps))\n"
+        "    assert len(found) == 1, found\n" % first)
