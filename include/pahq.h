@@ -512,6 +512,73 @@ int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32_t tokens, 
                 int64_t x_head, const int64_t* positions, const uint64_t* table, int32_t rot_dim, int32_t layout,
                 float magnitude, int32_t inverse, void* out, int64_t out_token, int64_t out_head);
 
+/* A paged cache of keys and values, and the attention that reads it.  Keys and values lie in pages of page_size rows, rows of d_head
+ * elements, one row a token and head; a sequence is a list of pages, its row j in row j % page_size of page j / page_size of the list.
+ *   pahq_kv_cache   keys, values: row `slot` of head `head` of page `page` begins page * page_stride + head * head_stride +
+ *                   slot * slot_stride elements behind the pointer, elements of a row contiguous; any order of the three, no two rows in
+ *                   one place, values the same way as keys (both may be parts of one tensor).  Pointers and strides in
+ *                   whole 16 bytes.  d_head a multiple of 8 up to PAHQ_KV_MAX_HEAD, heads up to 65535
+ *   pahq_kv_batch   DEVICE int32: `starts` [batch + 1], the tokens of sequence b being rows starts[b] .. starts[b + 1] - 1 of an
+ *                   operator's rows [tokens]; `lengths` [batch], how many rows sequence b has, its new tokens included, which are the
+ *                   last ones; `pages` [batch][width], row stride ld_pages >= width.  With n_b = starts[b + 1] - starts[b], new
+ *                   token i of sequence b is its row base_b + i, base_b = lengths[b] - n_b
+ * What the device arrays hold is not the host's to check, and whatever it is, no memory is touched that is not the operands': starts
+ * are clipped to 0 .. tokens and a negative n_b is 0; a length is clipped to width * page_size; a token whose row would be negative
+ * or behind its list of pages, or whose page is not 0 .. pages - 1, is not written, and a query that sees a row of such a
+ * page gets NaN.  Rows of tokens in front of starts[0] or behind starts[batch] are not written.  Two tokens with one place (a page
+ * in two lists, or twice in one) are written in any order.
+ *
+ * pahq_kv_append writes new tokens' rows: keys turned as pahq_rotary turns them, values as they are; and out gets the queries, turned the same way.
+ *   k, v [tokens][cache heads][d_head] and q, out [tokens][q_heads][d_head] in the cache's dtype, strides of their own for
+ *   tokens and heads.  positions int64 [tokens], NULL: a token's row in its sequence.  table, rot_dim, layout, magnitude as in
+ *   pahq_rotary; table NULL: nothing turns.  q NULL (with out NULL): no queries.  out may be q itself with the same strides.
+ *   The keys and queries have the bits pahq_rotary gives them. */
+typedef struct {
+  void *keys, *values;
+  int32_t dtype, pages, page_size, heads, d_head;
+  int64_t page_stride, head_stride, slot_stride;
+} pahq_kv_cache;
+typedef struct {
+  const int32_t *starts, *lengths, *pages;
+  int32_t batch, width;
+  int64_t ld_pages;
+  int32_t tokens;
+} pahq_kv_batch;
+typedef struct {
+  const void* at;
+  int64_t token, head;                        /* strides in elements */
+} pahq_kv_rows;
+enum { PAHQ_KV_MAX_HEAD = 256, PAHQ_KV_MAX_BATCH = 65535 };
+int pahq_kv_append(void* hip_stream, const pahq_kv_cache* cache, const pahq_kv_batch* batch, const pahq_kv_rows* k, const pahq_kv_rows* v,
+                   const int64_t* positions, const uint64_t* table, int32_t rot_dim, int32_t layout, float magnitude,
+                   const pahq_kv_rows* q, int32_t q_heads, const pahq_kv_rows* out);
+
+/* pahq_kv_attention: the new tokens' queries over their sequences' rows.  Query head h goes with cache head h / (q_heads / heads);
+ * heads divides q_heads.  For new token i of sequence b, over the rows j < lengths[b] it sees,
+ *     out = sum_j p_j values_j,  p_j = exp(s_j - max s) / sum exp(s - max s),  s_j = scale * (q . keys_j)
+ * It sees the rows in front of the new ones, j < base_b, and of the new ones
+ *     tree NULL   those up to itself, j - base_b <= i
+ *     tree        uint64 [tokens][words >= 1]: those whose bit (j - base_b) % 64 of word (j - base_b) / 64 of its row is set (none behind
+ *                 words * 64); for a drafted tree, of which the new tokens are the nodes, pahq_tree_bits fills HOST memory
+ *                 with [n][(n + 63) / 64] words, a node's own bit and its ancestors', from parents [n]: parents[i] < i, -1 at a root
+ * What a query does not see has no influence on it, infinities and NaN included.  One that sees nothing, or only scores of -inf, gets
+ * zeros.  Products in the cache's dtype with sums in fp32, softmax in fp32, its weights rounded to the dtype for their product
+ * with the values, the sum divided by the weights' sum and rounded once.  The same call gives the same bits.
+ * q, out as in pahq_kv_append; out may be q itself with the same strides.  tokens * (q_heads / heads) below 2^31 - 2^16.
+ * workspace: DEVICE, 16-byte aligned, of at least the bytes that pahq_kv_attention_workspace says for the same arguments (may be 0); its
+ * contents are lost, and calls that overlap need one each. */
+int pahq_tree_bits(const int32_t* parents, int32_t n, uint64_t* bits);
+int pahq_kv_attention_workspace(const pahq_kv_cache* cache, const pahq_kv_batch* batch, int32_t q_heads, size_t* bytes);
+int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, const pahq_kv_batch* batch, const pahq_kv_rows* q, int32_t q_heads,
+                      const uint64_t* tree, int32_t words, float scale, const pahq_kv_rows* out, void* workspace, size_t workspace_bytes);
+
+/* pahq_kv_keep: of sequence b's new tokens those at paths[b][0] < paths[b][1] < ... stay (a path through a drafted tree: keys and values
+ * of token paths[b][i] move to row base_b + i) and the rest is dropped: new_lengths[b] = base_b + how many stay.
+ *   paths DEVICE int32 [batch][depth]; a path ends with the row, or at the first entry that is not greater than the one before, is negative or
+ *   not below n_b.  new_lengths DEVICE int32 [batch], not the batch's own lengths.  Rows that cannot be read (as above) are not moved. */
+int pahq_kv_keep(void* hip_stream, const pahq_kv_cache* cache, const pahq_kv_batch* batch, const int32_t* paths, int32_t depth,
+                 int32_t* new_lengths);
+
 const char* pahq_strerror(int code);
 void pahq_free(pahq_model*);            /* frees host state only; the workspace stays the caller's */
 

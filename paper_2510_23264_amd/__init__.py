@@ -3,10 +3,11 @@ import importlib as _importlib
 import importlib.util as _importlib_util
 
 from .binding import (lib, PahqError, Config, Model, n_senders, n_receivers, n_upstream, edge_count, edge_id,
-                      node_of_receiver, workspace_bytes, measure_ceilings, quantize_rows_noalloc, tau_grid, rotary_entries, TraceRec,
+                      node_of_receiver, workspace_bytes, measure_ceilings, quantize_rows_noalloc, tau_grid, rotary_entries, tree_words, TraceRec,
                       ALL_FP32, ALL_FP8, PAHQ, MMA_FP8, MMA_F16_EXACT, METRIC_KL, METRIC_LOGIT_DIFF, W_Q, W_K, W_V, W_O, W_IN, W_GATE, W_OUT, W_U)
 
-_OF_TENSORS = ("Mx4", "mx4_quantize", "mx4_dequantize", "mx4_gemm", "rotary_table", "rotary")
+_OF_TENSORS = ("Mx4", "mx4_quantize", "mx4_dequantize", "mx4_gemm", "rotary_table", "rotary", "KvCache", "KvBatch", "kv_append", "kv_attention",
+               "kv_keep", "tree_bits")
 __all__ = [_n for _n in globals() if not _n.startswith("_")] + (list(_OF_TENSORS) if _importlib_util.find_spec("torch") else [])
 
 

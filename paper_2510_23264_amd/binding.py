@@ -56,6 +56,20 @@ class KernelStat(C.Structure):
     _fields_ = [("launches", C.c_int64), ("ms", C.c_double), ("flops", C.c_double), ("bytes", C.c_double)]
 
 
+class KvCacheArg(C.Structure):
+    _fields_ = [("keys", C.c_void_p), ("values", C.c_void_p), ("dtype", C.c_int32), ("pages", C.c_int32), ("page_size", C.c_int32),
+                ("heads", C.c_int32), ("d_head", C.c_int32), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64)]
+
+
+class KvBatchArg(C.Structure):
+    _fields_ = [("starts", C.c_void_p), ("lengths", C.c_void_p), ("pages", C.c_void_p), ("batch", C.c_int32), ("width", C.c_int32),
+                ("ld_pages", C.c_int64), ("tokens", C.c_int32)]
+
+
+class KvRowsArg(C.Structure):
+    _fields_ = [("at", C.c_void_p), ("token", C.c_int64), ("head", C.c_int64)]
+
+
 KERNEL_CLASSES = ("gather_norm_quant", "edge_patch", "gemm_fp8", "gemm_f32", "attention", "stream_update",
                   "hidden_quant", "logsumexp", "kl", "oproj_fused")
 
@@ -125,6 +139,13 @@ def lib():
             "pahq_rotary_table": [C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4 + [C.POINTER(C.c_uint64)],
             "pahq_rotary": [C.c_void_p, C.c_void_p] + [C.c_int32] * 4 + [C.c_int64] * 2 + [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                             C.c_float, C.c_int32, C.c_void_p, C.c_int64, C.c_int64],
+            "pahq_kv_append": [C.c_void_p, C.POINTER(KvCacheArg), C.POINTER(KvBatchArg), C.POINTER(KvRowsArg), C.POINTER(KvRowsArg), C.c_void_p, C.c_void_p,
+                               C.c_int32, C.c_int32, C.c_float, C.POINTER(KvRowsArg), C.c_int32, C.POINTER(KvRowsArg)],
+            "pahq_tree_bits": [C.POINTER(C.c_int32), C.c_int32, C.POINTER(C.c_uint64)],
+            "pahq_kv_attention_workspace": [C.POINTER(KvCacheArg), C.POINTER(KvBatchArg), C.c_int32, C.POINTER(C.c_size_t)],
+            "pahq_kv_attention": [C.c_void_p, C.POINTER(KvCacheArg), C.POINTER(KvBatchArg), C.POINTER(KvRowsArg), C.c_int32, C.c_void_p, C.c_int32,
+                                  C.c_float, C.POINTER(KvRowsArg), C.c_void_p, C.c_size_t],
+            "pahq_kv_keep": [C.c_void_p, C.POINTER(KvCacheArg), C.POINTER(KvBatchArg), C.c_void_p, C.c_int32, C.c_void_p],
             "pahq_compare_encoders": [C.c_void_p, C.c_void_p, C.POINTER(C.c_uint64), C.POINTER(C.c_uint32)],
             "pahq_measure_ceilings": [C.c_void_p, C.c_void_p, C.c_size_t, C.POINTER(C.c_double), C.POINTER(C.c_double)],
         }
@@ -211,6 +232,17 @@ def rotary_entries(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=
     out = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.uint64)
     _chk(lib().pahq_rotary_table(int(rot_dim), float(theta), ROTARY_SCALING[scaling], float(factor), float(original), float(turns[0]),
                                  float(turns[1]), _ptr(out, C.c_uint64)), "pahq_rotary_table")
+    return out
+
+
+def tree_words(parents):
+    """uint64 [n][(n + 63) / 64]: of every node of a drafted tree, bits of itself and its ancestors (pahq_tree_bits).  parents [n]: each
+    node's parent, which comes before it, -1 at a root."""
+    parents = np.ascontiguousarray(parents, dtype=np.int32)
+    if parents.ndim != 1:
+        raise ValueError("parents: one number a node")
+    out = np.zeros((len(parents), max(1, -(-len(parents) // 64))), dtype=np.uint64)
+    _chk(lib().pahq_tree_bits(_ptr(parents, C.c_int32), len(parents), _ptr(out, C.c_uint64)), "pahq_tree_bits")
     return out
 
 

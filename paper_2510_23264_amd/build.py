@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpahq.so")
 EXTENSION = os.path.join(HERE, "_tensors.so")
 SOURCES = ["rows.hip", "gemm.hip", "oproj.hip", "attn_kl.hip", "engine.hip", "api.hip", "ceilings.hip", "noalloc.hip", "mx4.hip",
-           "rotary.hip"]
+           "rotary.hip", "kv_cache.hip", "kv_attention.hip"]
 # -ffp-contract=off: a product and a sum are rounded separately unless the source says fmaf.  The same
 # expression (a norm's x * rstd * gain + offset, a GEMM epilogue's acc * scale + bias) is compiled into
 # several kernels -- cache passes and candidate passes take different ones -- and results that must agree

@@ -3,14 +3,14 @@
 //
 // The angle.  A frequency is kept as the fraction of a turn it advances in one position, in 64 binary digits, so position *
 // frequency modulo one turn is one 64-bit integer product, exact at every position; binary32 angles are off by more
-// than a hundredth of a radian from position 2^18 on.  The quarter turns come off as the product's two top digits, so
-// that what is left, at most an eighth of a turn, loses no more than 2^-25 of that when it becomes a float.
+// than a hundredth of a radian from position 2^18 on (rotary_turn.h).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
 #include <algorithm>
 #include "../../include/pahq.h"
 #include "device_tensor.h"
+#include "rotary_turn.h"
 
 namespace pahq {
 
@@ -39,13 +39,7 @@ __global__ __launch_bounds__(256) void rotary_k(const T* x, T* out, RotaryArgs q
   const int half = q.rot / 2, t0 = blockIdx.x * q.nt, nt = min(q.nt, q.tokens - t0), h0 = blockIdx.y * q.nh, nh = min(q.nh, q.heads - h0);
   for (int e = threadIdx.x; e < nt * half; e += 256) {
     const int t = e / half, i = e - t * half;
-    const unsigned long long phase = (unsigned long long)q.positions[t0 + t] * q.table[i] + (1ull << 61);
-    const int quarter = (int)(phase >> 62);
-    const int left = (int)(((long long)(phase << 2) >> 32) ^ 0x80000000ll);       // in 2^-34 turns, from -1/8 on
-    float s, c;
-    sincospif((float)left * 1.1641532182693481e-10f, &s, &c);                     // 2^-33: half turns
-    const float cq = quarter & 1 ? s : c, sq = quarter & 1 ? c : s;
-    turn[e] = make_float2((quarter == 1 || quarter == 2 ? -cq : cq) * q.magnitude, (quarter >= 2 ? -sq : sq) * q.magnitude * q.direction);
+    turn[e] = rotary_turn(q.positions[t0 + t], q.table[i], q.magnitude, q.direction);
   }
   __syncthreads();
   const int pairs = half / V;

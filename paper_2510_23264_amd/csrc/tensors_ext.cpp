@@ -13,6 +13,7 @@
 #include <c10/core/AutogradState.h>
 #include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <cmath>
 #include <exception>
 #include <optional>
 #include <stdexcept>
@@ -46,6 +47,11 @@ const Tensor& tensor(PyObject* o, const char* text) {
 long long number(PyObject* o) {
   const long long v = PyLong_AsLongLong(o);
   if (v == -1 && PyErr_Occurred()) throw PythonError();
+  return v;
+}
+double real(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw PythonError();
   return v;
 }
 int dtype_of(at::ScalarType t) {
@@ -225,8 +231,7 @@ PyObject* rotary(PyObject* const* a) {
        "positions: int64 [tokens], contiguous, on x's device");
   need(table.scalar_type() == at::kLong && table.dim() == 1 && on(table, device) && table.is_contiguous() && table.numel() >= 1 && 2 * table.numel() <= d,
        "table: from rotary_table, on x's device, for at most d_head elements");
-  const double magnitude = PyFloat_AsDouble(a[4]);
-  if (magnitude == -1.0 && PyErr_Occurred()) throw PythonError();
+  const double magnitude = real(a[4]);
   Tensor out;
   if (a[6] == Py_None) {
     out = at::empty_like(x, x.options(), at::MemoryFormat::Contiguous);
@@ -243,6 +248,154 @@ PyObject* rotary(PyObject* const* a) {
                                (const int64_t*)positions.data_ptr(), (const uint64_t*)table.data_ptr(), (int32_t)(2 * table.numel()), (int32_t)number(a[3]),
                                (float)magnitude, a[5] == Py_True, out.data_ptr(), ot, oh);
     if (rc) return PyLong_FromLong(rc);
+    written(out);
+  }
+  return THPVariable_Wrap(out);
+}
+
+// The first five arguments of every call on a cache: keys, values, starts, lengths, pages
+struct Paged {
+  Tensor keys, values;
+  pahq_kv_cache cache = {};
+  pahq_kv_batch batch = {};
+  at::DeviceIndex device;
+  Paged(PyObject* const* a, bool read_only) : keys(tensor(a[0], "keys: a tensor")), values(tensor(a[1], "values: a tensor")) {
+    device = keys.get_device();
+    need(keys.is_cuda() && keys.dim() == 4 && keys.sizes() == values.sizes() && keys.scalar_type() == values.scalar_type() && on(values, device) &&
+             dtype_of(keys.scalar_type()) >= 0 && keys.size(0) >= 1 && keys.size(1) >= 1 && keys.size(2) >= 1 && keys.size(3) >= 1,
+         "keys and values: [pages][heads][page_size][d_head] in float32, bfloat16 or float16 on one device");
+    need(!tracked(keys) && !tracked(values), read_only ? "a cache has no gradient: detach it" : "keys and values: without a gradient");
+    int64_t s[3];
+    for (int i = 0; i < 3; i++) {         // of a single one torch reports any stride
+      s[i] = keys.size(i) > 1 ? keys.stride(i) : 0;
+      need(s[i] == (values.size(i) > 1 ? values.stride(i) : 0), "keys and values: with the same strides");
+    }
+    need((keys.stride(3) == 1 && values.stride(3) == 1) || keys.size(3) == 1, "the elements of a row: contiguous");
+    cache = {keys.data_ptr(), values.data_ptr(), dtype_of(keys.scalar_type()), size32(keys.size(0)), size32(keys.size(2)), size32(keys.size(1)),
+             size32(keys.size(3)), s[0], s[1], s[2]};
+    const Tensor &starts = tensor(a[2], "starts: a tensor"), &lengths = tensor(a[3], "lengths: a tensor"), &pages = tensor(a[4], "pages: a tensor");
+    need(starts.scalar_type() == at::kInt && starts.dim() == 1 && starts.size(0) >= 1 && on(starts, device) && starts.is_contiguous(),
+         "starts: int32 [batch + 1], contiguous, on the cache's device");
+    need(lengths.scalar_type() == at::kInt && lengths.dim() == 1 && lengths.size(0) == starts.size(0) - 1 && on(lengths, device) && lengths.is_contiguous(),
+         "lengths: int32 [batch], contiguous, on the cache's device");
+    int64_t ld = 0;
+    need(pages.scalar_type() == at::kInt && pages.dim() == 2 && pages.size(0) == lengths.size(0) && on(pages, device) && (ld = row_stride(pages)) >= 0,
+         "pages: int32 [batch][width], rows contiguous, on the cache's device");
+    batch = {(const int32_t*)starts.data_ptr(), (const int32_t*)lengths.data_ptr(), (const int32_t*)pages.data_ptr(), size32(lengths.size(0)),
+             size32(pages.size(1)), ld, 0};
+  }
+  // rows [tokens][heads][d_head] of the cache's dtype; heads 0: any number
+  pahq_kv_rows rows(const Tensor& t, int64_t tokens, int64_t heads, const char* text) const {
+    need(t.dim() == 3 && (tokens < 0 || t.size(0) == tokens) && (heads ? t.size(1) == heads : t.size(1) >= 1) && t.size(2) == cache.d_head &&
+             t.scalar_type() == keys.scalar_type() && on(t, device) && !tracked(t),
+         text);
+    pahq_kv_rows r = {t.data_ptr(), 0, 0};
+    head_strides(t, &r.token, &r.head);
+    return r;
+  }
+};
+
+// (keys, values, starts, lengths, pages, k, v, positions, table, layout, magnitude, q, out)
+PyObject* kv_append(PyObject* const* a) {
+  Paged p(a, false);
+  const Tensor &k = tensor(a[5], "k: a tensor"), &v = tensor(a[6], "v: a tensor");
+  const pahq_kv_rows kr = p.rows(k, -1, p.cache.heads, "k: [tokens][cache heads][d_head] of the cache's dtype, on its device, without a gradient");
+  const int64_t tokens = k.size(0);
+  p.batch.tokens = size32(tokens);
+  const pahq_kv_rows vr = p.rows(v, tokens, p.cache.heads, "v: [tokens][cache heads][d_head] of the cache's dtype, on its device, without a gradient");
+  const int64_t* positions = nullptr;
+  const uint64_t* table = nullptr;
+  int64_t pairs = 0;
+  if (a[7] != Py_None) {
+    const Tensor& t = tensor(a[7], "positions: a tensor");
+    need(t.scalar_type() == at::kLong && t.dim() == 1 && t.size(0) == tokens && on(t, p.device) && t.is_contiguous(),
+         "positions: int64 [tokens], contiguous, on the cache's device");
+    positions = (const int64_t*)t.data_ptr();
+  }
+  if (a[8] != Py_None) {
+    const Tensor& t = tensor(a[8], "table: a tensor");
+    need(t.scalar_type() == at::kLong && t.dim() == 1 && on(t, p.device) && t.is_contiguous() && t.numel() >= 1 && 2 * t.numel() <= p.cache.d_head,
+         "table: from rotary_table, on the cache's device, for at most d_head elements");
+    table = (const uint64_t*)t.data_ptr();
+    pairs = t.numel();
+  }
+  const float magnitude = (float)real(a[10]);
+  Tensor out;
+  pahq_kv_rows qr = {}, outr = {};
+  int32_t q_heads = 0;
+  if (a[11] != Py_None) {
+    const Tensor& q = tensor(a[11], "q: a tensor");
+    qr = p.rows(q, tokens, 0, "q: [tokens][heads][d_head] of the cache's dtype, on its device, without a gradient");
+    q_heads = size32(q.size(1));
+    out = a[12] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(a[12], "out: a tensor");
+    outr = p.rows(out, tokens, q_heads, "out: of q's shape and dtype, on its device, without a gradient");
+  } else {
+    need(a[12] == Py_None, "out: for q only");
+  }
+  if (tokens && p.batch.batch) {
+    const On current(p.device);
+    const int rc = pahq_kv_append(current.stream, &p.cache, &p.batch, &kr, &vr, positions, table, (int32_t)(2 * pairs), (int32_t)number(a[9]), magnitude,
+                                  q_heads ? &qr : nullptr, q_heads, q_heads ? &outr : nullptr);
+    if (rc) return PyLong_FromLong(rc);
+    written(p.keys);
+    written(p.values);
+    if (q_heads) written(out);
+  }
+  if (!q_heads) Py_RETURN_NONE;
+  return THPVariable_Wrap(out);
+}
+
+// (keys, values, starts, lengths, pages, q, tree, scale, out)
+PyObject* kv_attention(PyObject* const* a) {
+  Paged p(a, true);
+  const Tensor& q = tensor(a[5], "q: a tensor");
+  const pahq_kv_rows qr = p.rows(q, -1, 0, "q: [tokens][heads][d_head] of the cache's dtype, on its device, without a gradient");
+  const int64_t tokens = q.size(0), heads = q.size(1);
+  need(heads % p.cache.heads == 0, "q: a multiple of the cache's heads");
+  p.batch.tokens = size32(tokens);
+  const uint64_t* tree = nullptr;
+  int32_t words = 0;
+  if (a[6] != Py_None) {
+    const Tensor& t = tensor(a[6], "tree: a tensor");
+    need(t.scalar_type() == at::kLong && t.dim() == 2 && t.size(0) == tokens && t.size(1) >= 1 && on(t, p.device) && t.is_contiguous(),
+         "tree: int64 [tokens][words], contiguous, on the cache's device");
+    tree = (const uint64_t*)t.data_ptr();
+    words = size32(t.size(1));
+  }
+  const float scale = a[7] == Py_None ? (float)(1.0 / std::sqrt((double)p.cache.d_head)) : (float)real(a[7]);
+  const Tensor out = a[8] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(a[8], "out: a tensor");
+  const pahq_kv_rows outr = p.rows(out, tokens, heads, "out: of q's shape and dtype, on its device, without a gradient");
+  if (tokens && p.batch.batch) {
+    const On current(p.device);
+    size_t bytes = 0;
+    int rc = pahq_kv_attention_workspace(&p.cache, &p.batch, size32(heads), &bytes);
+    if (rc) return PyLong_FromLong(rc);
+    Tensor space;
+    if (bytes) space = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
+    rc = pahq_kv_attention(current.stream, &p.cache, &p.batch, &qr, size32(heads), tree, words, scale, &outr, bytes ? space.data_ptr() : nullptr, bytes);
+    if (rc) return PyLong_FromLong(rc);
+    written(out);
+  }
+  return THPVariable_Wrap(out);
+}
+
+// (keys, values, starts, lengths, pages, paths, out)
+PyObject* kv_keep(PyObject* const* a) {
+  Paged p(a, false);
+  const int64_t batch = p.batch.batch;
+  const Tensor& paths = tensor(a[5], "paths: a tensor");
+  need(paths.scalar_type() == at::kInt && paths.dim() == 2 && paths.size(0) == batch && on(paths, p.device) && paths.is_contiguous(),
+       "paths: int32 [batch][depth], contiguous, on the cache's device");
+  const Tensor out = a[6] == Py_None ? at::empty({batch}, paths.options()) : tensor(a[6], "out: a tensor");
+  need(out.scalar_type() == at::kInt && out.dim() == 1 && out.size(0) == batch && on(out, p.device) && out.is_contiguous(),
+       "out: int32 [batch], contiguous, on the cache's device");
+  p.batch.tokens = INT32_MAX;
+  if (batch) {
+    const On current(p.device);
+    const int rc = pahq_kv_keep(current.stream, &p.cache, &p.batch, (const int32_t*)paths.data_ptr(), size32(paths.size(1)), (int32_t*)out.data_ptr());
+    if (rc) return PyLong_FromLong(rc);
+    written(p.keys);
+    written(p.values);
     written(out);
   }
   return THPVariable_Wrap(out);
@@ -280,7 +433,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return nullptr;
 }
 #define ENTRY(f, n) {#f, (PyCFunction)(void (*)())entry<f, n>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ENTRY(mx4_quantize, 3), ENTRY(mx4_dequantize, 3), ENTRY(mx4_gemm, 6), ENTRY(rotary, 7), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {ENTRY(mx4_quantize, 3), ENTRY(mx4_dequantize, 3), ENTRY(mx4_gemm, 6), ENTRY(rotary, 7),
+                         ENTRY(kv_append, 13), ENTRY(kv_attention, 9), ENTRY(kv_keep, 7), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 }  // namespace
 

@@ -1,5 +1,5 @@
 """The library's operators on device tensors (include/pahq.h, the section of that name) with torch tensors: matrices
-in 4 microscaled bits and their product, and rotary positions.
+in 4 microscaled bits and their product, rotary positions, and a paged cache of keys and values with the attention that reads it.
 
 Every call enqueues on the current stream of its tensors' device (whichever device is current) and does not wait.  Results are
 new tensors unless `out` is given.  Strided tensors are taken as they are where the C functions can walk them and refused
@@ -11,7 +11,7 @@ import numpy as np
 import torch
 from torch.autograd import forward_ad
 
-from .binding import lib, _chk, rotary_entries
+from .binding import lib, _chk, rotary_entries, tree_words
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _LAYOUTS = {"half": 0, "interleaved": 1}
@@ -185,3 +185,76 @@ def rotary(x, positions, table, layout="half", magnitude=1.0, inverse=False, out
         _need(out is None, "out: not where a gradient is recorded")
         return _Rotary.apply(x, positions, table, _LAYOUTS[layout], float(magnitude), bool(inverse))
     return _rotary(x, positions, table, _LAYOUTS[layout], magnitude, bool(inverse), out)
+
+
+class KvCache:
+    """A paged cache: `keys` and `values`, tensors [pages][heads][page_size][d_head] of float32, bfloat16 or float16 with the same strides, in any
+    order in memory (permuted views, or the two halves of one tensor), elements of a row contiguous, everything else in whole 16
+    bytes.  d_head: a multiple of 8 up to 256."""
+
+    __slots__ = ("keys", "values")
+
+    def __init__(self, keys, values):
+        _need(keys.dim() == 4 and keys.shape == values.shape and keys.dtype == values.dtype and keys.dtype in _DTYPES
+              and keys.device == values.device, "keys and values: [pages][heads][page_size][d_head] of one dtype, on one device")
+        self.keys, self.values = keys, values
+
+    @classmethod
+    def empty(cls, pages, page_size, heads, d_head, dtype=torch.bfloat16, device="cuda"):
+        """Memory for a cache: what it holds is not set."""
+        both = torch.empty(2, pages, heads, page_size, d_head, dtype=dtype, device=device)
+        return cls(both[0], both[1])
+
+
+class KvBatch:
+    """The sequences of a call, int32 tensors on the cache's device: `starts` [batch + 1], sequence b's new tokens being rows starts[b] to
+    starts[b + 1] - 1 of the operators' rows; `lengths` [batch], the new tokens included, which are a sequence's last; `pages` [batch][width],
+    each sequence's pages in order.  Row j of a sequence is row j % page_size of its page j // page_size.  The tensors are read when a
+    call's kernels run, so a captured graph finds what they hold when it is replayed."""
+
+    __slots__ = ("starts", "lengths", "pages")
+
+    def __init__(self, starts, lengths, pages):
+        _need(starts.dtype == lengths.dtype == pages.dtype == torch.int32 and starts.device == lengths.device == pages.device
+              and starts.dim() == lengths.dim() == 1 and pages.dim() == 2 and len(starts) == len(lengths) + 1 and len(pages) == len(lengths),
+              "starts [batch + 1], lengths [batch], pages [batch][width]: int32, on one device")
+        self.starts, self.lengths, self.pages = starts, lengths, pages
+
+
+def kv_append(cache, batch, k, v, positions=None, table=None, layout="half", magnitude=1.0, q=None, out=None):
+    """Writes new tokens' rows into their sequences' pages: k [tokens][cache heads][d_head] turned as `rotary` turns it (table None: as it is),
+    v as it is.  positions: int64 [tokens], or None for the tokens' rows in their sequences.  q [tokens][heads][d_head], if given, is
+    turned the same way and returned (in `out`, which may be q).  Rows of tokens that belong to no sequence are not written."""
+    if layout not in _LAYOUTS:
+        raise ValueError("layout: 'half' or 'interleaved'")
+    got = _ext.kv_append(cache.keys, cache.values, batch.starts, batch.lengths, batch.pages, k, v, positions, table, _LAYOUTS[layout], magnitude, q, out)
+    if type(got) is int:
+        _chk(got, "pahq_kv_append")
+    return got
+
+
+def tree_bits(parents, device="cuda"):
+    """The masks `kv_attention` takes for a drafted tree, int64 [nodes][words] (bit patterns): every node sees itself and its ancestors.
+    parents: each node's parent, which comes before it, -1 at a root.  Trees of a batch are joined below each other (torch.cat; of
+    as many words)."""
+    return torch.from_numpy(tree_words(parents).view(np.int64)).to(device)
+
+
+def kv_attention(q, cache, batch, tree=None, scale=None, out=None):
+    """Attention of the new tokens' queries q [tokens][heads][d_head] over their sequences' rows in the cache, whose heads go with heads / cache
+    heads query heads each: a token sees the rows in front of the new ones, and of the new ones those up to itself, or those that
+    its row of `tree` names (int64 [tokens][words], bit j % 64 of word j // 64 for new token j of its sequence).  scale: of the
+    products, d_head ** -0.5 unless given.  A query that sees nothing gets zeros.  out may be q; rows of tokens that belong to no sequence are not written."""
+    got = _ext.kv_attention(cache.keys, cache.values, batch.starts, batch.lengths, batch.pages, q, tree, scale, out)
+    if type(got) is int:
+        _chk(got, "pahq_kv_attention")
+    return got
+
+
+def kv_keep(cache, batch, paths, out=None):
+    """Of each sequence's new tokens those that its row of paths (int32 [batch][depth], growing, -1 behind the last) names stay: their rows move
+    together behind the ones in front of the new ones.  Returns the new lengths, int32 [batch] (in `out`, not the batch's own)."""
+    got = _ext.kv_keep(cache.keys, cache.values, batch.starts, batch.lengths, batch.pages, paths, out)
+    if type(got) is int:
+        _chk(got, "pahq_kv_keep")
+    return got
