@@ -1,11 +1,23 @@
 // Attention of new tokens over a paged cache (the definition is in include/pahq.h).
+//
+// Both kernels work on transposed products: S^T = K Q^T and O^T = V^T P^T.  The matrix instruction leaves of S^T in a lane one row
+// of queries and several rows of the cache, so a softmax row's maximum and sum stay in a lane but for an exchange or two, and the
+// weights P are, as they lie in the registers, the right operand of the second product, if V's rows are taken in the
+// same order: rows 4 h .. 4 h + 3 of every eight (or sixteen) for lane group h.  LDS reads that transpose (DS_READ_B64_TR_B16) give V that way.
+// Rows of the cache reach LDS without registers (global_load_lds), each 16 bytes a lane at an address of its own, which is what pages
+// need; their 16-byte chunks are XOR-swizzled by the row so that both products' reads spread over the banks.  What lies behind a
+// sequence's end comes from a chunk of zeros, what lies in a page that is none from a chunk of NaN.
 #include <hip/hip_runtime.h>
-#include <math.h>
 #include <stdint.h>
 #include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <type_traits>
 #include "../../include/pahq.h"
 #include "device_util.h"
+#include "mma_util.h"
 #include "kv.h"
+#include "kv_plan.h"
 
 namespace pahq {
 
@@ -15,56 +27,709 @@ struct AttendArgs {
   KvRows q, out;
   const unsigned long long* tree;
   int words, group;                                 // group: query heads of a cache head
-  float scale;                                      // times log2 e
+  float scale, sign;                                // of the scores: times log2 e and positive; of the queries: its sign, 0 for a scale of 0
+  float* part;                                      // [slot][rows][d] sums of pieces, then [slot][rows][2] maximum and sum
+  int slots, least;                                 // of pieces (kv_plan.h); slots 0: nothing is cut
 };
 
-// A workgroup takes a query head of a token, a wave every fourth row it sees, each with a running maximum and sum; the
-// four meet in LDS.
-template <typename T>
-__global__ __launch_bounds__(256) void kv_attend_k(AttendArgs a) {
-  __shared__ float part[4][PAHQ_KV_MAX_HEAD + 2];
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = a.c.d;
-  const int b = kv_owner(a.b.batch, t, [&](int i) { return kv_start(a.b, i); });
-  if (b < 0 || b >= a.b.batch) return;
-  const KvSequence s = kv_sequence(a.b, b);
-  if (t >= s.t0 + s.n) return;
-  const T* const q = (const T*)(a.q.at + t * a.q.token + h * a.q.head);
-  const long long head = (long long)(h / a.group) * a.c.head;
-  float x[4], o[4] = {0, 0, 0, 0}, m = -INFINITY, l = 0.f;
-  for (int e = 0; e < 4; e++) x[e] = lane * 4 + e < d ? as_float(q[lane * 4 + e]) : 0.f;
-  for (int j = wave; j < s.length; j += 4) {
-    const int ahead = j - s.base;
-    if (ahead >= 0) {
-      if (!a.tree && ahead > t - s.t0) break;
-      if (a.tree && (ahead >= 64ll * a.words || !(a.tree[(long long)t * a.words + ahead / 64] >> (ahead & 63) & 1))) continue;
+// ---------------------------------------------------------------- a workgroup's part
+struct Item {
+  KvSequence s;
+  int b, tile, tiles, piece, pieces, from;          // from: the tile's first slot in the workspace (pieces > 1)
+  int size;                                         // rows of the cache a piece
+};
+__device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+__device__ __forceinline__ int wave_sum_before(int v) {       // of the lanes in front
+  int s = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(s, o, 64);
+    if ((int)(threadIdx.x & 63) >= o) s += u;
+  }
+  return s - v;
+}
+// Every wave finds it by itself, 64 sequences at a time.  by_tile: the index counts tiles and not pieces.  false: no such item.
+template <int UNIT>
+__device__ bool find_item(const AttendArgs& a, int rows, int index, bool by_tile, Item* it) {
+  const int lane = threadIdx.x & 63, rounds = (a.b.batch + 63) / 64;
+  KvSequence s = {};
+  int tiles = 0, size = KV_MAX_LENGTH;
+  auto look = [&](int r) {
+    const int b = r * 64 + lane;
+    tiles = 0;
+    if (b < a.b.batch) {
+      s = kv_sequence(a.b, b);
+      tiles = kv_tiles((long long)s.n * a.group, rows);
     }
-    const long long row = kv_row(a.c, a.b.pages + b * a.b.ld, j);
-    float y = 0.f, v[4] = {0, 0, 0, 0};
-    for (int e = 0; e < 4; e++)
-      if (lane * 4 + e < d) {
-        y += row < 0 ? NAN : x[e] * as_float(((const T*)(a.c.keys + row + head))[lane * 4 + e]);
-        v[e] = row < 0 ? NAN : as_float(((const T*)(a.c.values + row + head))[lane * 4 + e]);
+  };
+  if (rounds == 1) look(0);
+  if (a.slots) {
+    double work = 0, all = 0;                       // sums that no batch can overflow
+    for (int r = 0; r < rounds; r++) {
+      if (rounds > 1) look(r);
+      work += tiles ? (double)tiles * s.length : 0;
+      all += tiles;
+    }
+    size = __builtin_amdgcn_readfirstlane(kv_first_piece(wave_sum_d(work) * a.c.heads, a.slots, UNIT, a.least));
+    if (__builtin_amdgcn_readfirstlane(wave_sum_d(all) * a.c.heads * 2 <= a.slots))
+      for (int guess = 0; guess < KV_GUESSES; guess++) {
+        all = 0;
+        for (int r = 0; r < rounds; r++) {
+          if (rounds > 1) look(r);
+          all += tiles ? (double)tiles * kv_pieces(s.length, size) : 0;
+        }
+        if (__builtin_amdgcn_readfirstlane(wave_sum_d(all) * a.c.heads <= a.slots)) break;
+        size = kv_longer_piece(size, UNIT);
       }
-    y = wave_sum(y) * a.scale;
-    const float top = fmaxf(m, y);
-    if (top == -INFINITY && y == y) continue;       // nothing so far weighs anything
-    const float keep = exp2f(m - top), p = exp2f(y - top);
-    m = top;
-    l = l * keep + p;
-    for (int e = 0; e < 4; e++) o[e] = o[e] * keep + p * v[e];
   }
-  for (int e = 0; e < 4; e++) part[wave][lane * 4 + e] = o[e];
-  if (lane == 0) part[wave][PAHQ_KV_MAX_HEAD] = m, part[wave][PAHQ_KV_MAX_HEAD + 1] = l;
+  int before = 0, cut_before = 0;
+  for (int r = 0; r < rounds; r++) {
+    if (rounds > 1) look(r);
+    // starts that do not grow can name more items than a launch has workgroups: no sum of theirs may pass 31 bits
+    const int pieces = tiles ? kv_pieces(s.length, size) : 0, items = (int)min((long long)tiles * pieces, (long long)KV_MOST_ITEMS);
+    const int count = by_tile ? min(tiles, KV_MOST_ITEMS) : items, cut = pieces > 1 ? items : 0;
+    const int at = before + wave_sum_before(count), slot = cut_before + wave_sum_before(cut);
+    const unsigned long long mine = __ballot(index >= at && index < at + count);
+    if (mine) {
+      const int l = __builtin_ctzll(mine);
+      it->b = r * 64 + l;
+      it->s = {lane_of(s.t0, l), lane_of(s.n, l), lane_of(s.length, l), lane_of(s.base, l)};
+      it->tiles = lane_of(tiles, l);
+      it->pieces = lane_of(pieces, l);
+      it->size = size;
+      const int local = index - lane_of(at, l);
+      // the last tiles see the most rows of the cache and come first
+      it->tile = it->tiles - 1 - (by_tile ? local : local / it->pieces);
+      it->piece = by_tile ? 0 : local % it->pieces;
+      it->from = lane_of(slot, l) + (it->tiles - 1 - it->tile) * it->pieces;
+      return true;
+    }
+    before = min(lane_of(at + count, 63), 1 << 29);
+    cut_before = min(lane_of(slot + cut, 63), 1 << 29);
+  }
+  return false;
+}
+// How many rows of the cache a tile sees at most
+__device__ __forceinline__ int tile_end(const AttendArgs& a, const Item& it, int rows) {
+  if (a.tree) return it.s.length;
+  const int last = min(it.s.n - 1, (int)((((long long)it.tile + 1) * rows - 1) / a.group));
+  return max(it.s.base + last + 1, 0);
+}
+// The rows of the cache of a piece of a tile; false: none, and nothing to write
+__device__ __forceinline__ bool piece_rows(const AttendArgs& a, const Item& it, int rows, int* begin, int* end) {
+  *begin = 0;
+  *end = tile_end(a, it, rows);
+  if (it.pieces <= 1) return true;
+  const long long from = (long long)it.piece * it.size;
+  if (from >= *end && it.piece) return false;       // the first one runs even if it sees nothing
+  *begin = (int)from;
+  *end = (int)min((long long)*end, from + it.size);
+  return true;
+}
+// Bit x: whether new token i (row t of the operator's) sees row k0 + x of the cache
+__device__ __forceinline__ unsigned long long seen_bits(const AttendArgs& a, const KvSequence& s, int i, int k0, int end) {
+  auto low = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
+  if (!a.tree) return low(min(s.base + i + 1, end) - k0);
+  unsigned long long m = low(s.base - k0);
+  const int ahead = k0 - s.base, word = ahead >> 6, shift = ahead & 63;            // rounded down
+  const unsigned long long* const w = a.tree + (long long)(s.t0 + i) * a.words;
+  if (word >= 0 && word < a.words) m |= w[word] >> shift;
+  if (shift && word + 1 >= 0 && word + 1 < a.words) m |= w[word + 1] << (64 - shift);
+  return m & low(end - k0);
+}
+
+// ---------------------------------------------------------------- fragments
+// Sixteen bytes of a row are one operand of a step of the 16-bit products and of four steps of the fp32 products
+template <typename T> struct Frag;
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+template <> struct Frag<bf16_t> {
+  typedef v8bf type;
+  static __device__ __forceinline__ v4f mma16(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ v16f mma32(v8bf a, v8bf b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Frag<f16_t> {
+  typedef v8h type;
+  static __device__ __forceinline__ v4f mma16(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ v16f mma32(v8h a, v8h b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Frag<float> {
+  typedef v4f type;
+  static __device__ __forceinline__ v4f mma16(v4f a, v4f b, v4f c) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ v16f mma32(v4f a, v4f b, v16f c) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+};
+// fp16 weights: times 2^7, so that those 2^-21 of the largest are still normal numbers, and 2^15 is the largest (the maximum lags by up to 2^8)
+template <typename T> constexpr float LIFT = sizeof(T) == 2 && !__is_same(T, bf16_t) ? 7.f : 0.f;
+constexpr float LAG = 8.f;
+
+alignas(16) __device__ const uint32_t kv_chunk[4][4] = {{0, 0, 0, 0}, {0x7FC00000, 0x7FC00000, 0x7FC00000, 0x7FC00000},
+                                                        {0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0}, {0x7E007E00, 0x7E007E00, 0x7E007E00, 0x7E007E00}};
+template <typename T> constexpr int NAN_CHUNK = sizeof(T) == 4 ? 1 : __is_same(T, bf16_t) ? 2 : 3;
+
+// Where chunk c of a row lies among the row's CH chunks.  Rows 4 apart in the low bits, so that four rows' 64 neighbouring bytes (what a
+// transposing read takes) lie in different quarters of the 64 banks, and so do one chunk of sixteen rows (what K's reads take).
+template <int CH> __device__ __forceinline__ int swizzle(int row) {
+  static_assert(CH >= 8, "rows of 128 bytes and more");
+  return CH >= 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
+}
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Rows of the cache on their way into LDS.  A lane keeps where its row of a block lies; the pages' numbers came through LDS themselves
+// (`ids`, asked for two blocks ahead), because a load into a register would make the compiler wait for everything in flight.
+constexpr long long ROW_BEHIND = -2, ROW_NONE = -1;
+__device__ __forceinline__ void ask_page(const KvCache& c, const int* pages, int row, int end, uint32_t lds) {
+  const int j = max(min(row, end - 1), 0);
+  lds_load4(pages + (int)((unsigned long long)(uint32_t)j * c.magic >> c.shift), lds);
+}
+__device__ __forceinline__ long long row_at(const KvCache& c, int row, int end, int page) {
+  if (row >= end) return ROW_BEHIND;
+  const int slot = row - (int)((unsigned long long)(uint32_t)row * c.magic >> c.shift) * c.page_size;
+  return (uint32_t)page < (uint32_t)c.pages ? page * c.page + slot * c.slot : ROW_NONE;
+}
+// Rows r0 .. of the block, 64 / CH of them, chunk by chunk: lane l writes the l-th 16 bytes behind lds.  `of` rows' offsets lie in
+// lanes `first` and on.
+template <typename T, int CH>
+__device__ __forceinline__ void ask_rows(const KvCache& c, long long head, long long mine, int first, int r0, uint32_t lds_k, uint32_t lds_v) {
+  const int lane = threadIdx.x & 63, r = lane / CH, p = lane % CH;
+  const int chunk = p ^ swizzle<CH>(r0 + r);
+  const long long at = (long long)__shfl((unsigned long long)mine, first + r, 64);
+  const char *k = c.keys + head + at + chunk * 16, *v = c.values + head + at + chunk * 16;
+  const bool none = at == ROW_NONE, zero = at == ROW_BEHIND || chunk * 16 >= c.d * (int)sizeof(T);
+  if (none || zero) k = v = (const char*)kv_chunk[zero ? 0 : NAN_CHUNK<T>];
+  slab_load16((const uint8_t*)k, lds_k);
+  slab_load16((const uint8_t*)v, lds_v);
+}
+
+// Values that some query of the tile does not see may be infinities or NaN, and 0 * NaN is one: they leave the product and come back
+// as how many of each kind a query sees.
+template <typename T, typename F> __device__ __forceinline__ bool not_finite(F v) {
+  constexpr int N = 16 / sizeof(T);
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < N; j++) bad |= !(fabsf((float)v[j]) < INFINITY);
+  return bad;
+}
+
+// ---------------------------------------------------------------- up to 16 RT rows of queries
+// A wave takes blocks of KVB rows of the cache in turn with the others of its workgroup, into two stages of LDS of its own, so nothing waits for
+// another wave until the waves' sums meet at the end.  Bound by memory: every row of the cache is read once a tile.
+template <typename T, int D, int RT, int NW>
+__global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
+  typedef typename Frag<T>::type F;
+  constexpr int EB = sizeof(T), CH = D * EB / 16, KT = EB == 2 ? 2 : 1, KVB = 16 * KT, ROWS = 16 * RT;
+  constexpr int HALF = KVB * D * EB, STAGE = 2 * HALF, ASKS = HALF / 1024, DT = D / 16;
+  static_assert(2 * STAGE >= ROWS * D * 4 && 2 * ASKS + 1 < 64, "the waves' sums fit their stages");
+  extern __shared__ __align__(16) char lds[];       // [NW][2][STAGE], [NW][4][64] pages' numbers
+  __shared__ float stat[NW][ROWS][2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, h4 = lane >> 4;
+  const int h = blockIdx.x % a.c.heads;
+  Item it;
+  if (!find_item<KVB * NW>(a, ROWS, blockIdx.x / a.c.heads, false, &it)) return;
+  int begin, end;
+  if (!piece_rows(a, it, ROWS, &begin, &end)) return;
+
+  // the tile's queries: lane l16 of row tile r holds chunks h4, h4 + 4, ... of row 16 r + l16
+  int token[RT];
+  F q[RT][CH / 4];
+#pragma unroll
+  for (int r = 0; r < RT; r++) {
+    const long long row = (long long)it.tile * ROWS + 16 * r + l16;
+    const bool there = row < (long long)it.s.n * a.group;
+    token[r] = there ? (int)(row / a.group) : -1;
+    const int g = (int)(row - (long long)(there ? token[r] : 0) * a.group);
+    const T* const x = (const T*)(a.q.at + (it.s.t0 + (there ? token[r] : 0)) * a.q.token + (h * a.group + (there ? g : 0)) * a.q.head);
+#pragma unroll
+    for (int s = 0; s < CH / 4; s++) {
+      const int e0 = (h4 + 4 * s) * (16 / EB);
+      Pack<T, 16 / EB> p = {};
+      if (there && e0 < a.c.d) p = *(const Pack<T, 16 / EB>*)(x + e0);
+#pragma unroll
+      for (int j = 0; j < 16 / EB; j++) q[r][s][j] = from_float<T>(as_float(p.v[j]) * a.sign);
+    }
+  }
+
+  const int* const pages = a.b.pages + it.b * a.b.ld;
+  const long long head = h * a.c.head;
+  char* const mine = lds + wave * 2 * STAGE;
+  const uint32_t stage0 = __builtin_amdgcn_readfirstlane(lds_addr_of(mine));
+  int* const ids = (int*)(lds + NW * 2 * STAGE) + wave * 4 * 64;
+  const uint32_t ids0 = __builtin_amdgcn_readfirstlane(lds_addr_of(ids));
+  const int blocks = end > begin ? (end - begin + KVB - 1) / KVB : 0, turns = blocks > wave ? (blocks - wave + NW - 1) / NW : 0;
+  auto first_row = [&](int n) { return begin + (wave + n * NW) * KVB; };
+  auto ask_ids = [&](int n) { ask_page(a.c, pages, first_row(n) + (lane & (KVB - 1)), end, ids0 + (n & 3) * 256); };
+  auto ask_block = [&](int n) {
+    const long long at = row_at(a.c, first_row(n) + (lane & (KVB - 1)), end, ids[(n & 3) * 64 + lane]);
+    const uint32_t to = stage0 + (n & 1) * STAGE;
+#pragma unroll
+    for (int j = 0; j < ASKS; j++) ask_rows<T, CH>(a.c, head, at, j * (64 / CH), j * (64 / CH), to + j * 1024, to + HALF + j * 1024);
+  };
+  v4f o[RT][DT] = {};
+  float m[RT], l[RT];
+#pragma unroll
+  for (int r = 0; r < RT; r++) m[r] = -INFINITY, l[r] = 0.f;
+
+  if (turns) {
+    ask_ids(0);
+    ask_ids(1);
+    ask_ids(2);
+    wait_vm_lds<0>();
+    ask_block(0);
+  }
+  auto block = [&](int n, auto is_masked) {
+    constexpr bool masked = decltype(is_masked)::value;
+    const int k0 = first_row(n);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // the stage's last reads
+    if (n + 1 < turns) {
+      ask_ids(n + 3);                                            // a place in the list is asked for even behind the last block
+      ask_block(n + 1);
+      wait_vm_lds<2 * ASKS + 1>();
+    } else {
+      wait_vm_lds<0>();
+    }
+    const char* const ks = mine + (n & 1) * STAGE;
+    v4f s[RT][KT];
+#pragma unroll
+    for (int t = 0; t < KT; t++) {
+#pragma unroll
+      for (int r = 0; r < RT; r++) s[r][t] = (v4f){0, 0, 0, 0};
+      const int row = 16 * t + l16;
+#pragma unroll
+      for (int c = 0; c < CH / 4; c++) {
+        const F k = *(const F*)(ks + row * (D * EB) + (((h4 + 4 * c) ^ swizzle<CH>(row)) * 16));
+#pragma unroll
+        for (int r = 0; r < RT; r++) s[r][t] = Frag<T>::mma16(k, q[r][c], s[r][t]);
+      }
+    }
+    unsigned long long seen[RT];
+    float p[RT][KT][4];
+#pragma unroll
+    for (int r = 0; r < RT; r++) {
+      if (masked) seen[r] = token[r] < 0 ? 0ull : seen_bits(a, it.s, token[r], k0, end);
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < KT; t++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          float x = s[r][t][i] * a.scale;
+          if (masked && !(seen[r] >> (16 * t + 4 * h4 + i) & 1)) x = -INFINITY;
+          p[r][t][i] = x;
+          top = fmaxf(top, x);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const bool more = top > m[r] + LAG;                        // of this row alone: its neighbours' scores change nothing in it
+      if (__any(more)) {
+        const float f = more ? __builtin_amdgcn_exp2f(m[r] - top) : 1.f;
+        if (more) m[r] = top;
+        l[r] *= f;
+#pragma unroll
+        for (int d = 0; d < DT; d++) o[r][d] *= f;
+      }
+      const float from = (m[r] == -INFINITY ? 0.f : m[r]) - LIFT<T>;
+#pragma unroll
+      for (int t = 0; t < KT; t++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          p[r][t][i] = __builtin_amdgcn_exp2f(p[r][t][i] - from);
+          l[r] += p[r][t][i];
+        }
+    }
+    const char* const vs = ks + HALF;
+    if constexpr (EB == 2) {
+      F w[RT];
+#pragma unroll
+      for (int r = 0; r < RT; r++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) w[r][j] = (T)p[r][j / 4][j % 4];
+#pragma unroll
+      for (int d = 0; d < DT; d++) {
+        union { F f; v4s half[2]; } v;
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+          const int row = 16 * t + 4 * h4 + l16 / 4, chunk = 2 * d + (l16 & 3) / 2;
+          v.half[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(lds_char*)(
+              vs + row * (D * EB) + ((chunk ^ swizzle<CH>(row)) * 16) + (l16 & 1) * 8));
+        }
+        if (masked && __any(not_finite<T>(v.f))) {
+          F up, down, no;
+#pragma unroll
+          for (int j = 0; j < 8; j++) {
+            const float x = (float)v.f[j];
+            up[j] = (T)(x == INFINITY ? 1.f : 0.f);
+            down[j] = (T)(x == -INFINITY ? 1.f : 0.f);
+            no[j] = (T)(x != x ? 1.f : 0.f);
+            if (!(fabsf(x) < INFINITY)) v.f[j] = (T)0.f;
+          }
+#pragma unroll
+          for (int r = 0; r < RT; r++) {
+            F one;
+#pragma unroll
+            for (int j = 0; j < 8; j++) one[j] = (T)(seen[r] >> (16 * (j / 4) + 4 * h4 + j % 4) & 1 ? 1.f : 0.f);
+            const v4f zero = {0, 0, 0, 0}, u = Frag<T>::mma16(up, one, zero), n = Frag<T>::mma16(down, one, zero), x = Frag<T>::mma16(no, one, zero);
+#pragma unroll
+            for (int i = 0; i < 4; i++) o[r][d][i] += (u[i] > 0.f ? INFINITY : 0.f) - (n[i] > 0.f ? INFINITY : 0.f) + (x[i] > 0.f ? NAN : 0.f);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; r++) o[r][d] = Frag<T>::mma16(v.f, w[r], o[r][d]);
+      }
+    } else {
+#pragma unroll
+      for (int d = 0; d < DT; d++) {
+        F v;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const int row = 4 * h4 + i, chunk = 4 * d + l16 / 4;
+          v[i] = *(const float*)(vs + row * (D * EB) + ((chunk ^ swizzle<CH>(row)) * 16) + (l16 & 3) * 4);
+        }
+        if (masked && __any(not_finite<T>(v))) {
+          F up, down, no;
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            up[i] = v[i] == INFINITY ? 1.f : 0.f;
+            down[i] = v[i] == -INFINITY ? 1.f : 0.f;
+            no[i] = v[i] != v[i] ? 1.f : 0.f;
+            if (!(fabsf(v[i]) < INFINITY)) v[i] = 0.f;
+          }
+#pragma unroll
+          for (int r = 0; r < RT; r++) {
+            F one;
+#pragma unroll
+            for (int i = 0; i < 4; i++) one[i] = seen[r] >> (4 * h4 + i) & 1 ? 1.f : 0.f;
+            const v4f zero = {0, 0, 0, 0}, u = Frag<T>::mma16(up, one, zero), n = Frag<T>::mma16(down, one, zero), x = Frag<T>::mma16(no, one, zero);
+#pragma unroll
+            for (int i = 0; i < 4; i++) o[r][d][i] += (u[i] > 0.f ? INFINITY : 0.f) - (n[i] > 0.f ? INFINITY : 0.f) + (x[i] > 0.f ? NAN : 0.f);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; r++) o[r][d] = Frag<T>::mma16(v, (F){p[r][0][0], p[r][0][1], p[r][0][2], p[r][0][3]}, o[r][d]);
+      }
+    }
+  };
+  // blocks that every query of the tile sees whole come first
+  const int sure = min(end, it.s.base + (a.tree ? 0 : (int)((long long)it.tile * ROWS / a.group) + 1));
+  int n = 0;
+  for (; n < turns && first_row(n) + KVB <= sure; n++) block(n, std::false_type());
+  for (; n < turns; n++) block(n, std::true_type());
+
+  // the waves' sums: [row][d] in the wave's stages, chunks of four swizzled by the row
+#pragma unroll
+  for (int r = 0; r < RT; r++) {
+    l[r] += __shfl_xor(l[r], 16, 64);
+    l[r] += __shfl_xor(l[r], 32, 64);
+    const int row = 16 * r + l16;
+    if (h4 == 0) stat[wave][row][0] = m[r], stat[wave][row][1] = l[r];
+#pragma unroll
+    for (int d = 0; d < DT; d++) *(v4f*)(mine + row * (D * 4) + (((4 * d + h4) ^ (row & 15)) * 16)) = o[r][d];
+  }
   __syncthreads();
-  float top = -INFINITY, sum = 0.f, y = 0.f;
-  for (int w = 0; w < 4; w++) top = fmaxf(top, part[w][PAHQ_KV_MAX_HEAD]);
-  if (top == -INFINITY) top = 0.f;
-  for (int w = 0; w < 4; w++) {
-    const float f = exp2f(part[w][PAHQ_KV_MAX_HEAD] - top);
-    sum += f * part[w][PAHQ_KV_MAX_HEAD + 1];
-    y += f * part[w][threadIdx.x];
+  for (int e = threadIdx.x; e < ROWS * (D / 4); e += NW * 64) {
+    const int row = e / (D / 4), c = e % (D / 4);
+    const long long of = (long long)it.tile * ROWS + row;
+    if (of >= (long long)it.s.n * a.group || c * 4 >= a.c.d) continue;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; w++) top = fmaxf(top, stat[w][row][0]);
+    v4f y = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < NW; w++) {
+      const float f = __builtin_amdgcn_exp2f(stat[w][row][0] - (top == -INFINITY ? 0.f : top));
+      sum += f * stat[w][row][1];
+      y += f * *(const v4f*)(lds + w * 2 * STAGE + row * (D * 4) + ((c ^ (row & 15)) * 16));
+    }
+    if (it.pieces > 1) {
+      const long long slot = (long long)(it.from + it.piece) * a.c.heads + h;
+      *(v4f*)(a.part + (slot * ROWS + row) * a.c.d + c * 4) = y;
+      float* const st = a.part + 2ll * a.slots * ROWS * a.c.d + (slot * ROWS + row) * 2;
+      if (c == 0) st[0] = top, st[1] = sum;
+    } else {
+      const int i = (int)(of / a.group), g = (int)(of - (long long)i * a.group);
+      Pack<T, 4> z;
+#pragma unroll
+      for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(sum == 0.f ? 0.f : y[j] / sum);
+      *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + (it.s.t0 + i) * a.out.token + (h * a.group + g) * a.out.head) + c * 4) = z;
+    }
   }
-  if ((int)threadIdx.x < d) ((T*)(a.out.at + t * a.out.token + h * a.out.head))[threadIdx.x] = from_float<T>(sum == 0.f ? 0.f : y / sum);
+}
+
+// ---------------------------------------------------------------- many rows of queries
+// Four waves of 32 RT rows each share blocks of KVB rows of the cache, in two stages of LDS: a block's products run while the next one
+// arrives.
+template <typename T, int D, int RT, int KVB>
+__global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void kv_tile_k(AttendArgs a) {
+  typedef typename Frag<T>::type F;
+  constexpr int EB = sizeof(T), CH = D * EB / 16, KT = KVB / 32, NW = 4, ROWS = 32 * RT * NW;
+  constexpr int HALF = KVB * D * EB, STAGE = 2 * HALF, MINE = KVB / NW, ASKS = HALF / 1024 / NW, DT = D / 32;
+  static_assert(ASKS >= 1 && MINE * CH == ASKS * 64 && KVB <= 64, "a wave asks for whole rows");
+  extern __shared__ __align__(16) char lds[];       // [2][STAGE], [NW][2][64] pages' numbers
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h2 = lane >> 5;
+  const int h = blockIdx.x % a.c.heads;
+  Item it;
+  if (!find_item<KVB>(a, ROWS, blockIdx.x / a.c.heads, false, &it)) return;
+  int begin, end;
+  if (!piece_rows(a, it, ROWS, &begin, &end)) return;
+
+  // the wave's queries: lane l32 of row tile r holds chunks h2, h2 + 2, ... of row 32 r + l32
+  const long long row0 = (long long)it.tile * ROWS + wave * 32 * RT;
+  int token[RT];
+  F q[RT][CH / 2];
+#pragma unroll
+  for (int r = 0; r < RT; r++) {
+    const long long row = row0 + 32 * r + l32;
+    const bool there = row < (long long)it.s.n * a.group;
+    token[r] = there ? (int)(row / a.group) : -1;
+    const int g = (int)(row - (long long)(there ? token[r] : 0) * a.group);
+    const T* const x = (const T*)(a.q.at + (it.s.t0 + (there ? token[r] : 0)) * a.q.token + (h * a.group + (there ? g : 0)) * a.q.head);
+#pragma unroll
+    for (int s = 0; s < CH / 2; s++) {
+      const int e0 = (h2 + 2 * s) * (16 / EB);
+      Pack<T, 16 / EB> p = {};
+      if (there && e0 < a.c.d) p = *(const Pack<T, 16 / EB>*)(x + e0);
+#pragma unroll
+      for (int j = 0; j < 16 / EB; j++) q[r][s][j] = from_float<T>(as_float(p.v[j]) * a.sign);
+    }
+  }
+  // what the wave's rows see at least (unmasked) and at most: blocks behind the latter are left out
+  const int first = (int)(row0 / a.group), last = min(it.s.n - 1, (int)((row0 + 32 * RT - 1) / a.group));
+  const int sure = it.s.base + (a.tree ? 0 : first + 1);
+  const int wave_end = row0 >= (long long)it.s.n * a.group ? 0 : a.tree ? end : min(end, it.s.base + last + 1);
+
+  const int* const pages = a.b.pages + it.b * a.b.ld;
+  const long long head = h * a.c.head;
+  const uint32_t stage0 = __builtin_amdgcn_readfirstlane(lds_addr_of(lds));
+  int* const ids = (int*)(lds + 2 * STAGE) + wave * 2 * 64;
+  const uint32_t ids0 = __builtin_amdgcn_readfirstlane(lds_addr_of(ids));
+  const int blocks = (end - begin + KVB - 1) / KVB;
+  auto ask_ids = [&](int n) { ask_page(a.c, pages, begin + n * KVB + wave * MINE + (lane & (MINE - 1)), end, ids0 + (n & 1) * 256); };
+  auto ask_block = [&](int n) {
+    const long long at = row_at(a.c, begin + n * KVB + wave * MINE + (lane & (MINE - 1)), end, ids[(n & 1) * 64 + lane]);
+    const uint32_t to = stage0 + (n & 1) * STAGE + wave * ASKS * 1024;
+#pragma unroll
+    for (int j = 0; j < ASKS; j++) ask_rows<T, CH>(a.c, head, at, j * (64 / CH), wave * MINE + j * (64 / CH), to + j * 1024, to + HALF + j * 1024);
+  };
+  v16f o[RT][DT] = {};
+  float m[RT], l[RT];
+#pragma unroll
+  for (int r = 0; r < RT; r++) m[r] = -INFINITY, l[r] = 0.f;
+
+  if (blocks > 0) {
+    ask_ids(0);
+    wait_vm_lds<0>();
+    ask_block(0);
+    ask_ids(1);
+  }
+  auto block = [&](int n, auto is_masked) {
+    constexpr bool masked = decltype(is_masked)::value;
+    const int k0 = begin + n * KVB;
+    wait_vm_barrier<0>();
+    if (n + 1 < blocks) {
+      ask_block(n + 1);
+      ask_ids(n + 2);
+    }
+    if (masked && k0 >= wave_end) return;
+    const char* const ks = lds + (n & 1) * STAGE;
+    v16f s[RT][KT];
+#pragma unroll
+    for (int t = 0; t < KT; t++) {
+#pragma unroll
+      for (int r = 0; r < RT; r++) s[r][t] = (v16f){0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+      const int row = 32 * t + l32;
+#pragma unroll
+      for (int c = 0; c < CH / 2; c++) {
+        const F k = *(const F*)(ks + row * (D * EB) + (((h2 + 2 * c) ^ swizzle<CH>(row)) * 16));
+#pragma unroll
+        for (int r = 0; r < RT; r++) s[r][t] = Frag<T>::mma32(k, q[r][c], s[r][t]);
+      }
+    }
+    unsigned long long seen[RT];
+#pragma unroll
+    for (int r = 0; r < RT; r++) {
+      if (masked) {
+        seen[r] = token[r] < 0 ? 0ull : seen_bits(a, it.s, token[r], k0, end);
+        const unsigned long long mine = seen[r] >> (4 * h2);
+#pragma unroll
+        for (int t = 0; t < KT; t++)
+#pragma unroll
+          for (int i = 0; i < 16; i++)
+            if (!(mine >> (32 * t + 8 * (i / 4) + i % 4) & 1)) s[r][t][i] = -INFINITY;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < KT; t++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) top = fmaxf(top, s[r][t][i]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.scale;
+      const bool more = top > m[r] + LAG;                        // of this row alone: its neighbours' scores change nothing in it
+      if (__any(more)) {
+        const float f = more ? __builtin_amdgcn_exp2f(m[r] - top) : 1.f;
+        if (more) m[r] = top;
+        l[r] *= f;
+#pragma unroll
+        for (int d = 0; d < DT; d++) o[r][d] *= f;
+      }
+      const float from = LIFT<T> - (m[r] == -INFINITY ? 0.f : m[r]);
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < KT; t++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+          s[r][t][i] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r][t][i], a.scale, from));
+          sum += s[r][t][i];
+        }
+      l[r] += sum;
+    }
+    const char* const vs = ks + HALF;
+#pragma unroll
+    for (int t = 0; t < KT; t++) {
+      constexpr int STEPS = EB == 2 ? 2 : 4;        // of 16 rows, or of 8
+#pragma unroll
+      for (int u = 0; u < STEPS; u++) {
+        constexpr int N = 16 / EB;
+        F w[RT];
+#pragma unroll
+        for (int r = 0; r < RT; r++)
+#pragma unroll
+          for (int j = 0; j < N; j++) w[r][j] = (T)s[r][t][N * u + j];
+#pragma unroll
+        for (int d = 0; d < DT; d++) {
+          F v;
+          if constexpr (EB == 2) {
+            union { F f; v4s half[2]; } x;
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+              const int row = 32 * t + 16 * u + 8 * j + 4 * h2 + (lane & 15) / 4, chunk = 4 * d + 2 * (lane >> 4 & 1) + (lane & 3) / 2;
+              x.half[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(lds_char*)(
+                  vs + row * (D * EB) + ((chunk ^ swizzle<CH>(row)) * 16) + (lane & 1) * 8));
+            }
+            v = x.f;
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+              const int row = 32 * t + 8 * u + 4 * h2 + j, chunk = 8 * d + l32 / 4;
+              v[j] = *(const float*)(vs + row * (D * EB) + ((chunk ^ swizzle<CH>(row)) * 16) + (l32 & 3) * 4);
+            }
+          }
+          if (masked && __any(not_finite<T>(v))) {
+            F up, down, no;
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+              const float x = (float)v[j];
+              up[j] = (T)(x == INFINITY ? 1.f : 0.f);
+              down[j] = (T)(x == -INFINITY ? 1.f : 0.f);
+              no[j] = (T)(x != x ? 1.f : 0.f);
+              if (!(fabsf(x) < INFINITY)) v[j] = (T)0.f;
+            }
+#pragma unroll
+            for (int r = 0; r < RT; r++) {
+              F one;
+#pragma unroll
+              for (int j = 0; j < N; j++) one[j] = (T)(seen[r] >> (32 * t + 4 * N * u / 2 + 8 * (j / 4) + 4 * h2 + j % 4) & 1 ? 1.f : 0.f);
+              const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+              const v16f x = Frag<T>::mma32(up, one, zero), y = Frag<T>::mma32(down, one, zero), z = Frag<T>::mma32(no, one, zero);
+#pragma unroll
+              for (int i = 0; i < 16; i++) o[r][d][i] += (x[i] > 0.f ? INFINITY : 0.f) - (y[i] > 0.f ? INFINITY : 0.f) + (z[i] > 0.f ? NAN : 0.f);
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < RT; r++) o[r][d] = Frag<T>::mma32(v, w[r], o[r][d]);
+        }
+      }
+    }
+  };
+  // blocks that every query of the wave sees whole come first
+  int n = 0;
+  for (; n < blocks && begin + n * KVB + KVB <= min(end, sure); n++) block(n, std::false_type());
+  for (; n < blocks; n++) block(n, std::true_type());
+#pragma unroll
+  for (int r = 0; r < RT; r++) {
+    l[r] += __shfl_xor(l[r], 32, 64);
+    if (token[r] < 0) continue;
+    const long long of = row0 + 32 * r + l32;
+    const long long slot = (long long)(it.from + it.piece) * a.c.heads + h, in = of - (long long)it.tile * ROWS;
+    float* const part = a.part + (slot * ROWS + in) * a.c.d;
+    T* const out = (T*)(const_cast<char*>(a.out.at) + (it.s.t0 + token[r]) * a.out.token + (h * a.group + (int)(of - (long long)token[r] * a.group)) * a.out.head);
+    const float by = l[r] == 0.f ? 0.f : 1.f / l[r];
+    if (it.pieces > 1 && h2 == 0) {
+      float* const st = a.part + 2ll * a.slots * ROWS * a.c.d + (slot * ROWS + in) * 2;
+      st[0] = m[r], st[1] = l[r];
+    }
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        const int e = 32 * d + 8 * k + 4 * h2;
+        if (e >= a.c.d) continue;
+        if (it.pieces > 1) {
+          *(v4f*)(part + e) = (v4f){o[r][d][4 * k], o[r][d][4 * k + 1], o[r][d][4 * k + 2], o[r][d][4 * k + 3]};
+        } else {
+          Pack<T, 4> z;
+#pragma unroll
+          for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(l[r] == 0.f ? 0.f : o[r][d][4 * k + j] * by);
+          *(Pack<T, 4>*)(out + e) = z;
+        }
+      }
+  }
+}
+
+// The pieces of a tile become its rows.  A workgroup takes `per` rows, `few` at a time: for each of them the pieces are shared out over the
+// threads that are left beside four elements each, and joined in LDS.
+template <typename T, int UNIT>
+__global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per, int few) {
+  __shared__ v4f sums[256];
+  __shared__ float stat[256][2];
+  const int groups = rows / per, h = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads, first = rest % groups * per;
+  Item it;
+  if (!find_item<UNIT>(a, rows, rest / groups, true, &it)) return;
+  const long long there = (long long)it.s.n * a.group - (long long)it.tile * rows;
+  if (it.pieces <= 1) return;
+  const int pieces = min(it.pieces, kv_pieces(max(tile_end(a, it, rows), 1), it.size));
+  const int quads = a.c.d / 4, share = 256 / (few * quads), e = threadIdx.x % (few * quads), part = threadIdx.x / (few * quads), c = e % quads;
+  for (int r0 = first; r0 < first + per && r0 < there; r0 += few) {
+    const int r = r0 + e / quads;
+    const bool mine = part < share && r < there;
+    float m = -INFINITY, l = 0.f;
+    v4f y = {0, 0, 0, 0};
+    if (mine)
+      for (int p = part; p < pieces; p += share) {
+        const long long slot = (long long)(it.from + p) * a.c.heads + h;
+        const float* const st = a.part + 2ll * a.slots * rows * a.c.d + (slot * rows + r) * 2;
+        const v4f x = *(const v4f*)(a.part + (slot * rows + r) * a.c.d + c * 4);
+        const float top = fmaxf(m, st[0]), safe = top == -INFINITY ? 0.f : top;
+        const float f = __builtin_amdgcn_exp2f(m - safe), g = __builtin_amdgcn_exp2f(st[0] - safe);
+        y = y * f + x * g;
+        l = l * f + st[1] * g;
+        m = top;
+      }
+    if (r0 > first) __syncthreads();
+    sums[threadIdx.x] = y;
+    stat[threadIdx.x][0] = m, stat[threadIdx.x][1] = l;
+    __syncthreads();
+    if (!mine || part) continue;
+    float top = m;
+    for (int p = 1; p < share; p++) top = fmaxf(top, stat[p * few * quads + e][0]);
+    const float safe = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    y = (v4f){0, 0, 0, 0};
+    for (int p = 0; p < share; p++) {
+      const float f = __builtin_amdgcn_exp2f(stat[p * few * quads + e][0] - safe);
+      sum += f * stat[p * few * quads + e][1];
+      y += f * sums[p * few * quads + e];
+    }
+    const long long of = (long long)it.tile * rows + r;
+    const int i = (int)(of / a.group), g = (int)(of - (long long)i * a.group);
+    Pack<T, 4> z;
+#pragma unroll
+    for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(sum == 0.f ? 0.f : y[j] / sum);
+    *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + (it.s.t0 + i) * a.out.token + (h * a.group + g) * a.out.head) + c * 4) = z;
+  }
 }
 
 namespace {
@@ -77,6 +742,64 @@ int attend_args(const pahq_kv_cache* cache, const pahq_kv_batch* batch, int q_he
   if (q_heads > 65535 || (long long)batch->tokens * a->group >= KV_MAX_LENGTH || batch->tokens > PAHQ_ROTARY_MAX_TOKENS) return PAHQ_ETOOBIG;
   return PAHQ_OK;
 }
+
+// How a call is cut: the tile's rows, and pieces for so many workgroups, none shorter than `least` rows of the cache
+struct Cut { int rows, slots, least; };
+Cut cut_of(const AttendArgs& a) {
+  Cut k;
+  const long long mean = (((long long)a.b.tokens + a.b.batch - 1) / std::max(a.b.batch, 1)) * a.group;      // rows a sequence and head
+  k.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : 128;
+  k.slots = 512;
+  k.least = k.rows <= 32 ? 256 : 512;
+  // the new tokens alone are so much work that a piece is as long as any sequence can be
+  const double work = (double)a.b.tokens * a.b.tokens * a.group / ((double)k.rows * std::max(a.b.batch, 1)) * a.c.heads / k.slots;
+  if (a.b.most <= k.least || a.b.most <= work) k.slots = 0;
+  return k;
+}
+size_t part_bytes(const AttendArgs& a, const Cut& k) { return k.slots ? 2ull * k.slots * k.rows * (a.c.d + 2) * 4 : 0; }
+
+template <void (*K)(AttendArgs), int THREADS, int LDS>
+int launch(hipStream_t st, unsigned grid, const AttendArgs& a) {
+  if (LDS > 65536) {
+    // more LDS than a launch gets by default: an attribute of the kernel on one device, set once for each
+    static std::atomic<bool> set[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return PAHQ_EHIP;
+    if (!set[dev].load(std::memory_order_acquire)) {
+      if (hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return PAHQ_EHIP;
+      set[dev].store(true, std::memory_order_release);
+    }
+  }
+  hipLaunchKernelGGL(K, dim3(grid), dim3(THREADS), LDS, st, a);
+  return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
+}
+template <typename T, int D>
+int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
+  constexpr int EB = sizeof(T), WIDE = D * EB, NW = WIDE <= 128 ? 4 : 2, FEW = 2 * NW * 2 * (EB == 2 ? 32 : 16) * WIDE + NW * 1024;
+  constexpr int KVB = WIDE <= 256 ? 64 : 32, FEW_UNIT = (EB == 2 ? 32 : 16) * NW;
+  const long long tiles = kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows), items = k.slots ? kv_most_items(tiles, a.c.heads, k.slots) : tiles;
+  // rows of a workgroup that joins: one where that is not too many workgroups
+  const int most = std::max(1, 256 / (a.c.d / 4));
+  int per = 1;
+  while (per < k.rows && tiles * a.c.heads * (k.rows / per) > 2048) per *= 2;
+  int few = 1;
+  while (few * 2 <= std::min(per, most)) few *= 2;
+  // threads of a launch are counted in 32 bits
+  if (items * a.c.heads >= KV_MOST_ITEMS || tiles * a.c.heads * (k.rows / per) >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
+  const unsigned grid = (unsigned)(items * a.c.heads);
+  const int rc = k.rows == 16   ? launch<kv_few_k<T, D, 1, NW>, NW * 64, FEW>(st, grid, a)
+                 : k.rows == 32 ? launch<kv_few_k<T, D, 2, NW>, NW * 64, FEW>(st, grid, a)
+                                : launch<kv_tile_k<T, D, 1, KVB>, 256, 4 * KVB * WIDE + 2048>(st, grid, a);
+  if (rc || !k.slots) return rc;
+  const dim3 joins((unsigned)(tiles * a.c.heads * (k.rows / per)));
+  if (k.rows < 128) hipLaunchKernelGGL((kv_join_k<T, FEW_UNIT>), joins, dim3(256), 0, st, a, k.rows, per, few);
+  else hipLaunchKernelGGL((kv_join_k<T, KVB>), joins, dim3(256), 0, st, a, k.rows, per, few);
+  return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
+}
+template <typename T>
+int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
+  return a.c.d <= 64 ? attend_as<T, 64>(st, a, k) : a.c.d <= 128 ? attend_as<T, 128>(st, a, k) : attend_as<T, 256>(st, a, k);
+}
 }  // namespace
 
 }  // namespace pahq
@@ -88,7 +811,7 @@ extern "C" int pahq_kv_attention_workspace(const pahq_kv_cache* cache, const pah
   KvRange held[2], lists[3];
   if (!bytes) return PAHQ_EINVAL;
   if (const int rc = attend_args(cache, batch, q_heads, &a, held, lists)) return rc;
-  *bytes = 0;
+  *bytes = a.b.batch && a.b.tokens ? part_bytes(a, cut_of(a)) : 0;
   return PAHQ_OK;
 }
 
@@ -97,24 +820,30 @@ extern "C" int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, c
   AttendArgs a = {};
   KvRange held[2], lists[3], qr, outr;
   if (const int rc = attend_args(cache, batch, q_heads, &a, held, lists)) return rc;
-  if (words < (tree ? 1 : 0) || (uintptr_t)tree % 8) return PAHQ_EINVAL;
+  if (words < (tree ? 1 : 0) || (uintptr_t)tree % 8 || !std::isfinite(scale * 1.4426950408889634)) return PAHQ_EINVAL;
   if (batch->batch == 0 || batch->tokens == 0) return PAHQ_OK;
   const int eb = dtype_bytes(cache->dtype), tokens = batch->tokens;
   if (!kv_rows_args(q, tokens, q_heads, a.c.d, eb, false, &a.q, &qr) || !kv_rows_args(out, tokens, q_heads, a.c.d, eb, true, &a.out, &outr)) return PAHQ_EINVAL;
-  const KvRange masks = {tree, (size_t)tokens * words * 8}, space = {workspace, workspace_bytes};
+  const Cut cut = cut_of(a);
+  const size_t need = part_bytes(a, cut);
+  if (need && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return PAHQ_EINVAL;
+  const KvRange masks = {tree, (size_t)tokens * words * 8}, space = {need ? workspace : nullptr, need};
   const KvRange read[] = {held[0], held[1], lists[0], lists[1], lists[2], masks, space, qr};
-  if (kv_meets(&outr, 1, read, 7) || (workspace_bytes && kv_meets(&space, 1, read, 6)) || (workspace_bytes && kv_meets(&space, 1, &qr, 1))) return PAHQ_EINVAL;
+  if (kv_meets(&outr, 1, read, 7) || kv_meets(&space, 1, read, 6) || kv_meets(&space, 1, &qr, 1)) return PAHQ_EINVAL;
   const bool in_place = q->at == out->at && q->token == out->token && q->head == out->head;
   if (!in_place && !kv_rows_apart(a.out, outr, q_heads, a.q, qr, q_heads, (size_t)a.c.d * eb)) return PAHQ_EINVAL;
   a.tree = (const unsigned long long*)tree;
   a.words = words;
-  a.scale = (float)(scale * 1.4426950408889634);
-  const dim3 grid(tokens, q_heads);
+  a.scale = (float)(std::fabs((double)scale) * 1.4426950408889634);
+  a.sign = scale < 0.f ? -1.f : a.scale > 0.f ? 1.f : 0.f;
+  if (!(a.scale > 0.f)) a.scale = 1.f;
+  a.part = (float*)workspace;
+  a.slots = cut.slots;
+  a.least = cut.least;
   hipStream_t st = (hipStream_t)hip_stream;
   switch (cache->dtype) {
-    case PAHQ_F32: hipLaunchKernelGGL(kv_attend_k<float>, grid, dim3(256), 0, st, a); break;
-    case PAHQ_BF16: hipLaunchKernelGGL(kv_attend_k<bf16_t>, grid, dim3(256), 0, st, a); break;
-    default: hipLaunchKernelGGL(kv_attend_k<f16_t>, grid, dim3(256), 0, st, a);
+    case PAHQ_F32: return attend_as<float>(st, a, cut);
+    case PAHQ_BF16: return attend_as<bf16_t>(st, a, cut);
+    default: return attend_as<f16_t>(st, a, cut);
   }
-  return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }

@@ -33,6 +33,7 @@ def append(P, **change):
 
 
 def attention(P, **change):
+    change = dict(dict(batch_width=400, batch_ld_pages=400), **change)             # long enough to be cut, which takes a workspace
     cache, batch, r = structs(P, change)
     a = dict(dict(tree=None, words=0, scale=1.0, q_heads=4, workspace=12 * A, bytes=A), **change)
     return P.lib().pahq_kv_attention(None, cache, batch, r["q"], a["q_heads"], a["tree"], a["words"], a["scale"], r["out"], a["workspace"], a["bytes"])
@@ -52,7 +53,7 @@ CACHES = [(dict(cache_dtype=3), EINVAL), (dict(cache_pages=0), EINVAL), (dict(ca
           (dict(cache_page_stride=1 << 60), EINVAL), (dict(cache_page_stride=1 << 62), EINVAL), (dict(cache_slot_stride=1 << 52), EINVAL), (dict(cache_heads=65536, cache_page_stride=1 << 30), ETOOBIG)]
 BATCHES = [(dict(batch_batch=-1), EINVAL), (dict(batch_width=-1), EINVAL), (dict(batch_tokens=-1), EINVAL), (dict(batch_starts=None), EINVAL),
            (dict(batch_lengths=None), EINVAL), (dict(batch_pages=None), EINVAL), (dict(batch_starts=3 * A + 2), EINVAL), (dict(batch_lengths=4 * A + 1), EINVAL),
-           (dict(batch_pages=5 * A + 3), EINVAL), (dict(batch_ld_pages=3), EINVAL), (dict(batch_ld_pages=1 << 62), EINVAL), (dict(batch_batch=65536), ETOOBIG)]
+           (dict(batch_pages=5 * A + 3), EINVAL), (dict(batch_width=400, batch_ld_pages=399), EINVAL), (dict(batch_ld_pages=1 << 62), EINVAL), (dict(batch_batch=65536), ETOOBIG)]
 
 
 @pytest.mark.parametrize("change, code", CACHES + BATCHES)
@@ -82,11 +83,12 @@ def test_append_refuses(P, change, code):
 
 
 @pytest.mark.parametrize("change, code", [
-    (dict(q=None), EINVAL), (dict(out=None), EINVAL), (dict(q_heads=0), EINVAL), (dict(q_heads=3), EINVAL), (dict(tree=15 * A, words=0), EINVAL), (dict(words=-1), EINVAL),
+    (dict(q=None), EINVAL), (dict(out=None), EINVAL), (dict(q_heads=0), EINVAL), (dict(q_heads=3), EINVAL), (dict(tree=15 * A, words=0), EINVAL), (dict(words=-1), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(scale=float("nan")), EINVAL),
     (dict(tree=15 * A + 4, words=1), EINVAL), (dict(q=(8 * A + 1, 256, 64)), EINVAL), (dict(q=(8 * A, -1, 64)), EINVAL), (dict(out=(9 * A, 255, 64)), EINVAL),
     (dict(out=(8 * A + 2, 256, 64)), EINVAL), (dict(out=(A, 256, 64)), EINVAL), (dict(out=(2 * A, 256, 64)), EINVAL), (dict(out=(3 * A, 256, 64)), EINVAL),
     (dict(out=(5 * A, 256, 64)), EINVAL), (dict(tree=9 * A, words=1), EINVAL), (dict(out=(12 * A, 256, 64)), EINVAL), (dict(workspace=A), EINVAL), (dict(workspace=8 * A), EINVAL),
-    (dict(workspace=5 * A), EINVAL), (dict(tree=12 * A, words=1), EINVAL), (dict(q_heads=131072, q=(8 * A, 1 << 24, 64), out=(9 * A, 1 << 24, 64)), ETOOBIG),
+    (dict(workspace=5 * A), EINVAL), (dict(workspace=None), EINVAL),
+    (dict(bytes=4096), EINVAL), (dict(workspace=12 * A + 8), EINVAL), (dict(tree=12 * A, words=1), EINVAL), (dict(q_heads=131072, q=(8 * A, 1 << 24, 64), out=(9 * A, 1 << 24, 64)), ETOOBIG),
     (dict(batch_tokens=1 << 24), ETOOBIG), (dict(batch_tokens=0, q=None, out=None), 0)])
 def test_attention_refuses(P, change, code):
     assert attention(P, **change) == code
