@@ -28,103 +28,96 @@ struct AttendArgs {
   const unsigned long long* tree;
   int words, group;                                 // group: query heads of a cache head
   float scale, sign;                                // of the scores: times log2 e and positive; of the queries: its sign, 0 for a scale of 0
-  float* part;                                      // [slot][rows][d] sums of pieces, then [slot][rows][2] maximum and sum
-  int slots, least;                                 // of pieces (kv_plan.h); slots 0: nothing is cut
+  float* part;                                      // [slot][rows][d] sums of a part, then [slot][rows][2] maximum and sum
+  int slots, least;                                 // of ranges (kv_plan.h); slots 0: nothing is cut
 };
 
 // ---------------------------------------------------------------- a workgroup's part
-struct Item {
-  KvSequence s;
-  int b, tile, tiles, piece, pieces, from;          // from: the tile's first slot in the workspace (pieces > 1)
-  int size;                                         // rows of the cache a piece
-};
 __device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
-__device__ __forceinline__ int wave_sum_before(int v) {       // of the lanes in front
-  int s = v;
+__device__ __forceinline__ uint64_t lane_of(uint64_t v, int l) {
+  return (uint64_t)(uint32_t)lane_of((int)(v >> 32), l) << 32 | (uint32_t)lane_of((int)v, l);
+}
+template <typename N> __device__ __forceinline__ N wave_sum_before(N v) {        // of the lanes in front
+  N s = v;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(s, o, 64);
+    const N u = __shfl_up(s, o, 64);
     if ((int)(threadIdx.x & 63) >= o) s += u;
   }
   return s - v;
 }
-// Every wave finds it by itself, 64 sequences at a time.  by_tile: the index counts tiles and not pieces.  false: no such item.
-template <int UNIT>
-__device__ bool find_item(const AttendArgs& a, int rows, int index, bool by_tile, Item* it) {
-  const int lane = threadIdx.x & 63, rounds = (a.b.batch + 63) / 64;
-  KvSequence s = {};
-  int tiles = 0, size = KV_MAX_LENGTH;
-  auto look = [&](int r) {
-    const int b = r * 64 + lane;
-    tiles = 0;
-    if (b < a.b.batch) {
-      s = kv_sequence(a.b, b);
-      tiles = kv_tiles((long long)s.n * a.group, rows);
-    }
-  };
-  if (rounds == 1) look(0);
-  if (a.slots) {
-    double work = 0, all = 0;                       // sums that no batch can overflow
-    for (int r = 0; r < rounds; r++) {
-      if (rounds > 1) look(r);
-      work += tiles ? (double)tiles * s.length : 0;
-      all += tiles;
-    }
-    size = __builtin_amdgcn_readfirstlane(kv_first_piece(wave_sum_d(work) * a.c.heads, a.slots, UNIT, a.least));
-    if (__builtin_amdgcn_readfirstlane(wave_sum_d(all) * a.c.heads * 2 <= a.slots))
-      for (int guess = 0; guess < KV_GUESSES; guess++) {
-        all = 0;
-        for (int r = 0; r < rounds; r++) {
-          if (rounds > 1) look(r);
-          all += tiles ? (double)tiles * kv_pieces(s.length, size) : 0;
-        }
-        if (__builtin_amdgcn_readfirstlane(wave_sum_d(all) * a.c.heads <= a.slots)) break;
-        size = kv_longer_piece(size, UNIT);
-      }
+// A sequence in a lane, 64 of them at a time
+struct Share { KvSequence s; int tiles; uint64_t units; };            // units: of all its tiles and heads
+template <int UNIT> __device__ __forceinline__ Share share_of(const AttendArgs& a, int rows, int b) {
+  Share x = {};
+  if (b < a.b.batch) {
+    x.s = kv_sequence(a.b, b);
+    x.tiles = kv_tiles((long long)x.s.n * a.group, rows);
+    x.units = kv_units(x.tiles, a.c.heads, x.s.length, UNIT);
   }
-  int before = 0, cut_before = 0;
-  for (int r = 0; r < rounds; r++) {
-    if (rounds > 1) look(r);
-    // starts that do not grow can name more items than a launch has workgroups: no sum of theirs may pass 31 bits
-    const int pieces = tiles ? kv_pieces(s.length, size) : 0, items = (int)min((long long)tiles * pieces, (long long)KV_MOST_ITEMS);
-    const int count = by_tile ? min(tiles, KV_MOST_ITEMS) : items, cut = pieces > 1 ? items : 0;
-    const int at = before + wave_sum_before(count), slot = cut_before + wave_sum_before(cut);
-    const unsigned long long mine = __ballot(index >= at && index < at + count);
-    if (mine) {
-      const int l = __builtin_ctzll(mine);
-      it->b = r * 64 + l;
-      it->s = {lane_of(s.t0, l), lane_of(s.n, l), lane_of(s.length, l), lane_of(s.base, l)};
-      it->tiles = lane_of(tiles, l);
-      it->pieces = lane_of(pieces, l);
-      it->size = size;
-      const int local = index - lane_of(at, l);
-      // the last tiles see the most rows of the cache and come first
-      it->tile = it->tiles - 1 - (by_tile ? local : local / it->pieces);
-      it->piece = by_tile ? 0 : local % it->pieces;
-      it->from = lane_of(slot, l) + (it->tiles - 1 - it->tile) * it->pieces;
-      return true;
-    }
-    before = min(lane_of(at + count, 63), 1 << 29);
-    cut_before = min(lane_of(slot + cut, 63), 1 << 29);
-  }
-  return false;
+  return x;
 }
+template <int UNIT> __device__ KvPlan plan_of(const AttendArgs& a, int rows) {
+  if (!a.slots) return {0, 0};
+  uint64_t units = 0;
+  int longest = 0;
+  for (int b = threadIdx.x & 63; b < a.b.batch; b += 64) {
+    const Share x = share_of<UNIT>(a, rows, b);
+    units += x.units;
+    if (x.tiles) longest = max(longest, kv_units_of(x.s.length, UNIT));
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    units += __shfl_xor(units, o, 64);
+    longest = max(longest, __shfl_xor(longest, o, 64));
+  }
+  return kv_plan(lane_of(units, 0), lane_of(longest, 0), a.slots, a.least);
+}
+struct Item {
+  KvSequence s;
+  int b, tile, h, begin, end, slot;                 // rows of the cache; slot in the workspace, -1: the whole tile
+};
 // How many rows of the cache a tile sees at most
-__device__ __forceinline__ int tile_end(const AttendArgs& a, const Item& it, int rows) {
-  if (a.tree) return it.s.length;
-  const int last = min(it.s.n - 1, (int)((((long long)it.tile + 1) * rows - 1) / a.group));
-  return max(it.s.base + last + 1, 0);
+__device__ __forceinline__ int tile_end(const AttendArgs& a, const KvSequence& s, int tile, int rows) {
+  if (a.tree) return s.length;
+  const int last = min(s.n - 1, (int)((((long long)tile + 1) * rows - 1) / a.group));
+  return max(s.base + last + 1, 0);
 }
-// The rows of the cache of a piece of a tile; false: none, and nothing to write
-__device__ __forceinline__ bool piece_rows(const AttendArgs& a, const Item& it, int rows, int* begin, int* end) {
-  *begin = 0;
-  *end = tile_end(a, it, rows);
-  if (it.pieces <= 1) return true;
-  const long long from = (long long)it.piece * it.size;
-  if (from >= *end && it.piece) return false;       // the first one runs even if it sees nothing
-  *begin = (int)from;
-  *end = (int)min((long long)*end, from + it.size);
-  return true;
+// What workgroup `wg` of the plan does at `at`, up to `stop` at most: units in front of `at` are done.  Returns how many it takes, 0 if there
+// is nothing.  Without ranges the units are tiles, those of a cache head apart.
+template <int UNIT> __device__ uint64_t next_item(const AttendArgs& a, int rows, const KvPlan& p, int wg, uint64_t at, uint64_t stop, Item* it) {
+  uint64_t before = 0;
+  for (int b0 = 0; b0 < a.b.batch; b0 += 64) {
+    const Share x = share_of<UNIT>(a, rows, b0 + (threadIdx.x & 63));
+    const uint64_t count = p.wgs ? x.units : (uint64_t)x.tiles, from = before + wave_sum_before(count);
+    const unsigned long long mine = __ballot(at >= from && at < from + count);
+    if (mine) {
+      const int l = __builtin_ctzll(mine), tiles = lane_of(x.tiles, l);
+      const uint64_t local = at - lane_of(from, l);
+      it->b = b0 + l;
+      it->s = {lane_of(x.s.t0, l), lane_of(x.s.n, l), lane_of(x.s.length, l), lane_of(x.s.base, l)};
+      it->begin = 0;
+      it->slot = -1;
+      if (!p.wgs) {                                 // the last tiles see the most rows and come first
+        it->h = wg;
+        it->tile = tiles - 1 - (int)local;
+        it->end = tile_end(a, it->s, it->tile, rows);
+        return 1;
+      }
+      const uint32_t whole = kv_units_of(it->s.length, UNIT);
+      const uint64_t pair = local / whole;
+      const uint32_t off = (uint32_t)(local - pair * whole), take = (uint32_t)min((uint64_t)(whole - off), stop - at);
+      it->h = (int)(pair / (uint32_t)tiles);
+      it->tile = (int)(pair - (uint64_t)it->h * tiles);
+      it->end = tile_end(a, it->s, it->tile, rows);
+      it->begin = min((int)min((uint64_t)off * UNIT, (uint64_t)KV_MAX_LENGTH), it->end);
+      if (off + take < whole) it->end = min(it->end, (int)((off + take) * UNIT));
+      if (take < whole) it->slot = 2 * wg + (off ? 0 : 1);
+      return take;
+    }
+    before = lane_of(from + count, 63);
+  }
+  return 0;
 }
 // Bit x: whether new token i (row t of the operator's) sees row k0 + x of the cache
 __device__ __forceinline__ unsigned long long seen_bits(const AttendArgs& a, const KvSequence& s, int i, int k0, int end) {
@@ -180,7 +173,15 @@ template <int CH> __device__ __forceinline__ int swizzle(int row) {
   static_assert(CH >= 8, "rows of 128 bytes and more");
   return CH >= 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
 }
-typedef __attribute__((address_space(3))) char lds_char;
+// What lies at an address of LDS.  The reads of a block differ from one base in the chunk, which XOR changes in place (rows begin at multiples of
+// their size), and in rows a constant apart: `base` is hidden from the compiler so that it derives each address where it is used instead of
+// keeping sixteen of them.
+template <typename F> __device__ __forceinline__ F at_lds(uint32_t a) { return *(const __attribute__((address_space(3))) F*)(uintptr_t)a; }
+__device__ __forceinline__ v4s at_lds_turned(uint32_t a) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)a); }
+__device__ __forceinline__ uint32_t hidden(uint32_t base) {
+  asm volatile("" : "+v"(base));
+  return base;
+}
 
 // Rows of the cache on their way into LDS.  A lane keeps where its row of a block lies; the pages' numbers came through LDS themselves
 // (`ids`, asked for two blocks ahead), because a load into a register would make the compiler wait for everything in flight.
@@ -194,28 +195,46 @@ __device__ __forceinline__ long long row_at(const KvCache& c, int row, int end, 
   const int slot = row - (int)((unsigned long long)(uint32_t)row * c.magic >> c.shift) * c.page_size;
   return (uint32_t)page < (uint32_t)c.pages ? page * c.page + slot * c.slot : ROW_NONE;
 }
-// Rows r0 .. of the block, 64 / CH of them, chunk by chunk: lane l writes the l-th 16 bytes behind lds.  `of` rows' offsets lie in
-// lanes `first` and on.
-template <typename T, int CH>
+// Rows r0 .. of the block, 64 / CH of them (r0 a multiple of that), chunk by chunk: lane l writes the l-th 16 bytes behind lds.  Their
+// offsets lie in lanes `first` and on.
+template <typename T, int CH, bool ONCE>
 __device__ __forceinline__ void ask_rows(const KvCache& c, long long head, long long mine, int first, int r0, uint32_t lds_k, uint32_t lds_v) {
-  const int lane = threadIdx.x & 63, r = lane / CH, p = lane % CH;
-  const int chunk = p ^ swizzle<CH>(r0 + r);
-  const long long at = (long long)__shfl((unsigned long long)mine, first + r, 64);
-  const char *k = c.keys + head + at + chunk * 16, *v = c.values + head + at + chunk * 16;
-  const bool none = at == ROW_NONE, zero = at == ROW_BEHIND || chunk * 16 >= c.d * (int)sizeof(T);
-  if (none || zero) k = v = (const char*)kv_chunk[zero ? 0 : NAN_CHUNK<T>];
-  slab_load16((const uint8_t*)k, lds_k);
-  slab_load16((const uint8_t*)v, lds_v);
+  const int lane = threadIdx.x & 63;
+  const int chunk = (lane % CH ^ swizzle<CH>(lane / CH)) ^ swizzle<CH>(r0);
+  const long long at = (long long)__shfl((unsigned long long)mine, first + lane / CH, 64), off = at + chunk * 16;
+  const char *k = c.keys + head + off, *v = c.values + head + off;
+  if (at < 0 || chunk * 16 >= c.d * (int)sizeof(T)) k = v = (const char*)kv_chunk[at == ROW_NONE && chunk * 16 < c.d * (int)sizeof(T) ? NAN_CHUNK<T> : 0];
+  if (ONCE) {
+    slab_load16_nt((const uint8_t*)k, lds_k);
+    slab_load16_nt((const uint8_t*)v, lds_v);
+  } else {
+    slab_load16((const uint8_t*)k, lds_k);
+    slab_load16((const uint8_t*)v, lds_v);
+  }
 }
 
-// Values that some query of the tile does not see may be infinities or NaN, and 0 * NaN is one: they leave the product and come back
-// as how many of each kind a query sees.
+// Values that some query of the tile does not see may be infinities or NaN, and 0 * NaN is one.  They leave the product, and come back
+// through another one, of which kinds a query sees: up to 32 rows count 1 each for infinity, 64 for -infinity, 4096 for NaN.
 template <typename T, typename F> __device__ __forceinline__ bool not_finite(F v) {
-  constexpr int N = 16 / sizeof(T);
   bool bad = false;
 #pragma unroll
-  for (int j = 0; j < N; j++) bad |= !(fabsf((float)v[j]) < INFINITY);
+  for (int j = 0; j < 16 / (int)sizeof(T); j++) bad |= !(fabsf((float)v[j]) < INFINITY);
   return bad;
+}
+template <typename T, typename F> __device__ __forceinline__ F take_kinds(F* v) {
+  F kinds;
+#pragma unroll
+  for (int j = 0; j < 16 / (int)sizeof(T); j++) {
+    const float x = (float)(*v)[j];
+    const bool fine = fabsf(x) < INFINITY;
+    kinds[j] = (T)(fine ? 0.f : x == INFINITY ? 1.f : x == -INFINITY ? 64.f : 4096.f);
+    if (!fine) (*v)[j] = (T)0.f;
+  }
+  return kinds;
+}
+__device__ __forceinline__ float of_kinds(float count) {
+  const int n = (int)count;
+  return n == 0 ? 0.f : n < 64 ? INFINITY : (n & 63) || n >= 4096 ? NAN : -INFINITY;
 }
 
 // ---------------------------------------------------------------- up to 16 RT rows of queries
@@ -227,14 +246,21 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   constexpr int EB = sizeof(T), CH = D * EB / 16, KT = EB == 2 ? 2 : 1, KVB = 16 * KT, ROWS = 16 * RT;
   constexpr int HALF = KVB * D * EB, STAGE = 2 * HALF, ASKS = HALF / 1024, DT = D / 16;
   static_assert(2 * STAGE >= ROWS * D * 4 && 2 * ASKS + 1 < 64, "the waves' sums fit their stages");
-  extern __shared__ __align__(16) char lds[];       // [NW][2][STAGE], [NW][4][64] pages' numbers
+  extern __shared__ __align__(1024) char lds[];       // [NW][2][STAGE], [NW][4][64] pages' numbers
   __shared__ float stat[NW][ROWS][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, h4 = lane >> 4;
-  const int h = blockIdx.x % a.c.heads;
+  const KvPlan plan = plan_of<KVB * NW>(a, ROWS);
+  const int wg = plan.wgs ? kv_wg_of(blockIdx.x, plan.wgs) : (int)(blockIdx.x % a.c.heads);
+  if (wg < 0) return;
+  uint64_t at = plan.wgs ? kv_from(plan.units, plan.wgs, wg) : blockIdx.x / a.c.heads;
+  const uint64_t stop = plan.wgs ? kv_from(plan.units, plan.wgs, wg + 1) : at + 1;
+  for (bool first = true; at < stop; first = false) {
   Item it;
-  if (!find_item<KVB * NW>(a, ROWS, blockIdx.x / a.c.heads, false, &it)) return;
-  int begin, end;
-  if (!piece_rows(a, it, ROWS, &begin, &end)) return;
+  const uint64_t take = next_item<KVB * NW>(a, ROWS, plan, wg, at, stop, &it);
+  if (!take) return;
+  at += take;
+  const int begin = it.begin, end = it.end, h = it.h;
+  if (!first) __syncthreads();                      // the stages held the last tile's sums
 
   // the tile's queries: lane l16 of row tile r holds chunks h4, h4 + 4, ... of row 16 r + l16
   int token[RT];
@@ -269,7 +295,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     const long long at = row_at(a.c, first_row(n) + (lane & (KVB - 1)), end, ids[(n & 3) * 64 + lane]);
     const uint32_t to = stage0 + (n & 1) * STAGE;
 #pragma unroll
-    for (int j = 0; j < ASKS; j++) ask_rows<T, CH>(a.c, head, at, j * (64 / CH), j * (64 / CH), to + j * 1024, to + HALF + j * 1024);
+    for (int j = 0; j < ASKS; j++) ask_rows<T, CH, true>(a.c, head, at, j * (64 / CH), j * (64 / CH), to + j * 1024, to + HALF + j * 1024);
   };
   v4f o[RT][DT] = {};
   float m[RT], l[RT];
@@ -294,16 +320,16 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     } else {
       wait_vm_lds<0>();
     }
-    const char* const ks = mine + (n & 1) * STAGE;
+    const uint32_t stage = stage0 + (n & 1) * STAGE;
+    const uint32_t ks = hidden(stage + l16 * (D * EB) + ((h4 ^ swizzle<CH>(l16)) * 16));
     v4f s[RT][KT];
 #pragma unroll
     for (int t = 0; t < KT; t++) {
 #pragma unroll
       for (int r = 0; r < RT; r++) s[r][t] = (v4f){0, 0, 0, 0};
-      const int row = 16 * t + l16;
 #pragma unroll
       for (int c = 0; c < CH / 4; c++) {
-        const F k = *(const F*)(ks + row * (D * EB) + (((h4 + 4 * c) ^ swizzle<CH>(row)) * 16));
+        const F k = at_lds<F>((ks ^ (4 * c * 16)) + 16 * t * (D * EB));
 #pragma unroll
         for (int r = 0; r < RT; r++) s[r][t] = Frag<T>::mma16(k, q[r][c], s[r][t]);
       }
@@ -342,7 +368,9 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
           l[r] += p[r][t][i];
         }
     }
-    const char* const vs = ks + HALF;
+    const int vrow = 4 * h4 + (EB == 2 ? l16 / 4 : 0);
+    const uint32_t vs = EB == 2 ? hidden(stage + HALF + vrow * (D * EB) + (((l16 & 3) / 2 ^ swizzle<CH>(vrow)) * 16) + (l16 & 1) * 8)
+                                : hidden(stage + HALF + vrow * (D * EB) + ((l16 / 4 ^ swizzle<CH>(vrow)) * 16) + (l16 & 3) * 4);
     if constexpr (EB == 2) {
       F w[RT];
 #pragma unroll
@@ -353,29 +381,17 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
       for (int d = 0; d < DT; d++) {
         union { F f; v4s half[2]; } v;
 #pragma unroll
-        for (int t = 0; t < 2; t++) {
-          const int row = 16 * t + 4 * h4 + l16 / 4, chunk = 2 * d + (l16 & 3) / 2;
-          v.half[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(lds_char*)(
-              vs + row * (D * EB) + ((chunk ^ swizzle<CH>(row)) * 16) + (l16 & 1) * 8));
-        }
+        for (int t = 0; t < 2; t++) v.half[t] = at_lds_turned((vs ^ (2 * d * 16)) + 16 * t * (D * EB));
         if (masked && __any(not_finite<T>(v.f))) {
-          F up, down, no;
-#pragma unroll
-          for (int j = 0; j < 8; j++) {
-            const float x = (float)v.f[j];
-            up[j] = (T)(x == INFINITY ? 1.f : 0.f);
-            down[j] = (T)(x == -INFINITY ? 1.f : 0.f);
-            no[j] = (T)(x != x ? 1.f : 0.f);
-            if (!(fabsf(x) < INFINITY)) v.f[j] = (T)0.f;
-          }
+          const F kinds = take_kinds<T>(&v.f);
 #pragma unroll
           for (int r = 0; r < RT; r++) {
             F one;
 #pragma unroll
             for (int j = 0; j < 8; j++) one[j] = (T)(seen[r] >> (16 * (j / 4) + 4 * h4 + j % 4) & 1 ? 1.f : 0.f);
-            const v4f zero = {0, 0, 0, 0}, u = Frag<T>::mma16(up, one, zero), n = Frag<T>::mma16(down, one, zero), x = Frag<T>::mma16(no, one, zero);
+            const v4f n = Frag<T>::mma16(kinds, one, (v4f){0, 0, 0, 0});
 #pragma unroll
-            for (int i = 0; i < 4; i++) o[r][d][i] += (u[i] > 0.f ? INFINITY : 0.f) - (n[i] > 0.f ? INFINITY : 0.f) + (x[i] > 0.f ? NAN : 0.f);
+            for (int i = 0; i < 4; i++) o[r][d][i] += of_kinds(n[i]);
           }
         }
 #pragma unroll
@@ -386,27 +402,17 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
       for (int d = 0; d < DT; d++) {
         F v;
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const int row = 4 * h4 + i, chunk = 4 * d + l16 / 4;
-          v[i] = *(const float*)(vs + row * (D * EB) + ((chunk ^ swizzle<CH>(row)) * 16) + (l16 & 3) * 4);
-        }
+        for (int i = 0; i < 4; i++) v[i] = at_lds<float>((vs ^ ((4 * d ^ swizzle<CH>(i)) * 16)) + i * (D * EB));
         if (masked && __any(not_finite<T>(v))) {
-          F up, down, no;
-#pragma unroll
-          for (int i = 0; i < 4; i++) {
-            up[i] = v[i] == INFINITY ? 1.f : 0.f;
-            down[i] = v[i] == -INFINITY ? 1.f : 0.f;
-            no[i] = v[i] != v[i] ? 1.f : 0.f;
-            if (!(fabsf(v[i]) < INFINITY)) v[i] = 0.f;
-          }
+          const F kinds = take_kinds<T>(&v);
 #pragma unroll
           for (int r = 0; r < RT; r++) {
             F one;
 #pragma unroll
             for (int i = 0; i < 4; i++) one[i] = seen[r] >> (4 * h4 + i) & 1 ? 1.f : 0.f;
-            const v4f zero = {0, 0, 0, 0}, u = Frag<T>::mma16(up, one, zero), n = Frag<T>::mma16(down, one, zero), x = Frag<T>::mma16(no, one, zero);
+            const v4f n = Frag<T>::mma16(kinds, one, (v4f){0, 0, 0, 0});
 #pragma unroll
-            for (int i = 0; i < 4; i++) o[r][d][i] += (u[i] > 0.f ? INFINITY : 0.f) - (n[i] > 0.f ? INFINITY : 0.f) + (x[i] > 0.f ? NAN : 0.f);
+            for (int i = 0; i < 4; i++) o[r][d][i] += of_kinds(n[i]);
           }
         }
 #pragma unroll
@@ -445,8 +451,8 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
       sum += f * stat[w][row][1];
       y += f * *(const v4f*)(lds + w * 2 * STAGE + row * (D * 4) + ((c ^ (row & 15)) * 16));
     }
-    if (it.pieces > 1) {
-      const long long slot = (long long)(it.from + it.piece) * a.c.heads + h;
+    if (it.slot >= 0) {
+      const long long slot = it.slot;
       *(v4f*)(a.part + (slot * ROWS + row) * a.c.d + c * 4) = y;
       float* const st = a.part + 2ll * a.slots * ROWS * a.c.d + (slot * ROWS + row) * 2;
       if (c == 0) st[0] = top, st[1] = sum;
@@ -457,6 +463,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
       for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(sum == 0.f ? 0.f : y[j] / sum);
       *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + (it.s.t0 + i) * a.out.token + (h * a.group + g) * a.out.head) + c * 4) = z;
     }
+  }
   }
 }
 
@@ -469,13 +476,20 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   constexpr int EB = sizeof(T), CH = D * EB / 16, KT = KVB / 32, NW = 4, ROWS = 32 * RT * NW;
   constexpr int HALF = KVB * D * EB, STAGE = 2 * HALF, MINE = KVB / NW, ASKS = HALF / 1024 / NW, DT = D / 32;
   static_assert(ASKS >= 1 && MINE * CH == ASKS * 64 && KVB <= 64, "a wave asks for whole rows");
-  extern __shared__ __align__(16) char lds[];       // [2][STAGE], [NW][2][64] pages' numbers
+  extern __shared__ __align__(1024) char lds[];       // [2][STAGE], [NW][2][64] pages' numbers
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h2 = lane >> 5;
-  const int h = blockIdx.x % a.c.heads;
+  const KvPlan plan = plan_of<KVB>(a, ROWS);
+  const int wg = plan.wgs ? kv_wg_of(blockIdx.x, plan.wgs) : (int)(blockIdx.x % a.c.heads);
+  if (wg < 0) return;
+  uint64_t at = plan.wgs ? kv_from(plan.units, plan.wgs, wg) : blockIdx.x / a.c.heads;
+  const uint64_t stop = plan.wgs ? kv_from(plan.units, plan.wgs, wg + 1) : at + 1;
+  for (bool first = true; at < stop; first = false) {
   Item it;
-  if (!find_item<KVB>(a, ROWS, blockIdx.x / a.c.heads, false, &it)) return;
-  int begin, end;
-  if (!piece_rows(a, it, ROWS, &begin, &end)) return;
+  const uint64_t take = next_item<KVB>(a, ROWS, plan, wg, at, stop, &it);
+  if (!take) return;
+  at += take;
+  const int begin = it.begin, end = it.end, h = it.h;
+  if (!first) __syncthreads();                      // the stages held the last tile's rows
 
   // the wave's queries: lane l32 of row tile r holds chunks h2, h2 + 2, ... of row 32 r + l32
   const long long row0 = (long long)it.tile * ROWS + wave * 32 * RT;
@@ -498,8 +512,8 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
     }
   }
   // what the wave's rows see at least (unmasked) and at most: blocks behind the latter are left out
-  const int first = (int)(row0 / a.group), last = min(it.s.n - 1, (int)((row0 + 32 * RT - 1) / a.group));
-  const int sure = it.s.base + (a.tree ? 0 : first + 1);
+  const int least = (int)(row0 / a.group), last = min(it.s.n - 1, (int)((row0 + 32 * RT - 1) / a.group));
+  const int sure = it.s.base + (a.tree ? 0 : least + 1);
   const int wave_end = row0 >= (long long)it.s.n * a.group ? 0 : a.tree ? end : min(end, it.s.base + last + 1);
 
   const int* const pages = a.b.pages + it.b * a.b.ld;
@@ -507,13 +521,13 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   const uint32_t stage0 = __builtin_amdgcn_readfirstlane(lds_addr_of(lds));
   int* const ids = (int*)(lds + 2 * STAGE) + wave * 2 * 64;
   const uint32_t ids0 = __builtin_amdgcn_readfirstlane(lds_addr_of(ids));
-  const int blocks = (end - begin + KVB - 1) / KVB;
+  const int blocks = end > begin ? (end - begin + KVB - 1) / KVB : 0;
   auto ask_ids = [&](int n) { ask_page(a.c, pages, begin + n * KVB + wave * MINE + (lane & (MINE - 1)), end, ids0 + (n & 1) * 256); };
   auto ask_block = [&](int n) {
     const long long at = row_at(a.c, begin + n * KVB + wave * MINE + (lane & (MINE - 1)), end, ids[(n & 1) * 64 + lane]);
     const uint32_t to = stage0 + (n & 1) * STAGE + wave * ASKS * 1024;
 #pragma unroll
-    for (int j = 0; j < ASKS; j++) ask_rows<T, CH>(a.c, head, at, j * (64 / CH), wave * MINE + j * (64 / CH), to + j * 1024, to + HALF + j * 1024);
+    for (int j = 0; j < ASKS; j++) ask_rows<T, CH, false>(a.c, head, at, j * (64 / CH), wave * MINE + j * (64 / CH), to + j * 1024, to + HALF + j * 1024);
   };
   v16f o[RT][DT] = {};
   float m[RT], l[RT];
@@ -535,16 +549,16 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
       ask_ids(n + 2);
     }
     if (masked && k0 >= wave_end) return;
-    const char* const ks = lds + (n & 1) * STAGE;
+    const uint32_t stage = stage0 + (n & 1) * STAGE;
+    const uint32_t ks = hidden(stage + l32 * (D * EB) + ((h2 ^ swizzle<CH>(l32)) * 16));
     v16f s[RT][KT];
 #pragma unroll
     for (int t = 0; t < KT; t++) {
 #pragma unroll
       for (int r = 0; r < RT; r++) s[r][t] = (v16f){0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-      const int row = 32 * t + l32;
 #pragma unroll
       for (int c = 0; c < CH / 2; c++) {
-        const F k = *(const F*)(ks + row * (D * EB) + (((h2 + 2 * c) ^ swizzle<CH>(row)) * 16));
+        const F k = at_lds<F>((ks ^ (2 * c * 16)) + 32 * t * (D * EB));
 #pragma unroll
         for (int r = 0; r < RT; r++) s[r][t] = Frag<T>::mma32(k, q[r][c], s[r][t]);
       }
@@ -586,7 +600,9 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
         }
       l[r] += sum;
     }
-    const char* const vs = ks + HALF;
+    const int vrow = 4 * h2 + (EB == 2 ? (lane & 15) / 4 : 0);
+    const uint32_t vs = EB == 2 ? hidden(stage + HALF + vrow * (D * EB) + ((2 * (lane >> 4 & 1) + (lane & 3) / 2 ^ swizzle<CH>(vrow)) * 16) + (lane & 1) * 8)
+                                : hidden(stage + HALF + vrow * (D * EB) + ((l32 / 4 ^ swizzle<CH>(vrow)) * 16) + (l32 & 3) * 4);
 #pragma unroll
     for (int t = 0; t < KT; t++) {
       constexpr int STEPS = EB == 2 ? 2 : 4;        // of 16 rows, or of 8
@@ -604,38 +620,22 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
           if constexpr (EB == 2) {
             union { F f; v4s half[2]; } x;
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-              const int row = 32 * t + 16 * u + 8 * j + 4 * h2 + (lane & 15) / 4, chunk = 4 * d + 2 * (lane >> 4 & 1) + (lane & 3) / 2;
-              x.half[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(lds_char*)(
-                  vs + row * (D * EB) + ((chunk ^ swizzle<CH>(row)) * 16) + (lane & 1) * 8));
-            }
+            for (int j = 0; j < 2; j++) x.half[j] = at_lds_turned((vs ^ ((4 * d ^ swizzle<CH>(8 * j)) * 16)) + (32 * t + 16 * u + 8 * j) * (D * EB));
             v = x.f;
           } else {
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-              const int row = 32 * t + 8 * u + 4 * h2 + j, chunk = 8 * d + l32 / 4;
-              v[j] = *(const float*)(vs + row * (D * EB) + ((chunk ^ swizzle<CH>(row)) * 16) + (l32 & 3) * 4);
-            }
+            for (int j = 0; j < 4; j++) v[j] = at_lds<float>((vs ^ ((8 * d ^ swizzle<CH>(8 * u + j)) * 16)) + (32 * t + 8 * u + j) * (D * EB));
           }
           if (masked && __any(not_finite<T>(v))) {
-            F up, down, no;
-#pragma unroll
-            for (int j = 0; j < N; j++) {
-              const float x = (float)v[j];
-              up[j] = (T)(x == INFINITY ? 1.f : 0.f);
-              down[j] = (T)(x == -INFINITY ? 1.f : 0.f);
-              no[j] = (T)(x != x ? 1.f : 0.f);
-              if (!(fabsf(x) < INFINITY)) v[j] = (T)0.f;
-            }
+            const F kinds = take_kinds<T>(&v);
 #pragma unroll
             for (int r = 0; r < RT; r++) {
               F one;
 #pragma unroll
-              for (int j = 0; j < N; j++) one[j] = (T)(seen[r] >> (32 * t + 4 * N * u / 2 + 8 * (j / 4) + 4 * h2 + j % 4) & 1 ? 1.f : 0.f);
-              const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-              const v16f x = Frag<T>::mma32(up, one, zero), y = Frag<T>::mma32(down, one, zero), z = Frag<T>::mma32(no, one, zero);
+              for (int j = 0; j < N; j++) one[j] = (T)(seen[r] >> (32 * t + 2 * N * u + 8 * (j / 4) + 4 * h2 + j % 4) & 1 ? 1.f : 0.f);
+              const v16f n = Frag<T>::mma32(kinds, one, (v16f){0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0});
 #pragma unroll
-              for (int i = 0; i < 16; i++) o[r][d][i] += (x[i] > 0.f ? INFINITY : 0.f) - (y[i] > 0.f ? INFINITY : 0.f) + (z[i] > 0.f ? NAN : 0.f);
+              for (int i = 0; i < 16; i++) o[r][d][i] += of_kinds(n[i]);
             }
           }
 #pragma unroll
@@ -653,11 +653,11 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
     l[r] += __shfl_xor(l[r], 32, 64);
     if (token[r] < 0) continue;
     const long long of = row0 + 32 * r + l32;
-    const long long slot = (long long)(it.from + it.piece) * a.c.heads + h, in = of - (long long)it.tile * ROWS;
+    const long long slot = it.slot, in = of - (long long)it.tile * ROWS;
     float* const part = a.part + (slot * ROWS + in) * a.c.d;
     T* const out = (T*)(const_cast<char*>(a.out.at) + (it.s.t0 + token[r]) * a.out.token + (h * a.group + (int)(of - (long long)token[r] * a.group)) * a.out.head);
     const float by = l[r] == 0.f ? 0.f : 1.f / l[r];
-    if (it.pieces > 1 && h2 == 0) {
+    if (it.slot >= 0 && h2 == 0) {
       float* const st = a.part + 2ll * a.slots * ROWS * a.c.d + (slot * ROWS + in) * 2;
       st[0] = m[r], st[1] = l[r];
     }
@@ -667,7 +667,7 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
       for (int k = 0; k < 4; k++) {
         const int e = 32 * d + 8 * k + 4 * h2;
         if (e >= a.c.d) continue;
-        if (it.pieces > 1) {
+        if (it.slot >= 0) {
           *(v4f*)(part + e) = (v4f){o[r][d][4 * k], o[r][d][4 * k + 1], o[r][d][4 * k + 2], o[r][d][4 * k + 3]};
         } else {
           Pack<T, 4> z;
@@ -677,6 +677,7 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
         }
       }
   }
+  }
 }
 
 // The pieces of a tile become its rows.  A workgroup takes `per` rows, `few` at a time: for each of them the pieces are shared out over the
@@ -685,12 +686,36 @@ template <typename T, int UNIT>
 __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per, int few) {
   __shared__ v4f sums[256];
   __shared__ float stat[256][2];
-  const int groups = rows / per, h = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads, first = rest % groups * per;
-  Item it;
-  if (!find_item<UNIT>(a, rows, rest / groups, true, &it)) return;
-  const long long there = (long long)it.s.n * a.group - (long long)it.tile * rows;
-  if (it.pieces <= 1) return;
-  const int pieces = min(it.pieces, kv_pieces(max(tile_end(a, it, rows), 1), it.size));
+  const KvPlan plan = plan_of<UNIT>(a, rows);
+  if (!plan.wgs) return;
+  const int groups = rows / per, first = blockIdx.x % groups * per;
+  // tile and head by number, over the batch
+  uint64_t number = blockIdx.x / groups, before = 0, units = 0, pair = 0;
+  KvSequence s;
+  bool found = false;
+  for (int b0 = 0; b0 < a.b.batch && !found; b0 += 64) {
+    const Share x = share_of<UNIT>(a, rows, b0 + (threadIdx.x & 63));
+    const uint64_t count = (uint64_t)x.tiles * a.c.heads, from = before + wave_sum_before(count), at = units + wave_sum_before(x.units);
+    const unsigned long long mine = __ballot(number >= from && number < from + count);
+    if (mine) {
+      const int l = __builtin_ctzll(mine);
+      s = {lane_of(x.s.t0, l), lane_of(x.s.n, l), lane_of(x.s.length, l), lane_of(x.s.base, l)};
+      pair = number - lane_of(from, l);
+      units = lane_of(at, l);
+      number = (uint32_t)lane_of(x.tiles, l);
+      found = true;
+    } else {
+      before = lane_of(from + count, 63);
+      units = lane_of(at + x.units, 63);
+    }
+  }
+  if (!found) return;
+  const int h = (int)(pair / number), tile = (int)(pair - (uint64_t)h * number);
+  const uint32_t whole = kv_units_of(s.length, UNIT);
+  const uint64_t start = units + pair * whole;
+  const int w0 = kv_holder(plan.units, plan.wgs, start), pieces = kv_holder(plan.units, plan.wgs, start + whole - 1) - w0 + 1;
+  if (pieces <= 1) return;
+  const long long there = (long long)s.n * a.group - (long long)tile * rows;
   const int quads = a.c.d / 4, share = 256 / (few * quads), e = threadIdx.x % (few * quads), part = threadIdx.x / (few * quads), c = e % quads;
   for (int r0 = first; r0 < first + per && r0 < there; r0 += few) {
     const int r = r0 + e / quads;
@@ -699,7 +724,7 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
     v4f y = {0, 0, 0, 0};
     if (mine)
       for (int p = part; p < pieces; p += share) {
-        const long long slot = (long long)(it.from + p) * a.c.heads + h;
+        const long long slot = 2 * (w0 + p) + (p == 0);
         const float* const st = a.part + 2ll * a.slots * rows * a.c.d + (slot * rows + r) * 2;
         const v4f x = *(const v4f*)(a.part + (slot * rows + r) * a.c.d + c * 4);
         const float top = fmaxf(m, st[0]), safe = top == -INFINITY ? 0.f : top;
@@ -723,12 +748,12 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
       sum += f * stat[p * few * quads + e][1];
       y += f * sums[p * few * quads + e];
     }
-    const long long of = (long long)it.tile * rows + r;
+    const long long of = (long long)tile * rows + r;
     const int i = (int)(of / a.group), g = (int)(of - (long long)i * a.group);
     Pack<T, 4> z;
 #pragma unroll
     for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(sum == 0.f ? 0.f : y[j] / sum);
-    *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + (it.s.t0 + i) * a.out.token + (h * a.group + g) * a.out.head) + c * 4) = z;
+    *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + (s.t0 + i) * a.out.token + (h * a.group + g) * a.out.head) + c * 4) = z;
   }
 }
 
@@ -743,17 +768,21 @@ int attend_args(const pahq_kv_cache* cache, const pahq_kv_batch* batch, int q_he
   return PAHQ_OK;
 }
 
-// How a call is cut: the tile's rows, and pieces for so many workgroups, none shorter than `least` rows of the cache
+// How a call is cut: the tile's rows, and ranges for so many workgroups, none shorter than `least` units
 struct Cut { int rows, slots, least; };
 Cut cut_of(const AttendArgs& a) {
   Cut k;
   const long long mean = (((long long)a.b.tokens + a.b.batch - 1) / std::max(a.b.batch, 1)) * a.group;      // rows a sequence and head
   k.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : 128;
+#ifdef SLOTS
+  k.slots = SLOTS; k.least = LEAST;
+#else
   k.slots = 512;
-  k.least = k.rows <= 32 ? 256 : 512;
+  k.least = 4;
+#endif
   // the new tokens alone are so much work that a piece is as long as any sequence can be
   const double work = (double)a.b.tokens * a.b.tokens * a.group / ((double)k.rows * std::max(a.b.batch, 1)) * a.c.heads / k.slots;
-  if (a.b.most <= k.least || a.b.most <= work) k.slots = 0;
+  if (a.b.most <= 256 || a.b.most <= work) k.slots = 0;
   return k;
 }
 size_t part_bytes(const AttendArgs& a, const Cut& k) { return k.slots ? 2ull * k.slots * k.rows * (a.c.d + 2) * 4 : 0; }
@@ -777,7 +806,7 @@ template <typename T, int D>
 int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
   constexpr int EB = sizeof(T), WIDE = D * EB, NW = WIDE <= 128 ? 4 : 2, FEW = 2 * NW * 2 * (EB == 2 ? 32 : 16) * WIDE + NW * 1024;
   constexpr int KVB = WIDE <= 256 ? 64 : 32, FEW_UNIT = (EB == 2 ? 32 : 16) * NW;
-  const long long tiles = kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows), items = k.slots ? kv_most_items(tiles, a.c.heads, k.slots) : tiles;
+  const long long tiles = kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows), items = std::max<long long>(tiles * a.c.heads, k.slots);
   // rows of a workgroup that joins: one where that is not too many workgroups
   const int most = std::max(1, 256 / (a.c.d / 4));
   int per = 1;
@@ -785,8 +814,8 @@ int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
   int few = 1;
   while (few * 2 <= std::min(per, most)) few *= 2;
   // threads of a launch are counted in 32 bits
-  if (items * a.c.heads >= KV_MOST_ITEMS || tiles * a.c.heads * (k.rows / per) >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
-  const unsigned grid = (unsigned)(items * a.c.heads);
+  if (items >= KV_MOST_ITEMS || tiles * a.c.heads * (k.rows / per) >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
+  const unsigned grid = (unsigned)items;
   const int rc = k.rows == 16   ? launch<kv_few_k<T, D, 1, NW>, NW * 64, FEW>(st, grid, a)
                  : k.rows == 32 ? launch<kv_few_k<T, D, 2, NW>, NW * 64, FEW>(st, grid, a)
                                 : launch<kv_tile_k<T, D, 1, KVB>, 256, 4 * KVB * WIDE + 2048>(st, grid, a);
