@@ -34,44 +34,34 @@ struct AttendArgs {
 
 // ---------------------------------------------------------------- a workgroup's part
 __device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
-__device__ __forceinline__ uint64_t lane_of(uint64_t v, int l) {
-  return (uint64_t)(uint32_t)lane_of((int)(v >> 32), l) << 32 | (uint32_t)lane_of((int)v, l);
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
+// Sums up to and with the own lane, sticking at 2^32 - 1: shifts by 1, 2, 4, 8 in rows of 16 lanes, then a row's last lane to the next row
+// and the second row's to the last two
+__device__ __forceinline__ uint32_t wave_sum_up_to(uint32_t v) {
+#define STEP(control, rows) v = __builtin_elementwise_add_sat(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, control, rows, 0xF, false))
+  STEP(0x111, 0xF);
+  STEP(0x112, 0xF);
+  STEP(0x114, 0xF);
+  STEP(0x118, 0xF);
+  STEP(0x142, 0xA);
+  STEP(0x143, 0xC);
+#undef STEP
+  return v;
 }
-template <typename N> __device__ __forceinline__ N wave_sum_before(N v) {        // of the lanes in front
-  N s = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const N u = __shfl_up(s, o, 64);
-    if ((int)(threadIdx.x & 63) >= o) s += u;
-  }
-  return s - v;
-}
-// A sequence in a lane, 64 of them at a time
-struct Share { KvSequence s; int tiles; uint64_t units; };            // units: of all its tiles and heads
-template <int UNIT> __device__ __forceinline__ Share share_of(const AttendArgs& a, int rows, int b) {
+// Sequences in lanes, 64 at a time from b0 on, and the sums of their tiles (with heads) and units up to and with each
+struct Share { KvSequence s; int tiles; uint32_t pairs, units, pairs_to, units_to; };
+template <int UNIT> __device__ __forceinline__ Share share_of(const AttendArgs& a, int rows, int b0, uint32_t pairs_before, uint32_t units_before) {
+  const int b = b0 + (threadIdx.x & 63);
   Share x = {};
   if (b < a.b.batch) {
     x.s = kv_sequence(a.b, b);
     x.tiles = kv_tiles((long long)x.s.n * a.group, rows);
-    x.units = kv_units(x.tiles, a.c.heads, x.s.length, UNIT);
+    x.pairs = kv_pairs(x.tiles, a.c.heads);
+    x.units = kv_units(x.pairs, x.s.length, UNIT);
   }
+  x.pairs_to = __builtin_elementwise_add_sat(wave_sum_up_to(x.pairs), pairs_before);
+  x.units_to = __builtin_elementwise_add_sat(wave_sum_up_to(x.units), units_before);
   return x;
-}
-template <int UNIT> __device__ KvPlan plan_of(const AttendArgs& a, int rows) {
-  if (!a.slots) return {0, 0};
-  uint64_t units = 0;
-  int longest = 0;
-  for (int b = threadIdx.x & 63; b < a.b.batch; b += 64) {
-    const Share x = share_of<UNIT>(a, rows, b);
-    units += x.units;
-    if (x.tiles) longest = max(longest, kv_units_of(x.s.length, UNIT));
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    units += __shfl_xor(units, o, 64);
-    longest = max(longest, __shfl_xor(longest, o, 64));
-  }
-  return kv_plan(lane_of(units, 0), lane_of(longest, 0), a.slots, a.least);
 }
 struct Item {
   KvSequence s;
@@ -83,42 +73,65 @@ __device__ __forceinline__ int tile_end(const AttendArgs& a, const KvSequence& s
   const int last = min(s.n - 1, (int)((((long long)tile + 1) * rows - 1) / a.group));
   return max(s.base + last + 1, 0);
 }
-// What workgroup `wg` of the plan does at `at`, up to `stop` at most: units in front of `at` are done.  Returns how many it takes, 0 if there
-// is nothing.  Without ranges the units are tiles, those of a cache head apart.
-template <int UNIT> __device__ uint64_t next_item(const AttendArgs& a, int rows, const KvPlan& p, int wg, uint64_t at, uint64_t stop, Item* it) {
-  uint64_t before = 0;
-  for (int b0 = 0; b0 < a.b.batch; b0 += 64) {
-    const Share x = share_of<UNIT>(a, rows, b0 + (threadIdx.x & 63));
-    const uint64_t count = p.wgs ? x.units : (uint64_t)x.tiles, from = before + wave_sum_before(count);
-    const unsigned long long mine = __ballot(at >= from && at < from + count);
-    if (mine) {
-      const int l = __builtin_ctzll(mine), tiles = lane_of(x.tiles, l);
-      const uint64_t local = at - lane_of(from, l);
-      it->b = b0 + l;
-      it->s = {lane_of(x.s.t0, l), lane_of(x.s.n, l), lane_of(x.s.length, l), lane_of(x.s.base, l)};
-      it->begin = 0;
-      it->slot = -1;
-      if (!p.wgs) {                                 // the last tiles see the most rows and come first
-        it->h = wg;
-        it->tile = tiles - 1 - (int)local;
-        it->end = tile_end(a, it->s, it->tile, rows);
-        return 1;
-      }
-      const uint32_t whole = kv_units_of(it->s.length, UNIT);
-      const uint64_t pair = local / whole;
-      const uint32_t off = (uint32_t)(local - pair * whole), take = (uint32_t)min((uint64_t)(whole - off), stop - at);
-      it->h = (int)(pair / (uint32_t)tiles);
-      it->tile = (int)(pair - (uint64_t)it->h * tiles);
-      it->end = tile_end(a, it->s, it->tile, rows);
-      it->begin = min((int)min((uint64_t)off * UNIT, (uint64_t)KV_MAX_LENGTH), it->end);
-      if (off + take < whole) it->end = min(it->end, (int)((off + take) * UNIT));
-      if (take < whole) it->slot = 2 * wg + (off ? 0 : 1);
-      return take;
+// Where a workgroup finds its part; every wave looks by itself.  Of up to 64 sequences KEEP keeps what was read.
+template <int UNIT, bool KEEP> struct Finder {
+  Share x;
+  KvPlan plan;
+  __device__ __forceinline__ bool kept(const AttendArgs& a) const { return KEEP && a.b.batch <= 64; }
+  __device__ __forceinline__ void look(const AttendArgs& a, int rows) {
+    uint32_t pairs = 0, units = 0;
+    int longest = 0;
+    for (int b0 = 0; b0 < a.b.batch && (a.slots || kept(a)); b0 += 64) {
+      x = share_of<UNIT>(a, rows, b0, pairs, units);
+      pairs = lane_of(x.pairs_to, 63);
+      units = lane_of(x.units_to, 63);
+      longest = max(longest, x.tiles ? kv_units_of(x.s.length, UNIT) : 0);
     }
-    before = lane_of(from + count, 63);
+    // a tile longer than the average range, somewhere: asked for every lane's longest
+    const uint32_t even = a.slots ? units / (uint32_t)a.slots : 0;
+    plan = kv_plan(units, a.slots && __any((uint32_t)longest > even), a.slots, a.least);
   }
-  return 0;
-}
+  // Sequence with the `at`-th unit, or tile and head where tiles are given out whole: its lane of x, -1 for none
+  __device__ __forceinline__ int lane_with(const AttendArgs& a, int rows, uint32_t at, bool by_units, int* b0) {
+    uint32_t pairs = 0, units = 0;
+    for (*b0 = 0; *b0 < a.b.batch; *b0 += 64) {
+      if (!kept(a)) x = share_of<UNIT>(a, rows, *b0, pairs, units);
+      const unsigned long long behind = __ballot(at < (by_units ? x.units_to : x.pairs_to));
+      if (behind) return __builtin_ctzll(behind);
+      pairs = lane_of(x.pairs_to, 63);
+      units = lane_of(x.units_to, 63);
+    }
+    return -1;
+  }
+  __device__ __forceinline__ KvSequence sequence(int l) const { return {lane_of(x.s.t0, l), lane_of(x.s.n, l), lane_of(x.s.length, l), lane_of(x.s.base, l)}; }
+  // What workgroup `wg` does at `at`, up to `stop` at most.  Returns how many units it takes, 0 if there is nothing.
+  __device__ __forceinline__ uint32_t next(const AttendArgs& a, int rows, int wg, uint32_t at, uint32_t stop, Item* it) {
+    int b0;
+    const int l = lane_with(a, rows, at, plan.wgs, &b0);
+    if (l < 0) return 0;
+    const uint32_t tiles = lane_of(x.tiles, l);
+    it->b = b0 + l;
+    it->s = sequence(l);
+    it->begin = 0;
+    it->slot = -1;
+    if (!plan.wgs) {                                // heads in turn, and the last tiles, which see the most rows, first
+      const uint32_t local = at - (lane_of(x.pairs_to, l) - lane_of(x.pairs, l)), heads = a.c.heads;
+      it->h = local % heads;
+      it->tile = tiles - 1 - local / heads;
+      it->end = tile_end(a, it->s, it->tile, rows);
+      return 1;
+    }
+    const uint32_t local = at - (lane_of(x.units_to, l) - lane_of(x.units, l)), whole = kv_units_of(it->s.length, UNIT), pair = local / whole;
+    const uint32_t off = local - pair * whole, take = min(whole - off, stop - at);
+    it->h = pair / tiles;
+    it->tile = pair - it->h * tiles;
+    it->end = tile_end(a, it->s, it->tile, rows);
+    it->begin = (int)min((uint32_t)min((uint64_t)off * UNIT, (uint64_t)KV_MAX_LENGTH), (uint32_t)it->end);
+    if (off + take < whole) it->end = min(it->end, (int)((off + take) * UNIT));
+    if (take < whole) it->slot = 2 * wg + (off ? 0 : 1);
+    return take;
+  }
+};
 // Bit x: whether new token i (row t of the operator's) sees row k0 + x of the cache
 __device__ __forceinline__ unsigned long long seen_bits(const AttendArgs& a, const KvSequence& s, int i, int k0, int end) {
   auto low = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
@@ -249,14 +262,15 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   extern __shared__ __align__(1024) char lds[];       // [NW][2][STAGE], [NW][4][64] pages' numbers
   __shared__ float stat[NW][ROWS][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, h4 = lane >> 4;
-  const KvPlan plan = plan_of<KVB * NW>(a, ROWS);
-  const int wg = plan.wgs ? kv_wg_of(blockIdx.x, plan.wgs) : (int)(blockIdx.x % a.c.heads);
+  Finder<KVB * NW, true> f;
+  f.look(a, ROWS);
+  const int wg = f.plan.wgs ? kv_wg_of(blockIdx.x, f.plan.wgs) : 0;
   if (wg < 0) return;
-  uint64_t at = plan.wgs ? kv_from(plan.units, plan.wgs, wg) : blockIdx.x / a.c.heads;
-  const uint64_t stop = plan.wgs ? kv_from(plan.units, plan.wgs, wg + 1) : at + 1;
+  uint32_t at = f.plan.wgs ? kv_from(f.plan, wg) : blockIdx.x;
+  const uint32_t stop = f.plan.wgs ? kv_from(f.plan, wg + 1) : at + 1;
   for (bool first = true; at < stop; first = false) {
   Item it;
-  const uint64_t take = next_item<KVB * NW>(a, ROWS, plan, wg, at, stop, &it);
+  const uint32_t take = f.next(a, ROWS, wg, at, stop, &it);
   if (!take) return;
   at += take;
   const int begin = it.begin, end = it.end, h = it.h;
@@ -478,14 +492,15 @@ __global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void 
   static_assert(ASKS >= 1 && MINE * CH == ASKS * 64 && KVB <= 64, "a wave asks for whole rows");
   extern __shared__ __align__(1024) char lds[];       // [2][STAGE], [NW][2][64] pages' numbers
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h2 = lane >> 5;
-  const KvPlan plan = plan_of<KVB>(a, ROWS);
-  const int wg = plan.wgs ? kv_wg_of(blockIdx.x, plan.wgs) : (int)(blockIdx.x % a.c.heads);
+  Finder<KVB, false> f;
+  f.look(a, ROWS);
+  const int wg = f.plan.wgs ? kv_wg_of(blockIdx.x, f.plan.wgs) : 0;
   if (wg < 0) return;
-  uint64_t at = plan.wgs ? kv_from(plan.units, plan.wgs, wg) : blockIdx.x / a.c.heads;
-  const uint64_t stop = plan.wgs ? kv_from(plan.units, plan.wgs, wg + 1) : at + 1;
+  uint32_t at = f.plan.wgs ? kv_from(f.plan, wg) : blockIdx.x;
+  const uint32_t stop = f.plan.wgs ? kv_from(f.plan, wg + 1) : at + 1;
   for (bool first = true; at < stop; first = false) {
   Item it;
-  const uint64_t take = next_item<KVB>(a, ROWS, plan, wg, at, stop, &it);
+  const uint32_t take = f.next(a, ROWS, wg, at, stop, &it);
   if (!take) return;
   at += take;
   const int begin = it.begin, end = it.end, h = it.h;
@@ -686,38 +701,22 @@ template <typename T, int UNIT>
 __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per, int few) {
   __shared__ v4f sums[256];
   __shared__ float stat[256][2];
-  const KvPlan plan = plan_of<UNIT>(a, rows);
-  if (!plan.wgs) return;
-  const int groups = rows / per, first = blockIdx.x % groups * per;
-  // tile and head by number, over the batch
-  uint64_t number = blockIdx.x / groups, before = 0, units = 0, pair = 0;
-  KvSequence s;
-  bool found = false;
-  for (int b0 = 0; b0 < a.b.batch && !found; b0 += 64) {
-    const Share x = share_of<UNIT>(a, rows, b0 + (threadIdx.x & 63));
-    const uint64_t count = (uint64_t)x.tiles * a.c.heads, from = before + wave_sum_before(count), at = units + wave_sum_before(x.units);
-    const unsigned long long mine = __ballot(number >= from && number < from + count);
-    if (mine) {
-      const int l = __builtin_ctzll(mine);
-      s = {lane_of(x.s.t0, l), lane_of(x.s.n, l), lane_of(x.s.length, l), lane_of(x.s.base, l)};
-      pair = number - lane_of(from, l);
-      units = lane_of(at, l);
-      number = (uint32_t)lane_of(x.tiles, l);
-      found = true;
-    } else {
-      before = lane_of(from + count, 63);
-      units = lane_of(at + x.units, 63);
-    }
-  }
-  if (!found) return;
-  const int h = (int)(pair / number), tile = (int)(pair - (uint64_t)h * number);
-  const uint32_t whole = kv_units_of(s.length, UNIT);
-  const uint64_t start = units + pair * whole;
-  const int w0 = kv_holder(plan.units, plan.wgs, start), pieces = kv_holder(plan.units, plan.wgs, start + whole - 1) - w0 + 1;
+  Finder<UNIT, true> find;
+  find.look(a, rows);
+  if (!find.plan.wgs) return;
+  const uint32_t groups = rows / per, number = blockIdx.x / groups, first = blockIdx.x % groups * per;
+  int b0;
+  const int lane = find.lane_with(a, rows, number, false, &b0);
+  if (lane < 0) return;
+  const KvSequence s = find.sequence(lane);
+  const uint32_t tiles = lane_of(find.x.tiles, lane), pair = number - (lane_of(find.x.pairs_to, lane) - lane_of(find.x.pairs, lane));
+  const int h = pair / tiles, tile = pair - h * tiles;
+  const uint32_t whole = kv_units_of(s.length, UNIT), start = lane_of(find.x.units_to, lane) - lane_of(find.x.units, lane) + pair * whole;
+  const int w0 = kv_holder(find.plan, start), pieces = kv_holder(find.plan, start + whole - 1) - w0 + 1;
   if (pieces <= 1) return;
   const long long there = (long long)s.n * a.group - (long long)tile * rows;
   const int quads = a.c.d / 4, share = 256 / (few * quads), e = threadIdx.x % (few * quads), part = threadIdx.x / (few * quads), c = e % quads;
-  for (int r0 = first; r0 < first + per && r0 < there; r0 += few) {
+  for (int r0 = first; r0 < (int)first + per && r0 < there; r0 += few) {
     const int r = r0 + e / quads;
     const bool mine = part < share && r < there;
     float m = -INFINITY, l = 0.f;
@@ -733,7 +732,7 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
         l = l * f + st[1] * g;
         m = top;
       }
-    if (r0 > first) __syncthreads();
+    if (r0 > (int)first) __syncthreads();
     sums[threadIdx.x] = y;
     stat[threadIdx.x][0] = m, stat[threadIdx.x][1] = l;
     __syncthreads();

@@ -23,33 +23,36 @@ namespace pahq {
 constexpr int KV_MOST_ITEMS = 1 << 24;              // workgroups of a launch, whose threads are counted in 32 bits
 PAHQ_HD int kv_tiles(long long rows, int tile) { return (int)((rows + tile - 1) / tile); }
 PAHQ_HD int kv_units_of(int length, int unit) { return length <= unit ? 1 : (int)(((uint32_t)length + (uint32_t)unit - 1) / (uint32_t)unit); }
-// Of a sequence; starts that do not grow can name more tiles than there are, and no sum over a batch may pass 64 bits
-PAHQ_HD uint64_t kv_units(int tiles, int heads, int length, int unit) {
-  const uint64_t pairs = (uint64_t)(uint32_t)tiles * (uint32_t)heads, most = 1ull << 47, each = (uint64_t)kv_units_of(length, unit);
-  return pairs < most / each ? pairs * each : most;
+// Of a sequence: tiles of all heads, and their units.  Sums over a batch stick at 2^32 - 1, with more units than that tiles are given out
+// whole; starts that do not grow can name more tiles than there are, which is why a sequence's own are bounded.
+PAHQ_HD uint32_t kv_pairs(int tiles, int heads) {
+  const uint64_t pairs = (uint64_t)(uint32_t)tiles * (uint32_t)heads;
+  return pairs < KV_MOST_ITEMS ? (uint32_t)pairs : (uint32_t)KV_MOST_ITEMS;
+}
+PAHQ_HD uint32_t kv_units(uint32_t pairs, int length, int unit) {
+  const uint64_t units = (uint64_t)pairs * (uint32_t)kv_units_of(length, unit);
+  return units < 0xFFFFFFFFull ? (uint32_t)units : 0xFFFFFFFFu;
 }
 
-struct KvPlan { uint64_t units; int wgs; };        // wgs 0: tiles are given out whole
-PAHQ_HD KvPlan kv_plan(uint64_t units, int longest, int slots, int least) {
-  if ((uint64_t)(uint32_t)longest * (uint32_t)slots <= units) return {units, 0};
-  const uint64_t parts = units / (uint32_t)least;
-  return {units, parts >= (uint64_t)slots ? slots : parts > 1 ? (int)parts : 1};
+struct KvPlan { uint32_t units, wgs; };            // wgs 0: tiles are given out whole
+// uneven: some tile is longer than units / slots
+PAHQ_HD KvPlan kv_plan(uint32_t units, bool uneven, int slots, int least) {
+  if (!uneven || units == 0xFFFFFFFFu) return {units, 0};
+  const uint32_t parts = units / (uint32_t)least;
+  return {units, parts >= (uint32_t)slots ? (uint32_t)slots : parts > 1 ? parts : 1u};
 }
 // Where range w begins: units * w / wgs, rounded down
-PAHQ_HD uint64_t kv_from(uint64_t units, int wgs, int w) {
-  const uint64_t each = units / (uint32_t)wgs, rest = units - each * (uint32_t)wgs;
-  return each * (uint32_t)w + rest * (uint32_t)w / (uint32_t)wgs;
-}
+PAHQ_HD uint32_t kv_from(const KvPlan& p, uint32_t w) { return (uint32_t)((uint64_t)p.units * w / p.wgs); }
 // Whose range a unit lies in: the last w that begins at or in front of it
-PAHQ_HD int kv_holder(uint64_t units, int wgs, uint64_t unit) {
-  const uint64_t w = ((unit + 1) * (uint32_t)wgs - 1) / units;
-  return w < (uint64_t)wgs ? (int)w : wgs - 1;      // also where a batch that makes no sense has more units than that holds
+PAHQ_HD int kv_holder(const KvPlan& p, uint32_t unit) {
+  const uint64_t w = (((uint64_t)unit + 1) * p.wgs - 1) / p.units;
+  return w < p.wgs ? (int)w : (int)p.wgs - 1;
 }
 // The range of a workgroup of the launch, -1 for none: neighbouring ranges, which share rows of the cache where tiles do, on one of the eight
 // XCDs, to which workgroups go in turn
-PAHQ_HD int kv_wg_of(unsigned block, int wgs) {
-  const unsigned each = ((unsigned)wgs + 7) / 8, w = block % 8 * each + block / 8;
-  return block / 8 < each && w < (unsigned)wgs ? (int)w : -1;
+PAHQ_HD int kv_wg_of(uint32_t block, uint32_t wgs) {
+  const uint32_t each = (wgs + 7) / 8, w = block % 8 * each + block / 8;
+  return block / 8 < each && w < wgs ? (int)w : -1;
 }
 
 // For the worst case: every sequence that has tokens ends in a tile of its own
