@@ -19,6 +19,9 @@
 #include "kv.h"
 #include "kv_plan.h"
 
+#ifndef JB
+#define JB 2048
+#endif
 namespace pahq {
 
 struct AttendArgs {
@@ -31,6 +34,18 @@ struct AttendArgs {
   float* part;                                      // [slot][rows][d] sums of a part, then [slot][rows][2] maximum and sum
   int slots, least;                                 // of ranges (kv_plan.h); slots 0: nothing is cut
 };
+
+// The kernel's one argument, read again where it is asked for: kept for the whole kernel it would take more scalar registers than there are.
+// The kernels take nothing but it, so it begins their argument memory.
+__device__ __forceinline__ AttendArgs args_again() {
+  uintptr_t p = (uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  static_assert(sizeof(AttendArgs) % 8 == 0, "whole words");
+  struct Words { uint64_t w[sizeof(AttendArgs) / 8]; } x;
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(AttendArgs) / 8; i++) x.w[i] = ((const __attribute__((address_space(4))) uint64_t*)p)[i];
+  return __builtin_bit_cast(AttendArgs, x);
+}
 
 // ---------------------------------------------------------------- a workgroup's part
 __device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
@@ -132,17 +147,25 @@ template <int UNIT, bool KEEP> struct Finder {
     return take;
   }
 };
-// Bit x: whether new token i (row t of the operator's) sees row k0 + x of the cache
+// Bit x: whether new token i sees row k0 + x of the cache; none for i < 0.  Without branches: lanes part here otherwise, and registers that
+// hold what is every lane's are not safe in the compiler's hands where lanes are off.
 __device__ __forceinline__ unsigned long long seen_bits(const AttendArgs& a, const KvSequence& s, int i, int k0, int end) {
-  auto low = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
-  if (!a.tree) return low(min(s.base + i + 1, end) - k0);
-  unsigned long long m = low(s.base - k0);
+  auto low = [](int n) { return n >= 64 ? ~0ull : (1ull << max(n, 0)) - 1; };
+  const unsigned long long here = low(end - k0) & (i < 0 ? 0ull : ~0ull);
+  if (!a.tree) return low(s.base + i + 1 - k0) & here;
   const int ahead = k0 - s.base, word = ahead >> 6, shift = ahead & 63;            // rounded down
-  const unsigned long long* const w = a.tree + (long long)(s.t0 + i) * a.words;
-  if (word >= 0 && word < a.words) m |= w[word] >> shift;
-  if (shift && word + 1 >= 0 && word + 1 < a.words) m |= w[word + 1] << (64 - shift);
-  return m & low(end - k0);
+  const unsigned long long* const w = a.tree + (long long)(s.t0 + max(i, 0)) * a.words;
+  const unsigned long long first = w[min(max(word, 0), a.words - 1)], second = w[min(max(word + 1, 0), a.words - 1)];
+  const unsigned long long of_first = word >= 0 && word < a.words ? ~0ull : 0ull, of_second = shift && word + 1 >= 0 && word + 1 < a.words ? ~0ull : 0ull;
+  return (low(s.base - k0) | (first >> shift & of_first) | (second << (64 - shift & 63) & of_second)) & here;
 }
+// x where bit n of seen is set, else -infinity
+__device__ __forceinline__ float seen_score(uint32_t seen, int n, float x) {
+  const uint32_t keep = (uint32_t)((int)(seen << (31 - n)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & keep) | (0xFF800000u & ~keep));
+}
+
+#define INLINE __attribute__((always_inline))
 
 // ---------------------------------------------------------------- fragments
 // Sixteen bytes of a row are one operand of a step of the 16-bit products and of four steps of the fp32 products
@@ -175,6 +198,20 @@ template <> struct Frag<float> {
 // fp16 weights: times 2^7, so that those 2^-21 of the largest are still normal numbers, and 2^15 is the largest (the maximum lags by up to 2^8)
 template <typename T> constexpr float LIFT = sizeof(T) == 2 && !__is_same(T, bf16_t) ? 7.f : 0.f;
 constexpr float LAG = 8.f;
+constexpr float OVER = 32768.f;
+// acc + the sum of a fragment's elements
+__device__ __forceinline__ float sum_of(v8bf x, float acc) {
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) acc = __builtin_amdgcn_fdot2_f32_bf16((v2bf){x[j], x[j + 1]}, (v2bf){(__bf16)1.f, (__bf16)1.f}, acc, false);
+  return acc;
+}
+__device__ __forceinline__ float sum_of(v8h x, float acc) {
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) acc = __builtin_amdgcn_fdot2((v2h){x[j], x[j + 1]}, (v2h){(_Float16)1.f, (_Float16)1.f}, acc, false);
+  return acc;
+}
+__device__ __forceinline__ float sum_of(v4f x, float acc) { return acc + ((x[0] + x[1]) + (x[2] + x[3])); }
 
 alignas(16) __device__ const uint32_t kv_chunk[4][4] = {{0, 0, 0, 0}, {0x7FC00000, 0x7FC00000, 0x7FC00000, 0x7FC00000},
                                                         {0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0}, {0x7E007E00, 0x7E007E00, 0x7E007E00, 0x7E007E00}};
@@ -208,23 +245,23 @@ __device__ __forceinline__ long long row_at(const KvCache& c, int row, int end, 
   const int slot = row - (int)((unsigned long long)(uint32_t)row * c.magic >> c.shift) * c.page_size;
   return (uint32_t)page < (uint32_t)c.pages ? page * c.page + slot * c.slot : ROW_NONE;
 }
-// Rows r0 .. of the block, 64 / CH of them (r0 a multiple of that), chunk by chunk: lane l writes the l-th 16 bytes behind lds.  Their
-// offsets lie in lanes `first` and on.
-template <typename T, int CH, bool ONCE>
-__device__ __forceinline__ void ask_rows(const KvCache& c, long long head, long long mine, int first, int r0, uint32_t lds_k, uint32_t lds_v) {
-  const int lane = threadIdx.x & 63;
+// Rows r0 .. of a block, 64 / CH of them (r0 a multiple of that), chunk by chunk: lane l writes the l-th 16 bytes behind lds.  Their
+// offsets lie in lanes `first` and on.  A lane's chunk: bytes behind the head's first row, or what stands for a chunk that is none.
+struct Chunk { long long off; const char* fill; };
+template <typename T, int CH> __device__ __forceinline__ Chunk chunk_of(const KvCache& c, int lane, long long mine, int first, int r0) {
   const int chunk = (lane % CH ^ swizzle<CH>(lane / CH)) ^ swizzle<CH>(r0);
-  const long long at = (long long)__shfl((unsigned long long)mine, first + lane / CH, 64), off = at + chunk * 16;
-  const char *k = c.keys + head + off, *v = c.values + head + off;
-  if (at < 0 || chunk * 16 >= c.d * (int)sizeof(T)) k = v = (const char*)kv_chunk[at == ROW_NONE && chunk * 16 < c.d * (int)sizeof(T) ? NAN_CHUNK<T> : 0];
-  if (ONCE) {
-    slab_load16_nt((const uint8_t*)k, lds_k);
-    slab_load16_nt((const uint8_t*)v, lds_v);
-  } else {
-    slab_load16((const uint8_t*)k, lds_k);
-    slab_load16((const uint8_t*)v, lds_v);
-  }
+  const long long at = (long long)__shfl((unsigned long long)mine, first + lane / CH, 64);
+  const bool behind = chunk * 16 >= c.d * (int)sizeof(T);
+  return {at + chunk * 16, at < 0 || behind ? (const char*)kv_chunk[at == ROW_NONE && !behind ? NAN_CHUNK<T> : 0] : nullptr};
 }
+template <bool ONCE> __device__ __forceinline__ void ask_chunk(const char* from, const Chunk& x, uint32_t lds) {
+  const uint8_t* const at = (const uint8_t*)(x.fill ? x.fill : from + x.off);
+  if (ONCE) slab_load16_nt(at, lds);
+  else slab_load16(at, lds);
+}
+
+// Nothing but arithmetic outside of the matrix cores may be moved across
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0x6); }
 
 // Values that some query of the tile does not see may be infinities or NaN, and 0 * NaN is one.  They leave the product, and come back
 // through another one, of which kinds a query sees: up to 32 rows count 1 each for infinity, 64 for -infinity, 4096 for NaN.
@@ -239,15 +276,18 @@ template <typename T, typename F> __device__ __forceinline__ F take_kinds(F* v) 
 #pragma unroll
   for (int j = 0; j < 16 / (int)sizeof(T); j++) {
     const float x = (float)(*v)[j];
-    const bool fine = fabsf(x) < INFINITY;
-    kinds[j] = (T)(fine ? 0.f : x == INFINITY ? 1.f : x == -INFINITY ? 64.f : 4096.f);
-    if (!fine) (*v)[j] = (T)0.f;
+    const uint32_t fine = fabsf(x) < INFINITY ? ~0u : 0u, up = x == INFINITY ? 0x3F800000u : 0u, down = x == -INFINITY ? 0x42800000u : 0u, no = x != x ? 0x45800000u : 0u;
+    kinds[j] = (T)__uint_as_float(up | down | no);            // 1, 64, 4096
+    (*v)[j] = (T)__uint_as_float(__float_as_uint(x) & fine);
   }
   return kinds;
 }
+// 1 where a bit is set, else 0
+template <typename T> __device__ __forceinline__ T one_bit(uint32_t seen, int n) { return (T)__uint_as_float((seen >> n & 1u) * 0x3F800000u); }
 __device__ __forceinline__ float of_kinds(float count) {
   const int n = (int)count;
-  return n == 0 ? 0.f : n < 64 ? INFINITY : (n & 63) || n >= 4096 ? NAN : -INFINITY;
+  const uint32_t up = (n & 63) ? 0x7F800000u : 0u, down = (n & 4032) ? 0xFF800000u : 0u, no = n >= 4096 ? 0x7FC00000u : 0u;
+  return __uint_as_float(up) + __uint_as_float(down) + __uint_as_float(no);        // inf - inf: NaN
 }
 
 // ---------------------------------------------------------------- up to 16 RT rows of queries
@@ -263,36 +303,40 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   __shared__ float stat[NW][ROWS][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, h4 = lane >> 4;
   Finder<KVB * NW, true> f;
-  f.look(a, ROWS);
+  f.look(args_again(), ROWS);
   const int wg = f.plan.wgs ? kv_wg_of(blockIdx.x, f.plan.wgs) : 0;
   if (wg < 0) return;
   uint32_t at = f.plan.wgs ? kv_from(f.plan, wg) : blockIdx.x;
   const uint32_t stop = f.plan.wgs ? kv_from(f.plan, wg + 1) : at + 1;
   for (bool first = true; at < stop; first = false) {
   Item it;
-  const uint32_t take = f.next(a, ROWS, wg, at, stop, &it);
+  const uint32_t take = f.next(args_again(), ROWS, wg, at, stop, &it);
   if (!take) return;
   at += take;
   const int begin = it.begin, end = it.end, h = it.h;
   if (!first) __syncthreads();                      // the stages held the last tile's sums
 
-  // the tile's queries: lane l16 of row tile r holds chunks h4, h4 + 4, ... of row 16 r + l16
+  // the tile's queries: lane l16 of row tile r holds chunks h4, h4 + 4, ... of row 16 r + l16; zeros where there is none, from memory that is there
+  const int group = a.group;
   int token[RT];
   F q[RT][CH / 4];
+  {
+    const AttendArgs k = args_again();
 #pragma unroll
-  for (int r = 0; r < RT; r++) {
-    const long long row = (long long)it.tile * ROWS + 16 * r + l16;
-    const bool there = row < (long long)it.s.n * a.group;
-    token[r] = there ? (int)(row / a.group) : -1;
-    const int g = (int)(row - (long long)(there ? token[r] : 0) * a.group);
-    const T* const x = (const T*)(a.q.at + (it.s.t0 + (there ? token[r] : 0)) * a.q.token + (h * a.group + (there ? g : 0)) * a.q.head);
+    for (int r = 0; r < RT; r++) {
+      const long long row = (long long)it.tile * ROWS + 16 * r + l16;
+      const bool there = row < (long long)it.s.n * group;
+      token[r] = there ? (int)(row / group) : -1;
+      const int t = there ? token[r] : 0, g = there ? (int)(row - (long long)t * group) : 0;
+      const T* const x = (const T*)(k.q.at + (it.s.t0 + t) * k.q.token + (h * group + g) * k.q.head);
 #pragma unroll
-    for (int s = 0; s < CH / 4; s++) {
-      const int e0 = (h4 + 4 * s) * (16 / EB);
-      Pack<T, 16 / EB> p = {};
-      if (there && e0 < a.c.d) p = *(const Pack<T, 16 / EB>*)(x + e0);
+      for (int s = 0; s < CH / 4; s++) {
+        const int e0 = (h4 + 4 * s) * (16 / EB);
+        const Pack<T, 16 / EB> p = *(const Pack<T, 16 / EB>*)(x + (e0 < k.c.d ? e0 : 0));
+        const float sign = there && e0 < k.c.d ? k.sign : 0.f;
 #pragma unroll
-      for (int j = 0; j < 16 / EB; j++) q[r][s][j] = from_float<T>(as_float(p.v[j]) * a.sign);
+        for (int j = 0; j < 16 / EB; j++) q[r][s][j] = sign == 0.f ? (T)0.f : from_float<T>(as_float(p.v[j]) * sign);
+      }
     }
   }
 
@@ -304,12 +348,16 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   const uint32_t ids0 = __builtin_amdgcn_readfirstlane(lds_addr_of(ids));
   const int blocks = end > begin ? (end - begin + KVB - 1) / KVB : 0, turns = blocks > wave ? (blocks - wave + NW - 1) / NW : 0;
   auto first_row = [&](int n) { return begin + (wave + n * NW) * KVB; };
-  auto ask_ids = [&](int n) { ask_page(a.c, pages, first_row(n) + (lane & (KVB - 1)), end, ids0 + (n & 3) * 256); };
-  auto ask_block = [&](int n) {
+  auto ask_ids = [&](int n) INLINE { ask_page(a.c, pages, first_row(n) + (lane & (KVB - 1)), end, ids0 + (n & 3) * 256); };
+  auto ask_block = [&](int n) INLINE {
     const long long at = row_at(a.c, first_row(n) + (lane & (KVB - 1)), end, ids[(n & 3) * 64 + lane]);
     const uint32_t to = stage0 + (n & 1) * STAGE;
 #pragma unroll
-    for (int j = 0; j < ASKS; j++) ask_rows<T, CH, true>(a.c, head, at, j * (64 / CH), j * (64 / CH), to + j * 1024, to + HALF + j * 1024);
+    for (int j = 0; j < ASKS; j++) {
+      const Chunk x = chunk_of<T, CH>(a.c, lane, at, j * (64 / CH), j * (64 / CH));
+      ask_chunk<true>(a.c.keys + head, x, to + j * 1024);
+      ask_chunk<true>(a.c.values + head, x, to + HALF + j * 1024);
+    }
   };
   v4f o[RT][DT] = {};
   float m[RT], l[RT];
@@ -323,7 +371,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     wait_vm_lds<0>();
     ask_block(0);
   }
-  auto block = [&](int n, auto is_masked) {
+  auto block = [&](int n, auto is_masked) INLINE {
     constexpr bool masked = decltype(is_masked)::value;
     const int k0 = first_row(n);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // the stage's last reads
@@ -348,18 +396,18 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
         for (int r = 0; r < RT; r++) s[r][t] = Frag<T>::mma16(k, q[r][c], s[r][t]);
       }
     }
-    unsigned long long seen[RT];
+    uint32_t seen[RT];
     float p[RT][KT][4];
 #pragma unroll
     for (int r = 0; r < RT; r++) {
-      if (masked) seen[r] = token[r] < 0 ? 0ull : seen_bits(a, it.s, token[r], k0, end);
+      if (masked) seen[r] = (uint32_t)(seen_bits(args_again(), it.s, token[r], k0, end) >> (4 * h4));
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < KT; t++)
 #pragma unroll
         for (int i = 0; i < 4; i++) {
           float x = s[r][t][i] * a.scale;
-          if (masked && !(seen[r] >> (16 * t + 4 * h4 + i) & 1)) x = -INFINITY;
+          if (masked) x = seen_score(seen[r], 16 * t + i, x);
           p[r][t][i] = x;
           top = fmaxf(top, x);
         }
@@ -402,7 +450,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
           for (int r = 0; r < RT; r++) {
             F one;
 #pragma unroll
-            for (int j = 0; j < 8; j++) one[j] = (T)(seen[r] >> (16 * (j / 4) + 4 * h4 + j % 4) & 1 ? 1.f : 0.f);
+            for (int j = 0; j < 8; j++) one[j] = one_bit<T>(seen[r], 16 * (j / 4) + j % 4);
             const v4f n = Frag<T>::mma16(kinds, one, (v4f){0, 0, 0, 0});
 #pragma unroll
             for (int i = 0; i < 4; i++) o[r][d][i] += of_kinds(n[i]);
@@ -423,7 +471,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
           for (int r = 0; r < RT; r++) {
             F one;
 #pragma unroll
-            for (int i = 0; i < 4; i++) one[i] = seen[r] >> (4 * h4 + i) & 1 ? 1.f : 0.f;
+            for (int i = 0; i < 4; i++) one[i] = one_bit<float>(seen[r], i);
             const v4f n = Frag<T>::mma16(kinds, one, (v4f){0, 0, 0, 0});
 #pragma unroll
             for (int i = 0; i < 4; i++) o[r][d][i] += of_kinds(n[i]);
@@ -435,7 +483,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     }
   };
   // blocks that every query of the tile sees whole come first
-  const int sure = min(end, it.s.base + (a.tree ? 0 : (int)((long long)it.tile * ROWS / a.group) + 1));
+  const int sure = min(end, it.s.base + (a.tree ? 0 : (int)((long long)it.tile * ROWS / group) + 1));
   int n = 0;
   for (; n < turns && first_row(n) + KVB <= sure; n++) block(n, std::false_type());
   for (; n < turns; n++) block(n, std::true_type());
@@ -451,10 +499,11 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     for (int d = 0; d < DT; d++) *(v4f*)(mine + row * (D * 4) + (((4 * d + h4) ^ (row & 15)) * 16)) = o[r][d];
   }
   __syncthreads();
+  const AttendArgs k = args_again();
   for (int e = threadIdx.x; e < ROWS * (D / 4); e += NW * 64) {
     const int row = e / (D / 4), c = e % (D / 4);
     const long long of = (long long)it.tile * ROWS + row;
-    if (of >= (long long)it.s.n * a.group || c * 4 >= a.c.d) continue;
+    if (of >= (long long)it.s.n * group || c * 4 >= k.c.d) continue;
     float top = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; w++) top = fmaxf(top, stat[w][row][0]);
@@ -467,231 +516,248 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     }
     if (it.slot >= 0) {
       const long long slot = it.slot;
-      *(v4f*)(a.part + (slot * ROWS + row) * a.c.d + c * 4) = y;
-      float* const st = a.part + 2ll * a.slots * ROWS * a.c.d + (slot * ROWS + row) * 2;
+      *(v4f*)(k.part + (slot * ROWS + row) * k.c.d + c * 4) = y;
+      float* const st = k.part + 2ll * k.slots * ROWS * k.c.d + (slot * ROWS + row) * 2;
       if (c == 0) st[0] = top, st[1] = sum;
     } else {
-      const int i = (int)(of / a.group), g = (int)(of - (long long)i * a.group);
+      const int i = (int)(of / group), g = (int)(of - (long long)i * group);
       Pack<T, 4> z;
 #pragma unroll
       for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(sum == 0.f ? 0.f : y[j] / sum);
-      *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + (it.s.t0 + i) * a.out.token + (h * a.group + g) * a.out.head) + c * 4) = z;
+      *(Pack<T, 4>*)((T*)(const_cast<char*>(k.out.at) + (it.s.t0 + i) * k.out.token + (h * group + g) * k.out.head) + c * 4) = z;
     }
   }
   }
 }
 
 // ---------------------------------------------------------------- many rows of queries
-// Four waves of 32 RT rows each share blocks of KVB rows of the cache, in two stages of LDS: a block's products run while the next one
+// Four waves of 32 rows each share blocks of KVB rows of the cache, in two stages of LDS: a block's products run while the next one
 // arrives.
-template <typename T, int D, int RT, int KVB>
-__global__ __launch_bounds__(256, RT == 1 && D * sizeof(T) <= 256 ? 2 : 1) void kv_tile_k(AttendArgs a) {
+#define TILE_WAVES(wide) ((wide) <= 128 ? 3 : (wide) <= 256 ? 2 : 1)
+template <typename T, int D, int KVB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE_WAVES(D * sizeof(T)), TILE_WAVES(D * sizeof(T))))) void kv_tile_k(AttendArgs a) {
   typedef typename Frag<T>::type F;
-  constexpr int EB = sizeof(T), CH = D * EB / 16, KT = KVB / 32, NW = 4, ROWS = 32 * RT * NW;
-  constexpr int HALF = KVB * D * EB, STAGE = 2 * HALF, MINE = KVB / NW, ASKS = HALF / 1024 / NW, DT = D / 32;
+  constexpr int EB = sizeof(T), CH = D * EB / 16, KT = KVB / 32, NW = 4, ROWS = 32 * NW, N = 16 / EB;
+  constexpr int HALF = KVB * D * EB, MINE = KVB / NW, ASKS = HALF / 1024 / NW, DT = D / 32;
   static_assert(ASKS >= 1 && MINE * CH == ASKS * 64 && KVB <= 64, "a wave asks for whole rows");
-  extern __shared__ __align__(1024) char lds[];       // [2][STAGE], [NW][2][64] pages' numbers
+  extern __shared__ __align__(1024) char lds[];     // [2] keys [HALF] and values [HALF], [NW][2][64] pages' numbers
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h2 = lane >> 5;
   Finder<KVB, false> f;
-  f.look(a, ROWS);
+  f.look(args_again(), ROWS);
   const int wg = f.plan.wgs ? kv_wg_of(blockIdx.x, f.plan.wgs) : 0;
   if (wg < 0) return;
   uint32_t at = f.plan.wgs ? kv_from(f.plan, wg) : blockIdx.x;
   const uint32_t stop = f.plan.wgs ? kv_from(f.plan, wg + 1) : at + 1;
   for (bool first = true; at < stop; first = false) {
-  Item it;
-  const uint32_t take = f.next(a, ROWS, wg, at, stop, &it);
-  if (!take) return;
-  at += take;
-  const int begin = it.begin, end = it.end, h = it.h;
-  if (!first) __syncthreads();                      // the stages held the last tile's rows
+    Item it;
+    const uint32_t take = f.next(args_again(), ROWS, wg, at, stop, &it);
+    if (!take) return;
+    at += take;
+    const int begin = it.begin, end = it.end, h = it.h;
+    if (!first) __syncthreads();                    // the stages held the last tile's rows
 
-  // the wave's queries: lane l32 of row tile r holds chunks h2, h2 + 2, ... of row 32 r + l32
-  const long long row0 = (long long)it.tile * ROWS + wave * 32 * RT;
-  int token[RT];
-  F q[RT][CH / 2];
-#pragma unroll
-  for (int r = 0; r < RT; r++) {
-    const long long row = row0 + 32 * r + l32;
-    const bool there = row < (long long)it.s.n * a.group;
-    token[r] = there ? (int)(row / a.group) : -1;
-    const int g = (int)(row - (long long)(there ? token[r] : 0) * a.group);
-    const T* const x = (const T*)(a.q.at + (it.s.t0 + (there ? token[r] : 0)) * a.q.token + (h * a.group + (there ? g : 0)) * a.q.head);
-#pragma unroll
-    for (int s = 0; s < CH / 2; s++) {
-      const int e0 = (h2 + 2 * s) * (16 / EB);
-      Pack<T, 16 / EB> p = {};
-      if (there && e0 < a.c.d) p = *(const Pack<T, 16 / EB>*)(x + e0);
-#pragma unroll
-      for (int j = 0; j < 16 / EB; j++) q[r][s][j] = from_float<T>(as_float(p.v[j]) * a.sign);
-    }
-  }
-  // what the wave's rows see at least (unmasked) and at most: blocks behind the latter are left out
-  const int least = (int)(row0 / a.group), last = min(it.s.n - 1, (int)((row0 + 32 * RT - 1) / a.group));
-  const int sure = it.s.base + (a.tree ? 0 : least + 1);
-  const int wave_end = row0 >= (long long)it.s.n * a.group ? 0 : a.tree ? end : min(end, it.s.base + last + 1);
-
-  const int* const pages = a.b.pages + it.b * a.b.ld;
-  const long long head = h * a.c.head;
-  const uint32_t stage0 = __builtin_amdgcn_readfirstlane(lds_addr_of(lds));
-  int* const ids = (int*)(lds + 2 * STAGE) + wave * 2 * 64;
-  const uint32_t ids0 = __builtin_amdgcn_readfirstlane(lds_addr_of(ids));
-  const int blocks = end > begin ? (end - begin + KVB - 1) / KVB : 0;
-  auto ask_ids = [&](int n) { ask_page(a.c, pages, begin + n * KVB + wave * MINE + (lane & (MINE - 1)), end, ids0 + (n & 1) * 256); };
-  auto ask_block = [&](int n) {
-    const long long at = row_at(a.c, begin + n * KVB + wave * MINE + (lane & (MINE - 1)), end, ids[(n & 1) * 64 + lane]);
-    const uint32_t to = stage0 + (n & 1) * STAGE + wave * ASKS * 1024;
-#pragma unroll
-    for (int j = 0; j < ASKS; j++) ask_rows<T, CH, false>(a.c, head, at, j * (64 / CH), wave * MINE + j * (64 / CH), to + j * 1024, to + HALF + j * 1024);
-  };
-  v16f o[RT][DT] = {};
-  float m[RT], l[RT];
-#pragma unroll
-  for (int r = 0; r < RT; r++) m[r] = -INFINITY, l[r] = 0.f;
-
-  if (blocks > 0) {
-    ask_ids(0);
-    wait_vm_lds<0>();
-    ask_block(0);
-    ask_ids(1);
-  }
-  auto block = [&](int n, auto is_masked) {
-    constexpr bool masked = decltype(is_masked)::value;
-    const int k0 = begin + n * KVB;
-    wait_vm_barrier<0>();
-    if (n + 1 < blocks) {
-      ask_block(n + 1);
-      ask_ids(n + 2);
-    }
-    if (masked && k0 >= wave_end) return;
-    const uint32_t stage = stage0 + (n & 1) * STAGE;
-    const uint32_t ks = hidden(stage + l32 * (D * EB) + ((h2 ^ swizzle<CH>(l32)) * 16));
-    v16f s[RT][KT];
-#pragma unroll
-    for (int t = 0; t < KT; t++) {
-#pragma unroll
-      for (int r = 0; r < RT; r++) s[r][t] = (v16f){0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    const int group = a.group;
+    // the wave's queries: lane l32 holds chunks h2, h2 + 2, ... of its row; zeros where there is none, from memory that is there
+    const long long row0 = (long long)it.tile * ROWS + wave * 32, row = row0 + l32;
+    const bool there = row < (long long)it.s.n * group;
+    const int token = there ? (int)(row / group) : -1;
+    F q[CH / 2];
+    {
+      const AttendArgs k = args_again();
+      const int g = there ? (int)(row - (long long)token * group) : 0;
+      const T* const x = (const T*)(k.q.at + (it.s.t0 + (there ? token : 0)) * k.q.token + (h * group + g) * k.q.head);
 #pragma unroll
       for (int c = 0; c < CH / 2; c++) {
-        const F k = at_lds<F>((ks ^ (2 * c * 16)) + 32 * t * (D * EB));
+        const int e0 = (h2 + 2 * c) * N;
+        const Pack<T, N> p = *(const Pack<T, N>*)(x + (e0 < k.c.d ? e0 : 0));
+        const float sign = there && e0 < k.c.d ? k.sign : 0.f;
 #pragma unroll
-        for (int r = 0; r < RT; r++) s[r][t] = Frag<T>::mma32(k, q[r][c], s[r][t]);
+        for (int j = 0; j < N; j++) q[c][j] = sign == 0.f ? (T)0.f : from_float<T>(as_float(p.v[j]) * sign);
       }
     }
-    unsigned long long seen[RT];
+    // what the wave's rows see at least (unmasked) and at most: blocks behind the latter are left out
+    const int last = min(it.s.n - 1, (int)((row0 + 31) / group));
+    const int sure = min(end, it.s.base + (a.tree ? 0 : (int)(row0 / group) + 1));
+    const int wave_end = row0 >= (long long)it.s.n * group ? 0 : a.tree ? end : min(end, it.s.base + last + 1);
+
+    const int* const pages = a.b.pages + it.b * a.b.ld;
+    const long long head = h * a.c.head;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(lds));
+    int* const ids = (int*)(lds + 4 * HALF) + wave * 2 * 64;
+    const uint32_t ids0 = __builtin_amdgcn_readfirstlane(lds_addr_of(ids));
+    const int blocks = end > begin ? (end - begin + KVB - 1) / KVB : 0;
+    const bool simple = a.c.page_size % MINE == 0 && a.c.d == D && a.c.slot < 1 << 24;
+    auto row_of = [&](int n) INLINE { return begin + n * KVB + wave * MINE; };
+    auto ask_ids = [&](int n) INLINE { ask_page(a.c, pages, row_of(n) + (lane & (MINE - 1)), end, ids0 + (n & 1) * 256); };
+    // Rows in one page, as those of a wave are where pages hold whole shares of a block: their place is the wave's, a lane's chunk an offset.
+    // Anything else row by row, which takes a hundred instructions instead of a dozen.
+    auto ask_block = [&](int n, bool whole) INLINE {
+      const uint32_t to = lds0 + (n & 1) * 2 * HALF + wave * ASKS * 1024;
+      const int page = __builtin_amdgcn_readfirstlane(ids[(n & 1) * 64]);
+      if (whole && (uint32_t)page < (uint32_t)a.c.pages) {
+        const int slot = row_of(n) - (int)((unsigned long long)(uint32_t)row_of(n) * a.c.magic >> a.c.shift) * a.c.page_size;
+        const char* k = a.c.keys + (head + page * a.c.page + slot * a.c.slot);
+        const long long apart = a.c.values - a.c.keys;
 #pragma unroll
-    for (int r = 0; r < RT; r++) {
+        for (int j = 0; j < ASKS; j++) {
+          const uint32_t off = ((lane % CH ^ swizzle<CH>(lane / CH)) ^ swizzle<CH>(wave * MINE + j * (64 / CH))) * 16 + lane / CH * (uint32_t)a.c.slot;
+          slab_load16s((const uint8_t*)k, off, to + j * 1024);
+          slab_load16s((const uint8_t*)k + apart, off, to + HALF + j * 1024);
+          k += 64 / CH * a.c.slot;
+        }
+      } else {
+        const int l = hidden(lane);                 // nothing of this is worth a register beside the blocks that do without it
+        const AttendArgs k = args_again();
+        const long long mine = row_at(k.c, row_of(n) + (l & (MINE - 1)), end, ids[(n & 1) * 64 + l]);
+#pragma unroll
+        for (int j = 0; j < ASKS; j++) {
+          const Chunk x = chunk_of<T, CH>(k.c, l, mine, j * (64 / CH), wave * MINE + j * (64 / CH));
+          ask_chunk<false>(k.c.keys + head, x, to + j * 1024);
+          ask_chunk<false>(k.c.values + head, x, to + HALF + j * 1024);
+        }
+      }
+    };
+    const uint32_t k_at = l32 * (D * EB) + ((h2 ^ swizzle<CH>(l32)) * 16);
+    const int v_row = 4 * h2 + (EB == 2 ? (lane & 15) / 4 : 0);
+    const uint32_t v_at = HALF + v_row * (D * EB) +
+                          (EB == 2 ? ((2 * (lane >> 4 & 1) + (lane & 3) / 2 ^ swizzle<CH>(v_row)) * 16) + (lane & 1) * 8
+                                   : ((l32 / 4 ^ swizzle<CH>(v_row)) * 16) + (l32 & 3) * 4);
+    v16f o[DT] = {};
+    float m = -INFINITY, l = 0.f;
+    auto block = [&](int n, auto is_masked) INLINE {
+      constexpr bool masked = decltype(is_masked)::value;
+      const int k0 = begin + n * KVB;
+      wait_vm_barrier<0>();
+      if (n + 1 < blocks) {
+        ask_block(n + 1, simple && k0 + 2 * KVB <= end);
+        ask_ids(n + 2);
+      }
+      if (masked && k0 >= wave_end) return;
+      const uint32_t ks = hidden(lds0 + (n & 1) * 2 * HALF + k_at);
+      // products and the reads AHEAD of them in a fixed order: left alone, the compiler waits for every read in front of its product
+      constexpr int QK = KT * CH / 2, STEPS = 16 / N, PV = KT * STEPS * DT, AHEAD = 4;         // a step: 16 rows, or 8
+      v16f s[KT];
+      F k[AHEAD];
+      auto key = [&](int i) INLINE { return at_lds<F>((ks ^ (2 * (i % (CH / 2)) * 16)) + 32 * (i / (CH / 2)) * (D * EB)); };
+#pragma unroll
+      for (int i = 0; i < AHEAD; i++) k[i] = key(i);
+#pragma unroll
+      for (int i = 0; i < QK; i++) {
+        const v16f zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        in_order();
+        s[i / (CH / 2)] = Frag<T>::mma32(k[i % AHEAD], q[i % (CH / 2)], i % (CH / 2) ? s[i / (CH / 2)] : zero);
+        if (i + AHEAD < QK) k[i % AHEAD] = key(i + AHEAD);
+      }
+      uint32_t seen[KT];
       if (masked) {
-        seen[r] = token[r] < 0 ? 0ull : seen_bits(a, it.s, token[r], k0, end);
-        const unsigned long long mine = seen[r] >> (4 * h2);
+        const unsigned long long bits = seen_bits(args_again(), it.s, token, k0, end) >> (4 * h2);
 #pragma unroll
-        for (int t = 0; t < KT; t++)
+        for (int t = 0; t < KT; t++) {
+          seen[t] = (uint32_t)(bits >> (32 * t));
 #pragma unroll
-          for (int i = 0; i < 16; i++)
-            if (!(mine >> (32 * t + 8 * (i / 4) + i % 4) & 1)) s[r][t][i] = -INFINITY;
-      }
-      float top = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < KT; t++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) top = fmaxf(top, s[r][t][i]);
-      top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.scale;
-      const bool more = top > m[r] + LAG;                        // of this row alone: its neighbours' scores change nothing in it
-      if (__any(more)) {
-        const float f = more ? __builtin_amdgcn_exp2f(m[r] - top) : 1.f;
-        if (more) m[r] = top;
-        l[r] *= f;
-#pragma unroll
-        for (int d = 0; d < DT; d++) o[r][d] *= f;
-      }
-      const float from = LIFT<T> - (m[r] == -INFINITY ? 0.f : m[r]);
-      float sum = 0.f;
-#pragma unroll
-      for (int t = 0; t < KT; t++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-          s[r][t][i] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r][t][i], a.scale, from));
-          sum += s[r][t][i];
-        }
-      l[r] += sum;
-    }
-    const int vrow = 4 * h2 + (EB == 2 ? (lane & 15) / 4 : 0);
-    const uint32_t vs = EB == 2 ? hidden(stage + HALF + vrow * (D * EB) + ((2 * (lane >> 4 & 1) + (lane & 3) / 2 ^ swizzle<CH>(vrow)) * 16) + (lane & 1) * 8)
-                                : hidden(stage + HALF + vrow * (D * EB) + ((l32 / 4 ^ swizzle<CH>(vrow)) * 16) + (l32 & 3) * 4);
-#pragma unroll
-    for (int t = 0; t < KT; t++) {
-      constexpr int STEPS = EB == 2 ? 2 : 4;        // of 16 rows, or of 8
-#pragma unroll
-      for (int u = 0; u < STEPS; u++) {
-        constexpr int N = 16 / EB;
-        F w[RT];
-#pragma unroll
-        for (int r = 0; r < RT; r++)
-#pragma unroll
-          for (int j = 0; j < N; j++) w[r][j] = (T)s[r][t][N * u + j];
-#pragma unroll
-        for (int d = 0; d < DT; d++) {
-          F v;
-          if constexpr (EB == 2) {
-            union { F f; v4s half[2]; } x;
-#pragma unroll
-            for (int j = 0; j < 2; j++) x.half[j] = at_lds_turned((vs ^ ((4 * d ^ swizzle<CH>(8 * j)) * 16)) + (32 * t + 16 * u + 8 * j) * (D * EB));
-            v = x.f;
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; j++) v[j] = at_lds<float>((vs ^ ((8 * d ^ swizzle<CH>(8 * u + j)) * 16)) + (32 * t + 8 * u + j) * (D * EB));
-          }
-          if (masked && __any(not_finite<T>(v))) {
-            const F kinds = take_kinds<T>(&v);
-#pragma unroll
-            for (int r = 0; r < RT; r++) {
-              F one;
-#pragma unroll
-              for (int j = 0; j < N; j++) one[j] = (T)(seen[r] >> (32 * t + 2 * N * u + 8 * (j / 4) + 4 * h2 + j % 4) & 1 ? 1.f : 0.f);
-              const v16f n = Frag<T>::mma32(kinds, one, (v16f){0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0});
-#pragma unroll
-              for (int i = 0; i < 16; i++) o[r][d][i] += of_kinds(n[i]);
-            }
-          }
-#pragma unroll
-          for (int r = 0; r < RT; r++) o[r][d] = Frag<T>::mma32(v, w[r], o[r][d]);
+          for (int i = 0; i < 16; i++) s[t][i] = seen_score(seen[t], 8 * (i / 4) + i % 4, s[t][i]);
         }
       }
-    }
-  };
-  // blocks that every query of the wave sees whole come first
-  int n = 0;
-  for (; n < blocks && begin + n * KVB + KVB <= min(end, sure); n++) block(n, std::false_type());
-  for (; n < blocks; n++) block(n, std::true_type());
+      // Weights against the maximum so far.  As long as their sum stays below OVER, which no sum does before the first maximum is taken, no
+      // weight is too large and the block's own maximum is not needed.
+      F w[KT * STEPS];
+      float sum;
+      auto weights = [&](float from) INLINE {
+        sum = 0.f;
 #pragma unroll
-  for (int r = 0; r < RT; r++) {
-    l[r] += __shfl_xor(l[r], 32, 64);
-    if (token[r] < 0) continue;
-    const long long of = row0 + 32 * r + l32;
-    const long long slot = it.slot, in = of - (long long)it.tile * ROWS;
-    float* const part = a.part + (slot * ROWS + in) * a.c.d;
-    T* const out = (T*)(const_cast<char*>(a.out.at) + (it.s.t0 + token[r]) * a.out.token + (h * a.group + (int)(of - (long long)token[r] * a.group)) * a.out.head);
-    const float by = l[r] == 0.f ? 0.f : 1.f / l[r];
-    if (it.slot >= 0 && h2 == 0) {
-      float* const st = a.part + 2ll * a.slots * ROWS * a.c.d + (slot * ROWS + in) * 2;
-      st[0] = m[r], st[1] = l[r];
-    }
+        for (int e = 0; e < KT * 16; e++) w[e / N][e % N] = (T)__builtin_amdgcn_exp2f(__fmaf_rn(s[e / 16][e % 16], a.scale, from));
 #pragma unroll
-    for (int d = 0; d < DT; d++)
+        for (int i = 0; i < KT * STEPS; i++) sum = sum_of(w[i], sum);
+      };
+      weights(LIFT<T> - m);
+      if (__any(!(sum <= OVER))) {
+        // of this row alone: its neighbours' scores change nothing in it
+        const float other = __shfl_xor(sum, 32, 64);
+        const bool more = !(sum <= OVER) || !(other <= OVER);
+        float top = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < 4; k++) {
-        const int e = 32 * d + 8 * k + 4 * h2;
-        if (e >= a.c.d) continue;
-        if (it.slot >= 0) {
-          *(v4f*)(part + e) = (v4f){o[r][d][4 * k], o[r][d][4 * k + 1], o[r][d][4 * k + 2], o[r][d][4 * k + 3]};
+        for (int e = 0; e < KT * 16; e++) top = fmaxf(top, s[e / 16][e % 16]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.scale;
+        const float to = more && top > m ? top : m, by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= by;
+#pragma unroll
+        for (int d = 0; d < DT; d++) o[d] *= by;
+        weights(LIFT<T> - (m == -INFINITY ? 0.f : m));       // nothing seen so far, or only scores of -inf: zeros
+      }
+      l += sum;
+      const uint32_t vs = hidden(lds0 + (n & 1) * 2 * HALF + v_at);
+      F v[AHEAD];
+      auto value = [&](int i) INLINE {
+        const int d = i % DT, row = i / DT * 2 * N;
+        F x;
+        if constexpr (EB == 2) {
+          union { F f; v4s half[2]; } y;
+#pragma unroll
+          for (int j = 0; j < 2; j++) y.half[j] = at_lds_turned((vs ^ ((4 * d ^ swizzle<CH>(8 * j)) * 16)) + (row + 8 * j) * (D * EB));
+          x = y.f;
         } else {
-          Pack<T, 4> z;
 #pragma unroll
-          for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(l[r] == 0.f ? 0.f : o[r][d][4 * k + j] * by);
-          *(Pack<T, 4>*)(out + e) = z;
+          for (int j = 0; j < 4; j++) x[j] = at_lds<float>((vs ^ ((8 * d ^ swizzle<CH>(row % 32 + j)) * 16)) + (row + j) * (D * EB));
         }
+        return x;
+      };
+#pragma unroll
+      for (int i = 0; i < AHEAD; i++) v[i] = value(i);
+#pragma unroll
+      for (int i = 0; i < PV; i++) {
+        const int d = i % DT, t = i / DT / STEPS, u = i / DT % STEPS;
+        if (masked && __any(not_finite<T>(v[i % AHEAD]))) {
+          const F kinds = take_kinds<T>(&v[i % AHEAD]);
+          F one;
+#pragma unroll
+          for (int j = 0; j < N; j++) one[j] = one_bit<T>(seen[t], 2 * N * u + 8 * (j / 4) + j % 4);
+          const v16f count = Frag<T>::mma32(kinds, one, (v16f){0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0});
+#pragma unroll
+          for (int e = 0; e < 16; e++) o[d][e] += of_kinds(count[e]);
+        }
+        in_order();
+        o[d] = Frag<T>::mma32(v[i % AHEAD], w[i / DT], o[d]);
+        if (i + AHEAD < PV) v[i % AHEAD] = value(i + AHEAD);
       }
-  }
+    };
+    if (blocks > 0) {
+      ask_ids(0);
+      wait_vm_lds<0>();
+      ask_block(0, simple && begin + KVB <= end);
+      ask_ids(1);
+    }
+    // blocks that every query of the wave sees whole come first
+    int n = 0;
+    for (; n < blocks && begin + n * KVB + KVB <= sure; n++) block(n, std::false_type());
+    for (; n < blocks; n++) block(n, std::true_type());
+    l += __shfl_xor(l, 32, 64);
+    if (there) {
+      const AttendArgs k = args_again();
+      const long long in = row - (long long)it.tile * ROWS;
+      float* const part = k.part + ((long long)it.slot * ROWS + in) * k.c.d;
+      T* const out = (T*)(const_cast<char*>(k.out.at) + (it.s.t0 + token) * k.out.token + (h * group + (int)(row - (long long)token * group)) * k.out.head);
+      const float by = l == 0.f ? 0.f : 1.f / l;
+      if (it.slot >= 0 && h2 == 0) {
+        float* const st = k.part + 2ll * k.slots * ROWS * k.c.d + ((long long)it.slot * ROWS + in) * 2;
+        st[0] = m, st[1] = l;
+      }
+#pragma unroll
+      for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int p = 0; p < 4; p++) {
+          const int e = 32 * d + 8 * p + 4 * h2;
+          if (e >= k.c.d) continue;
+          if (it.slot >= 0) {
+            *(v4f*)(part + e) = (v4f){o[d][4 * p], o[d][4 * p + 1], o[d][4 * p + 2], o[d][4 * p + 3]};
+          } else {
+            Pack<T, 4> z;
+#pragma unroll
+            for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(l == 0.f ? 0.f : o[d][4 * p + j] * by);
+            *(Pack<T, 4>*)(out + e) = z;
+          }
+        }
+    }
   }
 }
 
@@ -721,17 +787,35 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
     const bool mine = part < share && r < there;
     float m = -INFINITY, l = 0.f;
     v4f y = {0, 0, 0, 0};
-    if (mine)
-      for (int p = part; p < pieces; p += share) {
-        const long long slot = 2 * (w0 + p) + (p == 0);
+    constexpr int FLY = 4;                          // parts on their way at a time
+    for (int p = part; mine && p < pieces; p += FLY * share) {
+      v4f x[FLY];
+      float top[FLY], sum[FLY];
+#pragma unroll
+      for (int k = 0; k < FLY; k++) {
+        const int at = min(p + k * share, pieces - 1);
+        const long long slot = 2 * (w0 + at) + (at == 0);
         const float* const st = a.part + 2ll * a.slots * rows * a.c.d + (slot * rows + r) * 2;
-        const v4f x = *(const v4f*)(a.part + (slot * rows + r) * a.c.d + c * 4);
-        const float top = fmaxf(m, st[0]), safe = top == -INFINITY ? 0.f : top;
-        const float f = __builtin_amdgcn_exp2f(m - safe), g = __builtin_amdgcn_exp2f(st[0] - safe);
-        y = y * f + x * g;
-        l = l * f + st[1] * g;
-        m = top;
+        x[k] = *(const v4f*)(a.part + (slot * rows + r) * a.c.d + c * 4);
+        top[k] = p + k * share < pieces ? st[0] : -INFINITY;
+        sum[k] = st[1];
       }
+      float most = m;
+#pragma unroll
+      for (int k = 0; k < FLY; k++) most = fmaxf(most, top[k]);
+      const float safe = most == -INFINITY ? 0.f : most, by = __builtin_amdgcn_exp2f(m - safe);
+      y *= by;
+      l *= by;
+      m = most;
+#pragma unroll
+      for (int k = 0; k < FLY; k++) {
+        const float f = __builtin_amdgcn_exp2f(top[k] - safe);
+        const bool there = p + k * share < pieces;  // not again what stands in for a part behind the last
+        l += there ? sum[k] * f : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; j++) y[j] += there ? x[k][j] * f : 0.f;
+      }
+    }
     if (r0 > (int)first) __syncthreads();
     sums[threadIdx.x] = y;
     stat[threadIdx.x][0] = m, stat[threadIdx.x][1] = l;
@@ -773,12 +857,8 @@ Cut cut_of(const AttendArgs& a) {
   Cut k;
   const long long mean = (((long long)a.b.tokens + a.b.batch - 1) / std::max(a.b.batch, 1)) * a.group;      // rows a sequence and head
   k.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : 128;
-#ifdef SLOTS
-  k.slots = SLOTS; k.least = LEAST;
-#else
   k.slots = 512;
   k.least = 4;
-#endif
   // the new tokens alone are so much work that a piece is as long as any sequence can be
   const double work = (double)a.b.tokens * a.b.tokens * a.group / ((double)k.rows * std::max(a.b.batch, 1)) * a.c.heads / k.slots;
   if (a.b.most <= 256 || a.b.most <= work) k.slots = 0;
@@ -809,7 +889,7 @@ int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
   // rows of a workgroup that joins: one where that is not too many workgroups
   const int most = std::max(1, 256 / (a.c.d / 4));
   int per = 1;
-  while (per < k.rows && tiles * a.c.heads * (k.rows / per) > 2048) per *= 2;
+  while (per < k.rows && tiles * a.c.heads * (k.rows / per) > JB) per *= 2;
   int few = 1;
   while (few * 2 <= std::min(per, most)) few *= 2;
   // threads of a launch are counted in 32 bits
@@ -817,7 +897,7 @@ int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
   const unsigned grid = (unsigned)items;
   const int rc = k.rows == 16   ? launch<kv_few_k<T, D, 1, NW>, NW * 64, FEW>(st, grid, a)
                  : k.rows == 32 ? launch<kv_few_k<T, D, 2, NW>, NW * 64, FEW>(st, grid, a)
-                                : launch<kv_tile_k<T, D, 1, KVB>, 256, 4 * KVB * WIDE + 2048>(st, grid, a);
+                                : launch<kv_tile_k<T, D, KVB>, 256, 4 * KVB * WIDE + 2048>(st, grid, a);
   if (rc || !k.slots) return rc;
   const dim3 joins((unsigned)(tiles * a.c.heads * (k.rows / per)));
   if (k.rows < 128) hipLaunchKernelGGL((kv_join_k<T, FEW_UNIT>), joins, dim3(256), 0, st, a, k.rows, per, few);

@@ -37,7 +37,10 @@ def trees(case, P, sizes=None):
     ((1,), (1,), 1, 1, 8, 1), ((1,), (17,), 2, 1, 16, 16), ((1, 1, 1), (31, 32, 33), 2, 4, 64, 16), ((1, 1), (65, 300), 1, 7, 128, 24),
     ((1,), (129,), 3, 16, 256, 64), ((1, 1), (5, 700), 1, 33, 96, 100), ((5,), (5,), 2, 3, 80, 8), ((2, 9, 0, 1), (64, 9, 40, 1), 2, 4, 32, 16),
     ((33, 1), (33, 64), 1, 1, 64, 32), ((64,), (200,), 2, 2, 128, 16), ((70, 3), (70, 131), 1, 5, 40, 7), ((130,), (259,), 1, 1, 192, 16),
-    ((257, 20), (300, 300), 1, 2, 64, 64), ((40,), (40,), 1, 12, 72, 256), ((129,), (129,), 2, 1, 256, 48), ((1,), (1000,), 1, 48, 128, 1)])
+    ((257, 20), (300, 300), 1, 2, 64, 64), ((40,), (40,), 1, 12, 72, 256), ((129,), (129,), 2, 1, 256, 48), ((1,), (1000,), 1, 48, 128, 1),
+    # a wave of which some rows are queries and the rest is nobody's
+    ((100,), (100,), 1, 3, 224, 64), ((100,), (300,), 1, 3, 256, 64), ((97,), (97,), 1, 3, 192, 16), ((44,), (100,), 1, 1, 256, 64), ((44,), (100,), 1, 1, 128, 64),
+    ((97, 36), (300, 36), 2, 1, 64, 16)])
 def test_against_the_definition(P, dtype, new, lengths, heads, group, d, page):
     case = Case(new, lengths, heads, group, d, page, dtype, seed=sum(lengths) + d)
     want, lim = attend(case)
