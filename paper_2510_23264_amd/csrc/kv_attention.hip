@@ -19,9 +19,6 @@
 #include "kv.h"
 #include "kv_plan.h"
 
-#ifndef JB
-#define JB 2048
-#endif
 namespace pahq {
 
 struct AttendArgs {
@@ -31,8 +28,9 @@ struct AttendArgs {
   const unsigned long long* tree;
   int words, group;                                 // group: query heads of a cache head
   float scale, sign;                                // of the scores: times log2 e and positive; of the queries: its sign, 0 for a scale of 0
-  float* part;                                      // [slot][rows][d] sums of a part, then [slot][rows][2] maximum and sum
+  float* part;                                      // [slot][rows][d] sums of a part, [slot][rows][2] maximum and sum, then how many of Left there are, and they
   int slots, least;                                 // of ranges (kv_plan.h); slots 0: nothing is cut
+  int by_pair;                                      // Left are counted by tile and head, or by range: whichever are fewer
 };
 
 // The kernel's one argument, read again where it is asked for: kept for the whole kernel it would take more scalar registers than there are.
@@ -78,6 +76,10 @@ template <int UNIT> __device__ __forceinline__ Share share_of(const AttendArgs& 
   x.units_to = __builtin_elementwise_add_sat(wave_sum_up_to(x.units), units_before);
   return x;
 }
+// What the join needs of a tile that lies in several ranges, of which `w0` is the first; pieces 0: of one that does not
+struct Left { int t0, rows, tile, h, pieces, w0, unused[2]; };
+__device__ __forceinline__ int* count_of(const AttendArgs& a, int rows) { return (int*)(a.part + 2ll * a.slots * rows * (a.c.d + 2)); }
+__device__ __forceinline__ Left* left_of(const AttendArgs& a, int rows) { return (Left*)(count_of(a, rows) + 8); }
 struct Item {
   KvSequence s;
   int b, tile, h, begin, end, slot;                 // rows of the cache; slot in the workspace, -1: the whole tile
@@ -92,10 +94,12 @@ __device__ __forceinline__ int tile_end(const AttendArgs& a, const KvSequence& s
 template <int UNIT, bool KEEP> struct Finder {
   Share x;
   KvPlan plan;
+  uint32_t pairs;
   __device__ __forceinline__ bool kept(const AttendArgs& a) const { return KEEP && a.b.batch <= 64; }
   __device__ __forceinline__ void look(const AttendArgs& a, int rows) {
-    uint32_t pairs = 0, units = 0;
+    uint32_t units = 0;
     int longest = 0;
+    pairs = 0;
     for (int b0 = 0; b0 < a.b.batch && (a.slots || kept(a)); b0 += 64) {
       x = share_of<UNIT>(a, rows, b0, pairs, units);
       pairs = lane_of(x.pairs_to, 63);
@@ -144,7 +148,19 @@ template <int UNIT, bool KEEP> struct Finder {
     it->begin = (int)min((uint32_t)min((uint64_t)off * UNIT, (uint64_t)KV_MAX_LENGTH), (uint32_t)it->end);
     if (off + take < whole) it->end = min(it->end, (int)((off + take) * UNIT));
     if (take < whole) it->slot = 2 * wg + (off ? 0 : 1);
+    if (!off && (take < whole || a.by_pair) && threadIdx.x == 0) {
+      const uint32_t number = lane_of(x.pairs_to, l) - lane_of(x.pairs, l) + pair;
+      if (!a.by_pair || number < (uint32_t)a.slots)
+        left_of(a, rows)[a.by_pair ? number : wg] = {it->s.t0, (int)min((long long)it->s.n * a.group - (long long)it->tile * rows, (long long)rows), it->tile, it->h,
+                                                     take < whole ? kv_holder(plan, at + whole - 1) - wg + 1 : 0, wg, {}};
+    }
     return take;
+  }
+  // A range says first that it left nothing; the first one how many Left there are
+  __device__ __forceinline__ void begin(const AttendArgs& a, int rows, int wg) const {
+    if (!a.slots || threadIdx.x) return;
+    if (plan.wgs && !a.by_pair) left_of(a, rows)[wg].pieces = 0;
+    if (plan.wgs ? wg == 0 : blockIdx.x == 0) *count_of(a, rows) = plan.wgs ? (int)(a.by_pair ? min(pairs, (uint32_t)a.slots) : plan.wgs) : 0;
   }
 };
 // Bit x: whether new token i sees row k0 + x of the cache; none for i < 0.  Without branches: lanes part here otherwise, and registers that
@@ -306,6 +322,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   f.look(args_again(), ROWS);
   const int wg = f.plan.wgs ? kv_wg_of(blockIdx.x, f.plan.wgs) : 0;
   if (wg < 0) return;
+  f.begin(args_again(), ROWS, wg);
   uint32_t at = f.plan.wgs ? kv_from(f.plan, wg) : blockIdx.x;
   const uint32_t stop = f.plan.wgs ? kv_from(f.plan, wg + 1) : at + 1;
   for (bool first = true; at < stop; first = false) {
@@ -546,6 +563,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE_WAVES(
   f.look(args_again(), ROWS);
   const int wg = f.plan.wgs ? kv_wg_of(blockIdx.x, f.plan.wgs) : 0;
   if (wg < 0) return;
+  f.begin(args_again(), ROWS, wg);
   uint32_t at = f.plan.wgs ? kv_from(f.plan, wg) : blockIdx.x;
   const uint32_t stop = f.plan.wgs ? kv_from(f.plan, wg + 1) : at + 1;
   for (bool first = true; at < stop; first = false) {
@@ -761,28 +779,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE_WAVES(
   }
 }
 
-// The pieces of a tile become its rows.  A workgroup takes `per` rows, `few` at a time: for each of them the pieces are shared out over the
-// threads that are left beside four elements each, and joined in LDS.
-template <typename T, int UNIT>
+// The parts of a tile become its rows: of the blockIdx.x-th Left, rows blockIdx.y * per and on, `few` at a time: for each of them the parts are
+// shared out over the threads that are left beside four elements each, and joined in LDS.
+template <typename T>
 __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per, int few) {
   __shared__ v4f sums[256];
   __shared__ float stat[256][2];
-  Finder<UNIT, true> find;
-  find.look(a, rows);
-  if (!find.plan.wgs) return;
-  const uint32_t groups = rows / per, number = blockIdx.x / groups, first = blockIdx.x % groups * per;
-  int b0;
-  const int lane = find.lane_with(a, rows, number, false, &b0);
-  if (lane < 0) return;
-  const KvSequence s = find.sequence(lane);
-  const uint32_t tiles = lane_of(find.x.tiles, lane), pair = number - (lane_of(find.x.pairs_to, lane) - lane_of(find.x.pairs, lane));
-  const int h = pair / tiles, tile = pair - h * tiles;
-  const uint32_t whole = kv_units_of(s.length, UNIT), start = lane_of(find.x.units_to, lane) - lane_of(find.x.units, lane) + pair * whole;
-  const int w0 = kv_holder(find.plan, start), pieces = kv_holder(find.plan, start + whole - 1) - w0 + 1;
-  if (pieces <= 1) return;
-  const long long there = (long long)s.n * a.group - (long long)tile * rows;
+  const int first = blockIdx.y * per, count = *count_of(a, rows);
+  const Left t = left_of(a, rows)[blockIdx.x];      // behind the count: whatever the memory held
+  if ((int)blockIdx.x >= count || t.pieces <= 1 || first >= t.rows) return;
+  const int pieces = t.pieces, there = t.rows, tile = t.tile, h = t.h, w0 = t.w0;
   const int quads = a.c.d / 4, share = 256 / (few * quads), e = threadIdx.x % (few * quads), part = threadIdx.x / (few * quads), c = e % quads;
-  for (int r0 = first; r0 < (int)first + per && r0 < there; r0 += few) {
+  for (int r0 = first; r0 < first + per && r0 < there; r0 += few) {
     const int r = r0 + e / quads;
     const bool mine = part < share && r < there;
     float m = -INFINITY, l = 0.f;
@@ -816,7 +824,7 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
         for (int j = 0; j < 4; j++) y[j] += there ? x[k][j] * f : 0.f;
       }
     }
-    if (r0 > (int)first) __syncthreads();
+    if (r0 > first) __syncthreads();
     sums[threadIdx.x] = y;
     stat[threadIdx.x][0] = m, stat[threadIdx.x][1] = l;
     __syncthreads();
@@ -836,7 +844,7 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
     Pack<T, 4> z;
 #pragma unroll
     for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(sum == 0.f ? 0.f : y[j] / sum);
-    *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + (s.t0 + i) * a.out.token + (h * a.group + g) * a.out.head) + c * 4) = z;
+    *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + (t.t0 + i) * a.out.token + (h * a.group + g) * a.out.head) + c * 4) = z;
   }
 }
 
@@ -864,7 +872,7 @@ Cut cut_of(const AttendArgs& a) {
   if (a.b.most <= 256 || a.b.most <= work) k.slots = 0;
   return k;
 }
-size_t part_bytes(const AttendArgs& a, const Cut& k) { return k.slots ? 2ull * k.slots * k.rows * (a.c.d + 2) * 4 : 0; }
+size_t part_bytes(const AttendArgs& a, const Cut& k) { return k.slots ? 2ull * k.slots * k.rows * (a.c.d + 2) * 4 + 32 + k.slots * sizeof(Left) : 0; }
 
 template <void (*K)(AttendArgs), int THREADS, int LDS>
 int launch(hipStream_t st, unsigned grid, const AttendArgs& a) {
@@ -884,24 +892,21 @@ int launch(hipStream_t st, unsigned grid, const AttendArgs& a) {
 template <typename T, int D>
 int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
   constexpr int EB = sizeof(T), WIDE = D * EB, NW = WIDE <= 128 ? 4 : 2, FEW = 2 * NW * 2 * (EB == 2 ? 32 : 16) * WIDE + NW * 1024;
-  constexpr int KVB = WIDE <= 256 ? 64 : 32, FEW_UNIT = (EB == 2 ? 32 : 16) * NW;
+  constexpr int KVB = WIDE <= 256 ? 64 : 32;
   const long long tiles = kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows), items = std::max<long long>(tiles * a.c.heads, k.slots);
-  // rows of a workgroup that joins: one where that is not too many workgroups
-  const int most = std::max(1, 256 / (a.c.d / 4));
-  int per = 1;
-  while (per < k.rows && tiles * a.c.heads * (k.rows / per) > JB) per *= 2;
-  int few = 1;
-  while (few * 2 <= std::min(per, most)) few *= 2;
   // threads of a launch are counted in 32 bits
-  if (items >= KV_MOST_ITEMS || tiles * a.c.heads * (k.rows / per) >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
+  if (items >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
   const unsigned grid = (unsigned)items;
   const int rc = k.rows == 16   ? launch<kv_few_k<T, D, 1, NW>, NW * 64, FEW>(st, grid, a)
                  : k.rows == 32 ? launch<kv_few_k<T, D, 2, NW>, NW * 64, FEW>(st, grid, a)
                                 : launch<kv_tile_k<T, D, KVB>, 256, 4 * KVB * WIDE + 2048>(st, grid, a);
   if (rc || !k.slots) return rc;
-  const dim3 joins((unsigned)(tiles * a.c.heads * (k.rows / per)));
-  if (k.rows < 128) hipLaunchKernelGGL((kv_join_k<T, FEW_UNIT>), joins, dim3(256), 0, st, a, k.rows, per, few);
-  else hipLaunchKernelGGL((kv_join_k<T, KVB>), joins, dim3(256), 0, st, a, k.rows, per, few);
+  // as many rows of a workgroup that its launch, a workgroup in 3 to 4 ns, does not take longer than what they do
+  const int left = (int)std::min<long long>(tiles * a.c.heads, k.slots);
+  int per = 1, few = 1;
+  while (per < k.rows && left * (k.rows / per) > 2048) per *= 2;
+  while (few * 2 <= std::min(per, 4) && few * 2 * (a.c.d / 4) <= 256) few *= 2;
+  hipLaunchKernelGGL(kv_join_k<T>, dim3(left, k.rows / per), dim3(256), 0, st, a, k.rows, per, few);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
 template <typename T>
@@ -948,6 +953,7 @@ extern "C" int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, c
   a.part = (float*)workspace;
   a.slots = cut.slots;
   a.least = cut.least;
+  a.by_pair = kv_most_tiles(a.b.tokens, a.b.batch, a.group, cut.rows) * a.c.heads <= cut.slots;
   hipStream_t st = (hipStream_t)hip_stream;
   switch (cache->dtype) {
     case PAHQ_F32: return attend_as<float>(st, a, cut);
