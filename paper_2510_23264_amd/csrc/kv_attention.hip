@@ -29,12 +29,15 @@ struct AttendArgs {
   int words, group;                                 // group: query heads of a cache head
   float scale, sign;                                // of the scores: times log2 e and positive; of the queries: its sign, 0 for a scale of 0
   float* part;                                      // [slot][rows][d] sums of a part, [slot][rows][2] maximum and sum, then how many of Left there are, and they
-  int slots, least;                                 // of ranges (kv_plan.h); slots 0: nothing is cut
+  int slots, least, over, enough, brief;            // of ranges (kv_plan.h); slots 0: nothing is cut
   int by_pair;                                      // Left are counted by tile and head, or by range: whichever are fewer
 };
 
 // The kernel's one argument, read again where it is asked for: kept for the whole kernel it would take more scalar registers than there are.
 // The kernels take nothing but it, so it begins their argument memory.
+template <typename T> __device__ __forceinline__ void in_global(T*& p) {       // memory loads know only that it is some address
+  p = (T*)(__attribute__((address_space(1))) T*)(uintptr_t)p;
+}
 __device__ __forceinline__ AttendArgs args_again() {
   uintptr_t p = (uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(p));
@@ -42,7 +45,17 @@ __device__ __forceinline__ AttendArgs args_again() {
   struct Words { uint64_t w[sizeof(AttendArgs) / 8]; } x;
 #pragma unroll
   for (unsigned i = 0; i < sizeof(AttendArgs) / 8; i++) x.w[i] = ((const __attribute__((address_space(4))) uint64_t*)p)[i];
-  return __builtin_bit_cast(AttendArgs, x);
+  AttendArgs a = __builtin_bit_cast(AttendArgs, x);
+  in_global(a.c.keys);
+  in_global(a.c.values);
+  in_global(a.b.starts);
+  in_global(a.b.lengths);
+  in_global(a.b.pages);
+  in_global(a.q.at);
+  in_global(a.out.at);
+  in_global(a.tree);
+  in_global(a.part);
+  return a;
 }
 
 // ---------------------------------------------------------------- a workgroup's part
@@ -70,7 +83,7 @@ template <int UNIT> __device__ __forceinline__ Share share_of(const AttendArgs& 
     x.s = kv_sequence(a.b, b);
     x.tiles = kv_tiles((long long)x.s.n * a.group, rows);
     x.pairs = kv_pairs(x.tiles, a.c.heads);
-    x.units = kv_units(x.pairs, x.s.length, UNIT);
+    x.units = kv_units(x.pairs, x.s.length, UNIT, a.over);
   }
   x.pairs_to = __builtin_elementwise_add_sat(wave_sum_up_to(x.pairs), pairs_before);
   x.units_to = __builtin_elementwise_add_sat(wave_sum_up_to(x.units), units_before);
@@ -104,11 +117,11 @@ template <int UNIT, bool KEEP> struct Finder {
       x = share_of<UNIT>(a, rows, b0, pairs, units);
       pairs = lane_of(x.pairs_to, 63);
       units = lane_of(x.units_to, 63);
-      longest = max(longest, x.tiles ? kv_units_of(x.s.length, UNIT) : 0);
+      longest = max(longest, x.tiles ? kv_units_of(x.s.length, UNIT, a.over) : 0);
     }
-    // a tile longer than the average range, somewhere: asked for every lane's longest
-    const uint32_t even = a.slots ? units / (uint32_t)a.slots : 0;
-    plan = kv_plan(units, a.slots && __any((uint32_t)longest > even), a.slots, a.least);
+    // a long tile somewhere, asked for every lane's longest
+    const uint32_t from = a.slots ? kv_cut_from(units, pairs, a.slots, a.enough, a.brief) : 0;
+    plan = kv_plan(units, a.slots && __any((uint32_t)longest > from), a.slots, a.least);
   }
   // Sequence with the `at`-th unit, or tile and head where tiles are given out whole: its lane of x, -1 for none
   __device__ __forceinline__ int lane_with(const AttendArgs& a, int rows, uint32_t at, bool by_units, int* b0) {
@@ -123,38 +136,49 @@ template <int UNIT, bool KEEP> struct Finder {
     return -1;
   }
   __device__ __forceinline__ KvSequence sequence(int l) const { return {lane_of(x.s.t0, l), lane_of(x.s.n, l), lane_of(x.s.length, l), lane_of(x.s.base, l)}; }
-  // What workgroup `wg` does at `at`, up to `stop` at most.  Returns how many units it takes, 0 if there is nothing.
+  // What workgroup `wg` does at `at`, up to `stop` at most.  Returns how many units that takes, 0 if there is nothing.
   __device__ __forceinline__ uint32_t next(const AttendArgs& a, int rows, int wg, uint32_t at, uint32_t stop, Item* it) {
-    int b0;
-    const int l = lane_with(a, rows, at, plan.wgs, &b0);
-    if (l < 0) return 0;
-    const uint32_t tiles = lane_of(x.tiles, l);
-    it->b = b0 + l;
-    it->s = sequence(l);
-    it->begin = 0;
-    it->slot = -1;
-    if (!plan.wgs) {                                // heads in turn, and the last tiles, which see the most rows, first
-      const uint32_t local = at - (lane_of(x.pairs_to, l) - lane_of(x.pairs, l)), heads = a.c.heads;
-      it->h = local % heads;
-      it->tile = tiles - 1 - local / heads;
-      it->end = tile_end(a, it->s, it->tile, rows);
-      return 1;
+    const uint32_t begun = at, over = (uint32_t)a.over;
+    int b0, l;
+    uint32_t tiles, pair, off, take, whole;
+    for (;;) {
+      l = lane_with(a, rows, at, plan.wgs, &b0);
+      if (l < 0) return 0;
+      it->b = b0 + l;
+      it->s = sequence(l);
+      it->begin = 0;
+      it->slot = -1;
+      tiles = lane_of(x.tiles, l);
+      if (!plan.wgs) {                              // heads in turn, and the last tiles, which see the most rows, first
+        const uint32_t local = at - (lane_of(x.pairs_to, l) - lane_of(x.pairs, l)), heads = a.c.heads;
+        it->h = local % heads;
+        it->tile = tiles - 1 - local / heads;
+        it->end = tile_end(a, it->s, it->tile, rows);
+        return 1;
+      }
+      const uint32_t local = at - (lane_of(x.units_to, l) - lane_of(x.units, l));
+      whole = kv_units_of(it->s.length, UNIT, a.over);
+      pair = local / whole;
+      off = local - pair * whole;
+      take = min(whole - off, stop - at);
+      at += take;
+      if (off + take > over) break;
+      if (at >= stop) return 0;
     }
-    const uint32_t local = at - (lane_of(x.units_to, l) - lane_of(x.units, l)), whole = kv_units_of(it->s.length, UNIT), pair = local / whole;
-    const uint32_t off = local - pair * whole, take = min(whole - off, stop - at);
     it->h = pair / tiles;
     it->tile = pair - it->h * tiles;
     it->end = tile_end(a, it->s, it->tile, rows);
-    it->begin = (int)min((uint32_t)min((uint64_t)off * UNIT, (uint64_t)KV_MAX_LENGTH), (uint32_t)it->end);
-    if (off + take < whole) it->end = min(it->end, (int)((off + take) * UNIT));
-    if (take < whole) it->slot = 2 * wg + (off ? 0 : 1);
-    if (!off && (take < whole || a.by_pair) && threadIdx.x == 0) {
+    const bool starts = off <= over, ends = off + take == whole;
+    if (!starts) it->begin = (int)min((uint32_t)min((uint64_t)(off - over) * UNIT, (uint64_t)KV_MAX_LENGTH), (uint32_t)it->end);
+    if (!ends) it->end = min(it->end, (int)((off + take - over) * UNIT));
+    if (!starts || !ends) it->slot = 2 * wg + starts;
+    if (starts && (!ends || a.by_pair) && threadIdx.x == 0) {
       const uint32_t number = lane_of(x.pairs_to, l) - lane_of(x.pairs, l) + pair;
       if (!a.by_pair || number < (uint32_t)a.slots)
         left_of(a, rows)[a.by_pair ? number : wg] = {it->s.t0, (int)min((long long)it->s.n * a.group - (long long)it->tile * rows, (long long)rows), it->tile, it->h,
-                                                     take < whole ? kv_holder(plan, at + whole - 1) - wg + 1 : 0, wg, {}};
+                                                     ends ? 0 : kv_holder(plan, at - take - off + whole - 1) - wg + 1, wg, {}};
     }
-    return take;
+    return at - begun;
   }
   // A range says first that it left nothing; the first one how many Left there are
   __device__ __forceinline__ void begin(const AttendArgs& a, int rows, int wg) const {
@@ -231,6 +255,7 @@ __device__ __forceinline__ float sum_of(v4f x, float acc) { return acc + ((x[0] 
 
 alignas(16) __device__ const uint32_t kv_chunk[4][4] = {{0, 0, 0, 0}, {0x7FC00000, 0x7FC00000, 0x7FC00000, 0x7FC00000},
                                                         {0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0}, {0x7E007E00, 0x7E007E00, 0x7E007E00, 0x7E007E00}};
+template <typename T> constexpr uint32_t SIGNS = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
 template <typename T> constexpr int NAN_CHUNK = sizeof(T) == 4 ? 1 : __is_same(T, bf16_t) ? 2 : 3;
 
 // Where chunk c of a row lies among the row's CH chunks.  Rows 4 apart in the low bits, so that four rows' 64 neighbouring bytes (what a
@@ -339,6 +364,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   F q[RT][CH / 4];
   {
     const AttendArgs k = args_again();
+    const uint32_t keep = k.sign == 0.f ? 0u : ~0u, flip = k.sign < 0.f ? SIGNS<T> : 0u;
 #pragma unroll
     for (int r = 0; r < RT; r++) {
       const long long row = (long long)it.tile * ROWS + 16 * r + l16;
@@ -349,10 +375,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
 #pragma unroll
       for (int s = 0; s < CH / 4; s++) {
         const int e0 = (h4 + 4 * s) * (16 / EB);
-        const Pack<T, 16 / EB> p = *(const Pack<T, 16 / EB>*)(x + (e0 < k.c.d ? e0 : 0));
-        const float sign = there && e0 < k.c.d ? k.sign : 0.f;
-#pragma unroll
-        for (int j = 0; j < 16 / EB; j++) q[r][s][j] = sign == 0.f ? (T)0.f : from_float<T>(as_float(p.v[j]) * sign);
+        q[r][s] = __builtin_bit_cast(F, (load16(x + (e0 < k.c.d ? e0 : 0)) & (there && e0 < k.c.d ? keep : 0u)) ^ flip);
       }
     }
   }
@@ -582,15 +605,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE_WAVES(
     F q[CH / 2];
     {
       const AttendArgs k = args_again();
+      const uint32_t keep = k.sign == 0.f ? 0u : ~0u, flip = k.sign < 0.f ? SIGNS<T> : 0u;
       const int g = there ? (int)(row - (long long)token * group) : 0;
       const T* const x = (const T*)(k.q.at + (it.s.t0 + (there ? token : 0)) * k.q.token + (h * group + g) * k.q.head);
 #pragma unroll
       for (int c = 0; c < CH / 2; c++) {
         const int e0 = (h2 + 2 * c) * N;
-        const Pack<T, N> p = *(const Pack<T, N>*)(x + (e0 < k.c.d ? e0 : 0));
-        const float sign = there && e0 < k.c.d ? k.sign : 0.f;
-#pragma unroll
-        for (int j = 0; j < N; j++) q[c][j] = sign == 0.f ? (T)0.f : from_float<T>(as_float(p.v[j]) * sign);
+        q[c] = __builtin_bit_cast(F, (load16(x + (e0 < k.c.d ? e0 : 0)) & (there && e0 < k.c.d ? keep : 0u)) ^ flip);
       }
     }
     // what the wave's rows see at least (unmasked) and at most: blocks behind the latter are left out
@@ -859,17 +880,46 @@ int attend_args(const pahq_kv_cache* cache, const pahq_kv_batch* batch, int q_he
   return PAHQ_OK;
 }
 
-// How a call is cut: the tile's rows, and ranges for so many workgroups, none shorter than `least` units
-struct Cut { int rows, slots, least; };
-Cut cut_of(const AttendArgs& a) {
+// How a call is cut.  What the host sees of it decides, as the size of the workspace does too.
+struct Cut {
+  int rows;                                         // of a tile
+  bool waves;                                       // of few rows: a workgroup has a compute unit to itself, and so many waves
+  int slots;                                        // ranges at most (kv_plan.h), 0: tiles are given out whole in any case
+  int least, over;                                  // units of a range at least, and what beginning a tile counts
+  int enough, brief;                                // where that pays, see kv_cut_from
+};
+Cut cut_of(const AttendArgs& a, int eb) {
   Cut k;
-  const long long mean = (((long long)a.b.tokens + a.b.batch - 1) / std::max(a.b.batch, 1)) * a.group;      // rows a sequence and head
-  k.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : 128;
-  k.slots = 512;
+  // Rows a sequence and head.  Every tile reads its sequence's rows of the cache, so they decide: 8 sequences of 64 tokens, 4 heads of a
+  // group, over up to 1024 rows take 44 us in tiles of 128 and 140 us in tiles of 16; 64 single tokens of 4 heads over up to 16384 rows
+  // take 172 us in tiles of 16 and 198 us in tiles of 128, which then mostly hold nothing.
+  const long long mean = (((long long)a.b.tokens + a.b.batch - 1) / std::max(a.b.batch, 1)) * a.group;
+  // heads of more than 128 columns in fp32 stay with 16: more rows of theirs do not fit the registers
+  k.rows = mean <= 16 || (eb == 4 && a.c.d > 128) ? 16 : mean <= 32 ? 32 : 128;
+  const long long tiles = kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows) * a.c.heads;
+  // Few tiles: one workgroup of many waves on a compute unit has half the parts to join, and 4 us less of 94 to do for a token over 131072
+  // rows.  Many short ones hide each other's beginnings in two workgroups (256 tokens over 1024 rows, 8 heads: 181 us instead of 198).
+  k.waves = k.rows < 128 && tiles < 1024;
+  k.slots = k.waves ? 256 : 512;
   k.least = 4;
-  // the new tokens alone are so much work that a piece is as long as any sequence can be
+  k.over = k.rows < 128 ? 2 : 5;
+  // Equal tiles, some for each range, are cut for the last ones would leave workgroups idle: 40 tokens over 4096 rows, 8 heads, 109 us
+  // instead of 138, 200 over 512 80 instead of 90, 200 over 2048 274 instead of 291; at eight for a range (500 over 1024) it would lose 2 %.
+  // Prompts' do not: the first tiles see little, and are done while the last ones run.
+  k.enough = k.rows < 128 ? 5 * k.slots : 0;
+  // What cutting costs in units: the parts' way through memory and the join, 5 to 15 us.  One token of 4 heads over 500 rows takes 12.5 us
+  // whole and 16.5 cut, over 1000 rows 19 and 17; 1500 tokens of a prompt 42 and 67; 128 behind 640 others 22 and 24, behind 1372 37 and 27.
+  // In fp32, whose units take longer, 300 tokens of a prompt 28 and 32, 100 behind 300 others 66 and 36.
+  k.brief = k.rows < 128 ? 8 : eb == 2 ? 18 : 12;
+  // Not even the longest sequence that the lists of pages have room for would be cut, or the new tokens alone are so much work that a range is as
+  // long as any sequence can be
+  const int wide = eb * (a.c.d <= 64 ? 64 : a.c.d <= 128 ? 128 : 256), unit = k.rows < 128 ? 32768 / wide : wide <= 256 ? 64 : 32;
+  const bool few = k.rows == 128 || tiles <= KV_FEW_TILES;
   const double work = (double)a.b.tokens * a.b.tokens * a.group / ((double)k.rows * std::max(a.b.batch, 1)) * a.c.heads / k.slots;
-  if (a.b.most <= 256 || a.b.most <= work) k.slots = 0;
+  if (a.b.most <= 256 || (few && kv_units_of(a.b.most, unit, k.over) <= k.brief) || a.b.most <= work) {
+    k.slots = 0;
+    k.waves = k.rows < 128 && tiles <= KV_FEW_TILES;
+  }
   return k;
 }
 size_t part_bytes(const AttendArgs& a, const Cut& k) { return k.slots ? 2ull * k.slots * k.rows * (a.c.d + 2) * 4 + 32 + k.slots * sizeof(Left) : 0; }
@@ -891,15 +941,19 @@ int launch(hipStream_t st, unsigned grid, const AttendArgs& a) {
 }
 template <typename T, int D>
 int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
-  constexpr int EB = sizeof(T), WIDE = D * EB, NW = WIDE <= 128 ? 4 : 2, FEW = 2 * NW * 2 * (EB == 2 ? 32 : 16) * WIDE + NW * 1024;
+  constexpr int EB = sizeof(T), WIDE = D * EB, STAGES = 4 * (EB == 2 ? 32 : 16) * WIDE;       // a wave's
+  constexpr int NW = std::max(2, 65536 / STAGES), MANY = std::max(NW, 131072 / STAGES);
   constexpr int KVB = WIDE <= 256 ? 64 : 32;
   const long long tiles = kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows), items = std::max<long long>(tiles * a.c.heads, k.slots);
   // threads of a launch are counted in 32 bits
   if (items >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
   const unsigned grid = (unsigned)items;
-  const int rc = k.rows == 16   ? launch<kv_few_k<T, D, 1, NW>, NW * 64, FEW>(st, grid, a)
-                 : k.rows == 32 ? launch<kv_few_k<T, D, 2, NW>, NW * 64, FEW>(st, grid, a)
-                                : launch<kv_tile_k<T, D, KVB>, 256, 4 * KVB * WIDE + 2048>(st, grid, a);
+  int rc = PAHQ_EHIP;
+  if (k.rows == 16) rc = k.waves ? launch<kv_few_k<T, D, 1, MANY>, MANY * 64, MANY * (STAGES + 1024)>(st, grid, a) : launch<kv_few_k<T, D, 1, NW>, NW * 64, NW * (STAGES + 1024)>(st, grid, a);
+  if constexpr (WIDE <= 512) {
+    if (k.rows == 32) rc = k.waves ? launch<kv_few_k<T, D, 2, MANY>, MANY * 64, MANY * (STAGES + 1024)>(st, grid, a) : launch<kv_few_k<T, D, 2, NW>, NW * 64, NW * (STAGES + 1024)>(st, grid, a);
+    if (k.rows == 128) rc = launch<kv_tile_k<T, D, KVB>, 256, 4 * KVB * WIDE + 2048>(st, grid, a);
+  }
   if (rc || !k.slots) return rc;
   // as many rows of a workgroup that its launch, a workgroup in 3 to 4 ns, does not take longer than what they do
   const int left = (int)std::min<long long>(tiles * a.c.heads, k.slots);
@@ -924,7 +978,7 @@ extern "C" int pahq_kv_attention_workspace(const pahq_kv_cache* cache, const pah
   KvRange held[2], lists[3];
   if (!bytes) return PAHQ_EINVAL;
   if (const int rc = attend_args(cache, batch, q_heads, &a, held, lists)) return rc;
-  *bytes = a.b.batch && a.b.tokens ? part_bytes(a, cut_of(a)) : 0;
+  *bytes = a.b.batch && a.b.tokens ? part_bytes(a, cut_of(a, dtype_bytes(cache->dtype))) : 0;
   return PAHQ_OK;
 }
 
@@ -937,7 +991,7 @@ extern "C" int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, c
   if (batch->batch == 0 || batch->tokens == 0) return PAHQ_OK;
   const int eb = dtype_bytes(cache->dtype), tokens = batch->tokens;
   if (!kv_rows_args(q, tokens, q_heads, a.c.d, eb, false, &a.q, &qr) || !kv_rows_args(out, tokens, q_heads, a.c.d, eb, true, &a.out, &outr)) return PAHQ_EINVAL;
-  const Cut cut = cut_of(a);
+  const Cut cut = cut_of(a, eb);
   const size_t need = part_bytes(a, cut);
   if (need && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return PAHQ_EINVAL;
   const KvRange masks = {tree, (size_t)tokens * words * 8}, space = {need ? workspace : nullptr, need};
@@ -953,6 +1007,9 @@ extern "C" int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, c
   a.part = (float*)workspace;
   a.slots = cut.slots;
   a.least = cut.least;
+  a.over = cut.over;
+  a.enough = cut.enough;
+  a.brief = cut.brief;
   a.by_pair = kv_most_tiles(a.b.tokens, a.b.batch, a.group, cut.rows) * a.c.heads <= cut.slots;
   hipStream_t st = (hipStream_t)hip_stream;
   switch (cache->dtype) {

@@ -2,11 +2,12 @@
 //
 // The rows of a sequence and a cache head are (new token, query head of the group) pairs, in tiles of `rows`; a tile's work is its
 // sequence's length, in units of some rows of the cache.  The host knows neither the lengths nor how the tokens are spread over the
-// sequences, so each workgroup finds its part from the batch.  Where no tile is longer than what a workgroup would do on average, tiles
+// sequences, so each workgroup finds its part from the batch.  Where it does not pay to cut them (kv_cut_from) tiles
 // are given out whole, as workgroups end.  Otherwise the units of all tiles, heads and sequences stand in one line, which is cut into
 // equal ranges for at most `slots` workgroups, about as many as the chip holds at a time: one long sequence beside short ones, or
 // one alone, takes the whole chip.  A range ends inside tiles at its ends only, so every workgroup leaves at most two parts
-// of tiles in the workspace: in slot 2 w what it began inside of a tile, in slot 2 w + 1 what it left unfinished.
+// of tiles in the workspace: in slot 2 w what it began inside of a tile, in slot 2 w + 1 what it left unfinished.  A tile's first `over`
+// units stand for what it costs to begin one; a range that ends among them leaves the tile to the next.
 #pragma once
 #include <stdint.h>
 
@@ -22,22 +23,27 @@ namespace pahq {
 
 constexpr int KV_MOST_ITEMS = 1 << 24;              // workgroups of a launch, whose threads are counted in 32 bits
 PAHQ_HD int kv_tiles(long long rows, int tile) { return (int)((rows + tile - 1) / tile); }
-PAHQ_HD int kv_units_of(int length, int unit) { return length <= unit ? 1 : (int)(((uint32_t)length + (uint32_t)unit - 1) / (uint32_t)unit); }
+PAHQ_HD int kv_units_of(int length, int unit, int over) { return over + (length <= unit ? 1 : (int)(((uint32_t)length + (uint32_t)unit - 1) / (uint32_t)unit)); }
 // Of a sequence: tiles of all heads, and their units.  Sums over a batch stick at 2^32 - 1, with more units than that tiles are given out
 // whole; starts that do not grow can name more tiles than there are, which is why a sequence's own are bounded.
 PAHQ_HD uint32_t kv_pairs(int tiles, int heads) {
   const uint64_t pairs = (uint64_t)(uint32_t)tiles * (uint32_t)heads;
   return pairs < KV_MOST_ITEMS ? (uint32_t)pairs : (uint32_t)KV_MOST_ITEMS;
 }
-PAHQ_HD uint32_t kv_units(uint32_t pairs, int length, int unit) {
-  const uint64_t units = (uint64_t)pairs * (uint32_t)kv_units_of(length, unit);
+PAHQ_HD uint32_t kv_units(uint32_t pairs, int length, int unit, int over) {
+  const uint64_t units = (uint64_t)pairs * (uint32_t)kv_units_of(length, unit, over);
   return units < 0xFFFFFFFFull ? (uint32_t)units : 0xFFFFFFFFu;
 }
 
+// Tiles are cut if one has more units than this.  Given out whole, they take as long as the longest of them, or as the average range, or,
+// where there are some more than can run at a time, until the last ones are done; cut, the average range and `brief` units more.
+constexpr uint32_t KV_FEW_TILES = 256;              // one for each compute unit
+PAHQ_HD uint32_t kv_cut_from(uint32_t units, uint32_t pairs, int slots, int enough, int brief) {
+  return pairs > KV_FEW_TILES && pairs < (uint32_t)enough ? 0 : units / (uint32_t)slots + (uint32_t)brief;
+}
 struct KvPlan { uint32_t units, wgs; };            // wgs 0: tiles are given out whole
-// uneven: some tile is longer than units / slots
-PAHQ_HD KvPlan kv_plan(uint32_t units, bool uneven, int slots, int least) {
-  if (!uneven || units == 0xFFFFFFFFu) return {units, 0};
+PAHQ_HD KvPlan kv_plan(uint32_t units, bool cut, int slots, int least) {
+  if (!cut || units == 0xFFFFFFFFu) return {units, 0};
   const uint32_t parts = units / (uint32_t)least;
   return {units, parts >= (uint32_t)slots ? (uint32_t)slots : parts > 1 ? parts : 1u};
 }
