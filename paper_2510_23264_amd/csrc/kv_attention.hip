@@ -7,6 +7,10 @@
 // Rows of the cache reach LDS without registers (global_load_lds), each 16 bytes a lane at an address of its own, which is what pages
 // need; their 16-byte chunks are XOR-swizzled by the row so that both products' reads spread over the banks.  What lies behind a
 // sequence's end comes from a chunk of zeros, what lies in a page that is none from a chunk of NaN.
+//
+// Scores, the running maxima, the sums and the output's sums are fp32.  The weights P are rounded once to the cache's 16-bit type, at most
+// half a step of each, because the second product then takes one pass of the matrix cores instead of three; the
+// fp32 cache has fp32 products and no such rounding.  exp2 instead of exp: log2 e is part of the scale.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <algorithm>
@@ -235,7 +239,11 @@ template <> struct Frag<float> {
     return c;
   }
 };
-// fp16 weights: times 2^7, so that those 2^-21 of the largest are still normal numbers, and 2^15 is the largest (the maximum lags by up to 2^8)
+// A row's maximum is not followed at every step: weights may exceed 1, and rescaling the sums, which costs a product for each of the
+// output's columns, is left out for nearly every block after the first ones.  Few rows of queries: the maximum is taken over when it has grown by
+// more than LAG (as a power of two).  Many: when the block's weights add up to more than OVER, which costs no maximum of the block.
+// fp16 weights are multiplied by 2^7, so that those down to 2^-21 of the largest are normal numbers; the lag of 2^8 makes 2^15 of the largest,
+// and a sum below OVER none larger than that: half of what fp16 holds.  The factor leaves with the division by the sum.
 template <typename T> constexpr float LIFT = sizeof(T) == 2 && !__is_same(T, bf16_t) ? 7.f : 0.f;
 constexpr float LAG = 8.f;
 constexpr float OVER = 32768.f;
@@ -332,8 +340,18 @@ __device__ __forceinline__ float of_kinds(float count) {
 }
 
 // ---------------------------------------------------------------- up to 16 RT rows of queries
+// For query row r:  O_r = sum_j 2^(s_rj - m) V_j / sum_j 2^(s_rj - m),  s_rj = scale log2(e) q_r . k_j over the rows j that r sees, in one
+// pass over K and V with m the running maximum.  Bound by memory: 2 d bytes-an-element for 4 d operations a query row.
+//
 // A wave takes blocks of KVB rows of the cache in turn with the others of its workgroup, into two stages of LDS of its own, so nothing waits for
-// another wave until the waves' sums meet at the end.  Bound by memory: every row of the cache is read once a tile.
+// another wave until the waves' sums meet at the end.  The stages of
+// a compute unit hold 128 KB, half of it on its way, which is what the latency of memory takes at 7 TB/s; one workgroup of MANY waves holds all,
+// two of NW waves each half (cut_of).  Rows are read once a tile, so the reads are marked as non-temporal: 173 us instead of 194 for the 64 tokens below.
+// RT = 2 serves 17 to 32 rows with one pass instead of two (16 sequences, 8 tokens of 4 heads, 4096 rows: 58 us, 63 in tiles of 16, 65 of 128).
+//
+// Measured, bf16, 8 heads of 128 columns for 32 of queries: 64 tokens over 1024 to 16384 rows, 1.07 GB, 172 us (6.2 TB/s); one token over 131072
+// rows, 537 MB, 87 us (6.1 TB/s); fp32, 12 heads of 64 columns, one token over 200 rows 9.5 us, most of it the launch and the reads of the lists, the
+// page's number and its rows, which wait for one another.
 template <typename T, int D, int RT, int NW>
 __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   typedef typename Frag<T>::type F;
@@ -571,8 +589,15 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
 }
 
 // ---------------------------------------------------------------- many rows of queries
-// Four waves of 32 rows each share blocks of KVB rows of the cache, in two stages of LDS: a block's products run while the next one
-// arrives.
+// The same sums.  Four waves of 32 rows each share blocks of KVB rows of the cache, in two stages of LDS: a block's products run while the next one
+// arrives.  4 d operations for each row of queries against 2 d elements for all 128 of them: bound by instructions, not memory.  32x32 products
+// rather than 16x16, for they read half of the LDS for the same work.  K and V are read from LDS AHEAD = 4 products before they are used, held
+// there by in_order(): left to the compiler each product waits for its own read (the prompt below: 552 us with one read ahead, 519 with two, 517
+// with four; more do not fit the registers).  KVB is 64 where two stages of it fit twice into LDS (32: 553 us), 32 for rows of more than 256 bytes.
+//
+// Measured, bf16, 8 heads of 128 columns for 32 of queries: a prompt of 8192 tokens 517 to 540 us (1.02 to 1.06 PFLOP/s; the matrix cores are busy for
+// about half of it, the exponentials, masks and roundings beside them take the other half of the issue slots); 8 trees of 64 tokens over up to 8000
+// rows 44 us; 512 tokens of a prompt 18 us.
 #define TILE_WAVES(wide) ((wide) <= 128 ? 3 : (wide) <= 256 ? 2 : 1)
 template <typename T, int D, int KVB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE_WAVES(D * sizeof(T)), TILE_WAVES(D * sizeof(T))))) void kv_tile_k(AttendArgs a) {
@@ -800,7 +825,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE_WAVES(
   }
 }
 
-// The parts of a tile become its rows: of the blockIdx.x-th Left, rows blockIdx.y * per and on, `few` at a time: for each of them the parts are
+// The parts of a tile become its rows: with m the largest of the parts' maxima,  O = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p,  in the parts'
+// order, so that a call's result does not depend on which workgroup ended first.  A launch of its own, not an atomic count at the end of the others: 4 us
+// of one token over 131072 rows; bound by the latency of the list and of a part behind it, so parts are read four at a time.
+// Of the blockIdx.x-th Left, rows blockIdx.y * per and on, `few` at a time: for each of them the parts are
 // shared out over the threads that are left beside four elements each, and joined in LDS.
 template <typename T>
 __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per, int few) {
@@ -891,7 +919,7 @@ struct Cut {
 Cut cut_of(const AttendArgs& a, int eb) {
   Cut k;
   // Rows a sequence and head.  Every tile reads its sequence's rows of the cache, so they decide: 8 sequences of 64 tokens, 4 heads of a
-  // group, over up to 1024 rows take 44 us in tiles of 128 and 140 us in tiles of 16; 64 single tokens of 4 heads over up to 16384 rows
+  // group, over up to 8000 rows take 44 us in tiles of 128 and 140 us in tiles of 16; 64 single tokens of 4 heads over up to 16384 rows
   // take 172 us in tiles of 16 and 198 us in tiles of 128, which then mostly hold nothing.
   const long long mean = (((long long)a.b.tokens + a.b.batch - 1) / std::max(a.b.batch, 1)) * a.group;
   // heads of more than 128 columns in fp32 stay with 16: more rows of theirs do not fit the registers

@@ -18,9 +18,12 @@ struct AppendArgs {
   int rot, q_heads, nt;                             // nt: tokens of a workgroup
 };
 
-// Elements [at, at + 8) of a head, turned where they belong to pairs, in steps of a pair for any rot and layout.
+// Keys and queries: pair i of a token at position p becomes (f cos - g sin, f sin + g cos) at p times the table's i-th frequency, in fp32, rounded
+// once.  Bound by memory: each element is read and written once, the cosines and sines are made once for a token and not for each of its heads.
 // A workgroup takes nt neighbouring tokens: their places and their cosines and sines into LDS, then the heads: of keys and queries an
-// item is V pairs (the last one of a head fewer) or V elements behind them, of values V elements.
+// item is V pairs (the last one of a head fewer) or V elements behind them, of values V elements: 16 bytes a read and write.
+// Measured: 8192 tokens, bf16, 8 heads of 128 columns for 32 of queries, 201 MB, 47 us (4.3 TB/s, a copy reaches 5.1); 4 tokens 5.1 us, which is
+// the launch and the reads of the lists that wait for one another.
 template <typename T, bool HALF>
 __global__ __launch_bounds__(256) void kv_append_k(AppendArgs a) {
   constexpr int V = 16 / sizeof(T), MOST = 32;
@@ -100,6 +103,8 @@ __global__ __launch_bounds__(256) void kv_append_k(AppendArgs a) {
 
 // A workgroup takes a head of a sequence, as many path nodes at a time as its threads hold 16 bytes of: it reads their rows, waits and
 // writes.  Sources grow and lie at or behind their targets, so no later read finds a row that an earlier step wrote.
+// A copy of little; measured: 192 sequences, up to 8 of 64 nodes, fp16, 12 heads of 64 columns 5 us, at most 9 MB: the launch and the reads of lists, paths
+// and pages' numbers, which wait for one another.
 __global__ __launch_bounds__(256) void kv_keep_k(KvCache c, KvBatch q, const int* paths, int depth, int row_bytes, int* new_lengths) {
   __shared__ int stay;
   const int b = blockIdx.x, h = blockIdx.y;
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(256) void kv_keep_k(KvCache c, KvBatch q, const int
 namespace {
 template <typename T>
 int append_as(hipStream_t st, AppendArgs a, int layout) {
-  // tokens of a workgroup: as many as give every thread a sine, fewer where the chip would not be full
+  // tokens of a workgroup: as many as give every thread a sine, fewer where the chip would not be full (four workgroups for each compute unit)
   a.nt = std::max(1, std::min(std::min(a.rot ? 512 / a.rot : 32, 32), a.b.tokens / 1024));
   const dim3 grid((a.b.tokens + a.nt - 1) / a.nt);
   const size_t lds = (size_t)a.nt * (a.rot / 2) * sizeof(float2);
