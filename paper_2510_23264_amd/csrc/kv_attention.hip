@@ -987,7 +987,7 @@ int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
   const int left = (int)std::min<long long>(tiles * a.c.heads, k.slots);
   int per = 1, few = 1;
   while (per < k.rows && left * (k.rows / per) > 2048) per *= 2;
-  while (few * 2 <= std::min(per, 4) && few * 2 * (a.c.d / 4) <= 256) few *= 2;
+  while (few * 2 <= std::min(per, 8) && few * 2 * (a.c.d / 4) <= 256) few *= 2;
   hipLaunchKernelGGL(kv_join_k<T>, dim3(left, k.rows / per), dim3(256), 0, st, a, k.rows, per, few);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
