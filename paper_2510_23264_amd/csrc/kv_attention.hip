@@ -79,7 +79,8 @@ __device__ __forceinline__ uint32_t wave_sum_up_to(uint32_t v) {
   return v;
 }
 // Sequences in lanes, 64 at a time from b0 on, and the sums of their tiles (with heads) and units up to and with each
-struct Share { KvSequence s; int tiles; uint32_t pairs, units, pairs_to, units_to; };
+struct Share { KvSequence s; int tiles, each; uint32_t pairs, units, pairs_to, units_to; };        // each: units of a tile, or of a couple of them
+__device__ __forceinline__ bool in_couples(const AttendArgs& a, int tiles) { return !a.tree && tiles > 1; }
 template <int UNIT> __device__ __forceinline__ Share share_of(const AttendArgs& a, int rows, int b0, uint32_t pairs_before, uint32_t units_before) {
   const int b = b0 + (threadIdx.x & 63);
   Share x = {};
@@ -87,7 +88,11 @@ template <int UNIT> __device__ __forceinline__ Share share_of(const AttendArgs& 
     x.s = kv_sequence(a.b, b);
     x.tiles = kv_tiles((long long)x.s.n * a.group, rows);
     x.pairs = kv_pairs(x.tiles, a.c.heads);
-    x.units = kv_units(x.pairs, x.s.length, UNIT, a.over);
+    if (a.slots) {
+      const bool couples = in_couples(a, x.tiles);
+      x.each = couples ? kv_couple_units(x.s.base, x.tiles, rows, a.group, UNIT, a.over) : kv_units_of(x.s.length, UNIT, a.over);
+      x.units = kv_units(couples ? kv_pairs((x.tiles + 1) / 2, a.c.heads) : x.pairs, x.each);
+    }
   }
   x.pairs_to = __builtin_elementwise_add_sat(wave_sum_up_to(x.pairs), pairs_before);
   x.units_to = __builtin_elementwise_add_sat(wave_sum_up_to(x.units), units_before);
@@ -101,11 +106,8 @@ struct Item {
   KvSequence s;
   int b, tile, h, begin, end, slot;                 // rows of the cache; slot in the workspace, -1: the whole tile
 };
-// How many rows of the cache a tile sees at most
 __device__ __forceinline__ int tile_end(const AttendArgs& a, const KvSequence& s, int tile, int rows) {
-  if (a.tree) return s.length;
-  const int last = min(s.n - 1, (int)((((long long)tile + 1) * rows - 1) / a.group));
-  return max(s.base + last + 1, 0);
+  return a.tree ? s.length : kv_tile_end(s.n, s.base, tile, rows, a.group);
 }
 // Where a workgroup finds its part; every wave looks by itself.  Of up to 64 sequences KEEP keeps what was read.
 template <int UNIT, bool KEEP> struct Finder {
@@ -144,7 +146,7 @@ template <int UNIT, bool KEEP> struct Finder {
   __device__ __forceinline__ uint32_t next(const AttendArgs& a, int rows, int wg, uint32_t at, uint32_t stop, Item* it) {
     const uint32_t begun = at, over = (uint32_t)a.over;
     int b0, l;
-    uint32_t tiles, pair, off, take, whole;
+    uint32_t tiles, off, take, whole;
     for (;;) {
       l = lane_with(a, rows, at, plan.wgs, &b0);
       if (l < 0) return 0;
@@ -160,24 +162,32 @@ template <int UNIT, bool KEEP> struct Finder {
         it->end = tile_end(a, it->s, it->tile, rows);
         return 1;
       }
-      const uint32_t local = at - (lane_of(x.units_to, l) - lane_of(x.units, l));
-      whole = kv_units_of(it->s.length, UNIT, a.over);
-      pair = local / whole;
-      off = local - pair * whole;
-      take = min(whole - off, stop - at);
+      const bool couples = in_couples(a, tiles);
+      const uint32_t local = at - (lane_of(x.units_to, l) - lane_of(x.units, l)), each = lane_of(x.each, l), lines = couples ? (tiles + 1) / 2 : tiles;
+      const uint32_t line = local / each, in = local - line * each;
+      it->h = line / lines;
+      const int i = line - it->h * lines;
+      it->tile = couples ? (int)tiles - 1 - i : i;
+      off = in;
+      whole = kv_units_of(tile_end(a, it->s, it->tile, rows), UNIT, a.over);
+      if (off >= whole && i != it->tile) {          // behind the late tile the early one
+        off -= whole;
+        it->tile = i;
+        whole = kv_units_of(tile_end(a, it->s, i, rows), UNIT, a.over);
+      }
+      const bool work = off < whole;
+      take = min(work ? whole - off : each - in, stop - at);
       at += take;
-      if (off + take > over) break;
+      if (work && off + take > over) break;
       if (at >= stop) return 0;
     }
-    it->h = pair / tiles;
-    it->tile = pair - it->h * tiles;
     it->end = tile_end(a, it->s, it->tile, rows);
     const bool starts = off <= over, ends = off + take == whole;
     if (!starts) it->begin = (int)min((uint32_t)min((uint64_t)(off - over) * UNIT, (uint64_t)KV_MAX_LENGTH), (uint32_t)it->end);
     if (!ends) it->end = min(it->end, (int)((off + take - over) * UNIT));
     if (!starts || !ends) it->slot = 2 * wg + starts;
     if (starts && (!ends || a.by_pair) && threadIdx.x == 0) {
-      const uint32_t number = lane_of(x.pairs_to, l) - lane_of(x.pairs, l) + pair;
+      const uint32_t number = lane_of(x.pairs_to, l) - lane_of(x.pairs, l) + it->h * tiles + it->tile;
       if (!a.by_pair || number < (uint32_t)a.slots)
         left_of(a, rows)[a.by_pair ? number : wg] = {it->s.t0, (int)min((long long)it->s.n * a.group - (long long)it->tile * rows, (long long)rows), it->tile, it->h,
                                                      ends ? 0 : kv_holder(plan, at - take - off + whole - 1) - wg + 1, wg, {}};

@@ -30,8 +30,8 @@ PAHQ_HD uint32_t kv_pairs(int tiles, int heads) {
   const uint64_t pairs = (uint64_t)(uint32_t)tiles * (uint32_t)heads;
   return pairs < KV_MOST_ITEMS ? (uint32_t)pairs : (uint32_t)KV_MOST_ITEMS;
 }
-PAHQ_HD uint32_t kv_units(uint32_t pairs, int length, int unit, int over) {
-  const uint64_t units = (uint64_t)pairs * (uint32_t)kv_units_of(length, unit, over);
+PAHQ_HD uint32_t kv_units(uint32_t pairs, int each) {
+  const uint64_t units = (uint64_t)pairs * (uint32_t)each;
   return units < 0xFFFFFFFFull ? (uint32_t)units : 0xFFFFFFFFu;
 }
 
@@ -40,6 +40,21 @@ PAHQ_HD uint32_t kv_units(uint32_t pairs, int length, int unit, int over) {
 constexpr uint32_t KV_FEW_TILES = 256;              // one for each compute unit
 PAHQ_HD uint32_t kv_cut_from(uint32_t units, uint32_t pairs, int slots, int enough, int brief) {
   return pairs > KV_FEW_TILES && pairs < (uint32_t)enough ? 0 : units / (uint32_t)slots + (uint32_t)brief;
+}
+// How many rows of the cache a tile sees at most, its sequence having n new tokens behind base others; (token, query head) pairs are fewer than
+// KV_MAX_LENGTH, so that a tile more of them is counted in 32 bits
+PAHQ_HD int kv_tile_end(int n, int base, int tile, int rows, int group) {
+  const int last = (int)((((uint32_t)tile + 1) * (uint32_t)rows - 1) / (uint32_t)group), end = base + (last < n - 1 ? last : n - 1) + 1;
+  return end > 0 ? end : 0;
+}
+// Of a causal sequence's T > 1 tiles the late ones see more, and a line of tiles that count the same would leave those who find early ones idle.  Tile T - 1 - i
+// and tile i together see about as much for every i, so the line is made of such couples, whose units this bounds: their ends add up to at
+// most 2 base + ((T + 1) rows - 2) / group + 2, and two quotients rounded up are at most two above the rounded-down quotient of their sum.  What is
+// left of a couple's units, or of the middle tile's, is nobody's work.  A prompt of 4096 tokens in fp32, 12 heads of 64 columns: 260 us, 385 with tiles
+// that count the same.
+PAHQ_HD int kv_couple_units(int base, int tiles, int rows, int group, int unit, int over) {
+  const uint32_t behind = base > 0 ? (uint32_t)base : 0, ends = (((uint32_t)tiles + 1) * (uint32_t)rows - 2) / (uint32_t)group + 2;
+  return 2 * over + (int)(behind / (uint32_t)unit * 2 + (ends + behind % (uint32_t)unit * 2) / (uint32_t)unit) + 2;
 }
 struct KvPlan { uint32_t units, wgs; };            // wgs 0: tiles are given out whole
 PAHQ_HD KvPlan kv_plan(uint32_t units, bool cut, int slots, int least) {

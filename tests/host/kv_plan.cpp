@@ -6,7 +6,25 @@
 #include "kv_plan.h"
 using namespace pahq;
 
-int main() {
+// A line "n length rows group unit over": tiles, a couple's units, and the most and the fewest that two tiles of one have
+int couples() {
+  int n, length, rows, group, unit, over;
+  while (std::scanf("%d %d %d %d %d %d", &n, &length, &rows, &group, &unit, &over) == 6) {
+    const int tiles = kv_tiles((long long)n * group, rows), base = length - n;
+    int most = 0, fewest = 1 << 30;
+    for (int i = 0; i < tiles / 2; i++) {
+      int sum = 0;
+      for (const int tile : {i, tiles - 1 - i}) sum += kv_units_of(kv_tile_end(n, base, tile, rows, group), unit, over);
+      most = std::max(most, sum);
+      fewest = std::min(fewest, sum);
+    }
+    std::printf("%d %d %d %d\n", tiles, kv_couple_units(base, tiles, rows, group, unit, over), most, fewest);
+  }
+  return 0;
+}
+
+int main(int argc, char**) {
+  if (argc > 1) return couples();
   int slots, least, over, brief, enough, unit, n;
   while (std::scanf("%d %d %d %d %d %d %d", &slots, &least, &over, &brief, &enough, &unit, &n) == 7) {
     std::vector<uint32_t> of;                       // units of each tile, in the line's order
@@ -16,7 +34,7 @@ int main() {
       if (std::scanf("%d %d %d", &tiles, &heads, &length) != 3) return 1;
       const uint32_t p = kv_pairs(tiles, heads), u = kv_units_of(length, unit, over);
       pairs += p;
-      units += kv_units(p, length, unit, over);
+      units += kv_units(p, u);
       if (p) longest = std::max(longest, u);
       of.insert(of.end(), p, u);
     }

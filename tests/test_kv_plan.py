@@ -20,10 +20,10 @@ def plan(tmp_path_factory):
     exe = str(tmp_path_factory.mktemp("plan") / "kv_plan")
     subprocess.run(["g++", "-std=c++17", "-O1", "-I" + CSRC, os.path.join(ROOT, "tests", "host", "kv_plan.cpp"), "-o", exe], check=True)
 
-    def run(calls):
+    def run(calls, *mode):
         """For each (rule, unit, [(tiles, heads, length)]): ranges, units, the longest tile's, the longest range's, and whether all is in its place."""
-        text = "".join(" ".join(map(str, (*rule, unit, len(batch), *(v for s in batch for v in s)))) + "\n" for rule, unit, batch in calls)
-        out = subprocess.run([exe], input=text, stdout=subprocess.PIPE, text=True, check=True).stdout.splitlines()
+        text = "".join(" ".join(map(str, c if mode else (*c[0], c[1], len(c[2]), *(v for s in c[2] for v in s)))) + "\n" for c in calls)
+        out = subprocess.run([exe, *mode], input=text, stdout=subprocess.PIPE, text=True, check=True).stdout.splitlines()
         assert len(out) == len(calls)
         return [tuple(map(int, x.split())) for x in out]
     return run
@@ -58,6 +58,21 @@ def test_where_tiles_are_cut(plan):
     assert plan([(FEW, 128, [(1, 8, 4096)] * 200 + [(1, 8, 200000)])])[0][0] == 256
     # units that 32 bits do not count
     assert plan([(FEW, 1, [(1, 8, 2 ** 31 - 70000)])])[0][1] == 2 ** 32 - 1 and plan([(FEW, 1, [(1, 8, 2 ** 31 - 70000)])])[0][0] == 0
+
+
+def test_couples_of_tiles_fit_their_units(plan):
+    """A late and an early tile of a causal sequence together: never more than what the line counts for them, and at most four units and a tile's rows less."""
+    rng = random.Random(8)
+    calls = []
+    for _ in range(20000):
+        rows, group, unit = rng.choice([16, 32, 128]), rng.choice([1, 2, 3, 4, 7, 16, 33, 130]), rng.choice([32, 64, 128, 256])
+        n = int(2 ** rng.uniform(0, 13))
+        calls.append((n, rng.choice([n, n + int(2 ** rng.uniform(0, 30)), rng.randrange(n + 1), 0, 2 ** 31 - 70000]), rows, group, unit, rng.choice([2, 5])))
+    for (n, length, rows, group, unit, over), (tiles, each, most, fewest) in zip(calls, plan(calls, "couples")):
+        if tiles > 1:
+            assert most <= each
+            if length >= n:
+                assert each - fewest <= 4 + (rows // group + 2) // unit, (n, length, rows, group, unit)
 
 
 @pytest.mark.parametrize("source", ["kv_attention", "kv_cache"])
