@@ -987,9 +987,11 @@ int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
   if (items >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
   const unsigned grid = (unsigned)items;
   int rc = PAHQ_EHIP;
-  if (k.rows == 16) rc = k.waves ? launch<kv_few_k<T, D, 1, MANY>, MANY * 64, MANY * (STAGES + 1024)>(st, grid, a) : launch<kv_few_k<T, D, 1, NW>, NW * 64, NW * (STAGES + 1024)>(st, grid, a);
+  if (k.rows == 16) rc = k.waves ? launch<kv_few_k<T, D, 1, MANY>, MANY * 64, MANY * (STAGES + 1024)>(st, grid, a)
+                                 : launch<kv_few_k<T, D, 1, NW>, NW * 64, NW * (STAGES + 1024)>(st, grid, a);
   if constexpr (WIDE <= 512) {
-    if (k.rows == 32) rc = k.waves ? launch<kv_few_k<T, D, 2, MANY>, MANY * 64, MANY * (STAGES + 1024)>(st, grid, a) : launch<kv_few_k<T, D, 2, NW>, NW * 64, NW * (STAGES + 1024)>(st, grid, a);
+    if (k.rows == 32) rc = k.waves ? launch<kv_few_k<T, D, 2, MANY>, MANY * 64, MANY * (STAGES + 1024)>(st, grid, a)
+                                   : launch<kv_few_k<T, D, 2, NW>, NW * 64, NW * (STAGES + 1024)>(st, grid, a);
     if (k.rows == 128) rc = launch<kv_tile_k<T, D, KVB>, 256, 4 * KVB * WIDE + 2048>(st, grid, a);
   }
   if (rc || !k.slots) return rc;
