@@ -608,9 +608,9 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
 // Measured, bf16, 8 heads of 128 columns for 32 of queries: a prompt of 8192 tokens 517 to 540 us (1.02 to 1.06 PFLOP/s; the matrix cores are busy for
 // about half of it, the exponentials, masks and roundings beside them take the other half of the issue slots); 8 trees of 64 tokens over up to 8000
 // rows 44 us; 512 tokens of a prompt 18 us.
-#define TILE_WAVES(wide) ((wide) <= 128 ? 3 : (wide) <= 256 ? 2 : 1)
+template <typename T, int D> constexpr int TILE_WAVES = D * sizeof(T) <= 128 ? 3 : D * sizeof(T) <= 256 ? 2 : 1;       // of a SIMD
 template <typename T, int D, int KVB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE_WAVES(D * sizeof(T)), TILE_WAVES(D * sizeof(T))))) void kv_tile_k(AttendArgs a) {
+__global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs a) {
   typedef typename Frag<T>::type F;
   constexpr int EB = sizeof(T), CH = D * EB / 16, KT = KVB / 32, NW = 4, ROWS = 32 * NW, N = 16 / EB;
   constexpr int HALF = KVB * D * EB, MINE = KVB / NW, ASKS = HALF / 1024 / NW, DT = D / 32;
