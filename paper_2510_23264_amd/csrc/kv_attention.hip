@@ -495,7 +495,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; i++) {
           p[r][t][i] = __builtin_amdgcn_exp2f(p[r][t][i] - from);
-          l[r] += p[r][t][i];
+          if (EB == 4) l[r] += p[r][t][i];
         }
     }
     const int vrow = 4 * h4 + (EB == 2 ? l16 / 4 : 0);
@@ -504,9 +504,11 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     if constexpr (EB == 2) {
       F w[RT];
 #pragma unroll
-      for (int r = 0; r < RT; r++)
+      for (int r = 0; r < RT; r++) {
 #pragma unroll
         for (int j = 0; j < 8; j++) w[r][j] = (T)p[r][j / 4][j % 4];
+        l[r] = sum_of(w[r], l[r]);                               // of the weights as they multiply the values
+      }
 #pragma unroll
       for (int d = 0; d < DT; d++) {
         union { F f; v4s half[2]; } v;
