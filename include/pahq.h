@@ -555,7 +555,7 @@ int pahq_kv_append(void* hip_stream, const pahq_kv_cache* cache, const pahq_kv_b
 
 /* pahq_kv_attention: the new tokens' queries over their sequences' rows.  Query head h goes with cache head h / (q_heads / heads);
  * heads divides q_heads.  For new token i of sequence b, over the rows j < lengths[b] it sees,
- *     out = sum_j p_j values_j,  p_j = exp(s_j - max s) / sum exp(s - max s),  s_j = scale * (q . keys_j),  scale finite
+ *     out = sum_j p_j values_j,  p_j = exp(s_j - max s) / sum exp(s - max s),  s_j = scale * (q . keys_j),  scale finite, times log2 e as well (up to 2.358e38)
  * It sees the rows in front of the new ones, j < base_b, and of the new ones
  *     tree NULL   those up to itself, j - base_b <= i
  *     tree        uint64 [tokens][words >= 1]: those whose bit (j - base_b) % 64 of word (j - base_b) / 64 of its row is set (none behind

@@ -1029,7 +1029,8 @@ extern "C" int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, c
   AttendArgs a = {};
   KvRange held[2], lists[3], qr, outr;
   if (const int rc = attend_args(cache, batch, q_heads, &a, held, lists)) return rc;
-  if (words < (tree ? 1 : 0) || (uintptr_t)tree % 8 || !std::isfinite(scale * 1.4426950408889634)) return PAHQ_EINVAL;
+  const float factor = (float)(std::fabs((double)scale) * 1.4426950408889634);        // of the scores, for exp2
+  if (words < (tree ? 1 : 0) || (uintptr_t)tree % 8 || !std::isfinite(factor)) return PAHQ_EINVAL;
   if (batch->batch == 0 || batch->tokens == 0) return PAHQ_OK;
   const int eb = dtype_bytes(cache->dtype), tokens = batch->tokens;
   if (!kv_rows_args(q, tokens, q_heads, a.c.d, eb, false, &a.q, &qr) || !kv_rows_args(out, tokens, q_heads, a.c.d, eb, true, &a.out, &outr)) return PAHQ_EINVAL;
@@ -1043,9 +1044,8 @@ extern "C" int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, c
   if (!in_place && !kv_rows_apart(a.out, outr, q_heads, a.q, qr, q_heads, (size_t)a.c.d * eb)) return PAHQ_EINVAL;
   a.tree = (const unsigned long long*)tree;
   a.words = words;
-  a.scale = (float)(std::fabs((double)scale) * 1.4426950408889634);
-  a.sign = scale < 0.f ? -1.f : a.scale > 0.f ? 1.f : 0.f;
-  if (!(a.scale > 0.f)) a.scale = 1.f;
+  a.scale = factor > 0.f ? factor : 1.f;
+  a.sign = scale < 0.f ? -1.f : factor > 0.f ? 1.f : 0.f;
   a.part = (float*)workspace;
   a.slots = cut.slots;
   a.least = cut.least;

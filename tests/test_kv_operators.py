@@ -94,6 +94,15 @@ def test_attention_refuses(P, change, code):
     assert attention(P, **change) == code
 
 
+@pytest.mark.parametrize("scale", [2.36e38, 3e38, -2.36e38, -3.4e38])
+def test_attention_refuses_scales_that_overflow(P, scale):
+    """Finite, but not what the scores are multiplied by: scale * log2 e, in fp32, is at most 3.4028e38."""
+    assert attention(P, scale=scale) == EINVAL
+    # what does not overflow gets as far as the next check, of the workspace
+    assert attention(P, scale=2.358e38, workspace=None) == EINVAL and attention(P, scale=scale, batch_tokens=0) == EINVAL
+    assert attention(P, scale=2.358e38, batch_tokens=0) == 0
+
+
 @pytest.mark.parametrize("change, code", [
     (dict(paths=None), EINVAL), (dict(after=None), EINVAL), (dict(depth=-1), EINVAL), (dict(paths=13 * A + 2), EINVAL), (dict(after=14 * A + 1), EINVAL), (dict(after=4 * A), EINVAL),
     (dict(after=3 * A + 8), EINVAL), (dict(after=5 * A), EINVAL), (dict(after=13 * A + 12), EINVAL), (dict(after=A), EINVAL), (dict(paths=2 * A), EINVAL), (dict(batch_batch=0, paths=None, after=None), 0)])
