@@ -564,9 +564,13 @@ int pahq_kv_append(void* hip_stream, const pahq_kv_cache* cache, const pahq_kv_b
  * What a query does not see has no influence on it, infinities and NaN included.  One that sees nothing, or only scores of -inf, gets
  * zeros.  Products in the cache's dtype with sums in fp32, softmax in fp32, its weights rounded to the dtype for their product
  * with the values, the sum divided by the weights' sum and rounded once.  The same call gives the same bits.
- * q, out as in pahq_kv_append; out may be q itself with the same strides.  tokens * (q_heads / heads) below 2^31 - 2^16.
+ * q, out as in pahq_kv_append; out may be q itself with the same strides.  tokens * (q_heads / heads) below 2^31 - 2^16; more than that is too
+ * big, as are 2^24 tiles of 16 to 128 (token, query head) pairs of one cache head and sequence: fewer where tokens * q_heads / 16 + batch * heads
+ * is below 2^24.
  * workspace: DEVICE, 16-byte aligned, of at least the bytes that pahq_kv_attention_workspace says for the same arguments (may be 0); its
- * contents are lost, and calls that overlap need one each. */
+ * contents are lost, and calls that overlap need one each.  The host does not know the lengths and goes by the room in the lists of pages:
+ * where that is for more than some hundred rows, 4 (d_head + 2) bytes for each of 8192 (single tokens) to 131072 (more than 32 rows a
+ * sequence and head) rows of queries: 4.3 to 68 MB for 128 columns, 8.5 to 135 MB for 256. */
 int pahq_tree_bits(const int32_t* parents, int32_t n, uint64_t* bits);
 int pahq_kv_attention_workspace(const pahq_kv_cache* cache, const pahq_kv_batch* batch, int32_t q_heads, size_t* bytes);
 int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, const pahq_kv_batch* batch, const pahq_kv_rows* q, int32_t q_heads,

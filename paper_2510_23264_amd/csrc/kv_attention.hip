@@ -928,6 +928,7 @@ struct Cut {
   int least, over;                                  // units of a range at least, and what beginning a tile counts
   int enough, brief;                                // where that pays, see kv_cut_from
 };
+long long tiles_of(const AttendArgs& a, const Cut& k) { return kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows) * a.c.heads; }
 Cut cut_of(const AttendArgs& a, int eb) {
   Cut k;
   // Rows a sequence and head.  Every tile reads its sequence's rows of the cache, so they decide: 8 sequences of 64 tokens, 4 heads of a
@@ -936,7 +937,7 @@ Cut cut_of(const AttendArgs& a, int eb) {
   const long long mean = (((long long)a.b.tokens + a.b.batch - 1) / std::max(a.b.batch, 1)) * a.group;
   // heads of more than 128 columns in fp32 stay with 16: more rows of theirs do not fit the registers
   k.rows = mean <= 16 || (eb == 4 && a.c.d > 128) ? 16 : mean <= 32 ? 32 : 128;
-  const long long tiles = kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows) * a.c.heads;
+  const long long tiles = tiles_of(a, k);
   // Few tiles: one workgroup of many waves on a compute unit has half the parts to join, and 4 us less of 94 to do for a token over 131072
   // rows.  Many short ones hide each other's beginnings in two workgroups (256 tokens over 1024 rows, 8 heads: 181 us instead of 198).
   k.waves = k.rows < 128 && tiles < 1024;
@@ -984,10 +985,8 @@ int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
   constexpr int EB = sizeof(T), WIDE = D * EB, STAGES = 4 * (EB == 2 ? 32 : 16) * WIDE;       // a wave's
   constexpr int NW = std::max(2, 65536 / STAGES), MANY = std::max(NW, 131072 / STAGES);
   constexpr int KVB = WIDE <= 256 ? 64 : 32;
-  const long long tiles = kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows), items = std::max<long long>(tiles * a.c.heads, k.slots);
-  // threads of a launch are counted in 32 bits
-  if (items >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
-  const unsigned grid = (unsigned)items;
+  const long long tiles = tiles_of(a, k);
+  const unsigned grid = (unsigned)std::max<long long>(tiles, k.slots);
   int rc = PAHQ_EHIP;
   if (k.rows == 16) rc = k.waves ? launch<kv_few_k<T, D, 1, MANY>, MANY * 64, MANY * (STAGES + 1024)>(st, grid, a)
                                  : launch<kv_few_k<T, D, 1, NW>, NW * 64, NW * (STAGES + 1024)>(st, grid, a);
@@ -998,7 +997,7 @@ int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
   }
   if (rc || !k.slots) return rc;
   // as many rows of a workgroup that its launch, a workgroup in 3 to 4 ns, does not take longer than what they do
-  const int left = (int)std::min<long long>(tiles * a.c.heads, k.slots);
+  const int left = (int)std::min<long long>(tiles, k.slots);
   int per = 1, few = 1;
   while (per < k.rows && left * (k.rows / per) > 2048) per *= 2;
   while (few * 2 <= std::min(per, 8) && few * 2 * (a.c.d / 4) <= 256) few *= 2;
@@ -1020,7 +1019,11 @@ extern "C" int pahq_kv_attention_workspace(const pahq_kv_cache* cache, const pah
   KvRange held[2], lists[3];
   if (!bytes) return PAHQ_EINVAL;
   if (const int rc = attend_args(cache, batch, q_heads, &a, held, lists)) return rc;
-  *bytes = a.b.batch && a.b.tokens ? part_bytes(a, cut_of(a, dtype_bytes(cache->dtype))) : 0;
+  *bytes = 0;
+  if (a.b.batch == 0 || a.b.tokens == 0) return PAHQ_OK;
+  const Cut cut = cut_of(a, dtype_bytes(cache->dtype));
+  if (tiles_of(a, cut) >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
+  *bytes = part_bytes(a, cut);
   return PAHQ_OK;
 }
 
@@ -1035,6 +1038,7 @@ extern "C" int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, c
   const int eb = dtype_bytes(cache->dtype), tokens = batch->tokens;
   if (!kv_rows_args(q, tokens, q_heads, a.c.d, eb, false, &a.q, &qr) || !kv_rows_args(out, tokens, q_heads, a.c.d, eb, true, &a.out, &outr)) return PAHQ_EINVAL;
   const Cut cut = cut_of(a, eb);
+  if (tiles_of(a, cut) >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;      // workgroups of a launch, whose threads are counted in 32 bits
   const size_t need = part_bytes(a, cut);
   if (need && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return PAHQ_EINVAL;
   const KvRange masks = {tree, (size_t)tokens * words * 8}, space = {need ? workspace : nullptr, need};
@@ -1052,7 +1056,7 @@ extern "C" int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, c
   a.over = cut.over;
   a.enough = cut.enough;
   a.brief = cut.brief;
-  a.by_pair = kv_most_tiles(a.b.tokens, a.b.batch, a.group, cut.rows) * a.c.heads <= cut.slots;
+  a.by_pair = tiles_of(a, cut) <= cut.slots;
   hipStream_t st = (hipStream_t)hip_stream;
   switch (cache->dtype) {
     case PAHQ_F32: return attend_as<float>(st, a, cut);

@@ -103,6 +103,20 @@ def test_attention_refuses_scales_that_overflow(P, scale):
     assert attention(P, scale=2.358e38, batch_tokens=0) == 0
 
 
+@pytest.mark.parametrize("tokens, heads, group, batch", [(65535, 2, 32767, 1), (16448, 65280, 1, 16448), ((1 << 24) - 1, 129, 1, 1)])
+def test_tiles_beyond_a_launch_are_too_big_for_the_workspace_too(P, tokens, heads, group, batch):
+    """2^24 tiles and more: the size of the workspace is refused as the call is."""
+    q_heads = heads * group
+    rows = (8 * A, q_heads * 64, 64)
+    change = dict(cache_heads=heads, cache_head_stride=1024, cache_page_stride=1024 * heads, cache_values=1 << 40, batch_batch=batch, batch_tokens=tokens, q_heads=q_heads,
+                  q=rows, out=(1 << 52,) + rows[1:], batch_starts=1 << 41, batch_lengths=1 << 42, batch_pages=1 << 43, workspace=1 << 44)
+    assert attention(P, **dict(change)) == ETOOBIG
+    left = dict(change)
+    cache, batch_arg, _ = structs(P, left)
+    n = C.c_size_t()
+    assert P.lib().pahq_kv_attention_workspace(cache, batch_arg, q_heads, C.byref(n)) == ETOOBIG
+
+
 @pytest.mark.parametrize("change, code", [
     (dict(paths=None), EINVAL), (dict(after=None), EINVAL), (dict(depth=-1), EINVAL), (dict(paths=13 * A + 2), EINVAL), (dict(after=14 * A + 1), EINVAL), (dict(after=4 * A), EINVAL),
     (dict(after=3 * A + 8), EINVAL), (dict(after=5 * A), EINVAL), (dict(after=13 * A + 12), EINVAL), (dict(after=A), EINVAL), (dict(paths=2 * A), EINVAL), (dict(batch_batch=0, paths=None, after=None), 0)])
