@@ -238,9 +238,12 @@ def rotary_entries(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=
 def tree_words(parents):
     """uint64 [n][(n + 63) / 64]: of every node of a drafted tree, bits of itself and its ancestors (pahq_tree_bits).  parents [n]: each
     node's parent, which comes before it, -1 at a root."""
-    parents = np.ascontiguousarray(parents, dtype=np.int32)
-    if parents.ndim != 1:
-        raise ValueError("parents: one number a node")
+    given = np.asarray(parents)
+    if given.ndim != 1 or (given.size and given.dtype.kind not in "iu"):
+        raise ValueError("parents: one whole number a node")
+    if given.size and not -1 <= int(given.min()) <= int(given.max()) < given.size:       # beyond 32 bits among them
+        raise PahqError(-1, "pahq_tree_bits")
+    parents = np.ascontiguousarray(given, dtype=np.int32)
     out = np.zeros((len(parents), max(1, -(-len(parents) // 64))), dtype=np.uint64)
     _chk(lib().pahq_tree_bits(_ptr(parents, C.c_int32), len(parents), _ptr(out, C.c_uint64)), "pahq_tree_bits")
     return out

@@ -140,6 +140,18 @@ def test_masks_of_trees(P):
     assert P.lib().pahq_tree_bits(None, 1, None) == EINVAL and P.lib().pahq_tree_bits(None, -1, None) == EINVAL
 
 
+def test_parents_are_whole_numbers_that_are_nodes(P):
+    """Numbers that 32 bits would turn into others, and fractions that would be cut off."""
+    import numpy as np
+    for bad in (np.array([2 ** 32 - 1]), np.array([-1, 2 ** 32]), np.array([-1, -2 ** 32 - 1]), np.array([-1, 2 ** 64 - 1], dtype=np.uint64)[1:]):
+        with pytest.raises(P.PahqError):
+            P.tree_words(bad)
+    for bad in ([-1.0, 0.5], [-1, None], ["-1"], [True, False], -1):
+        with pytest.raises(ValueError):
+            P.tree_words(bad)
+    assert P.tree_words(np.array([-1, 0], dtype=np.int64)).tolist() == P.tree_words(np.array([-1, 0], dtype=np.int8)).tolist() == [[1], [3]]
+
+
 def test_the_quotient_of_a_page_size_is_exact():
     """j / p as a product and a shift: at the multiples' borders, for every size a shift's range turns on, and at random."""
     import random
