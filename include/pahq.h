@@ -561,8 +561,8 @@ int pahq_kv_append(void* hip_stream, const pahq_kv_cache* cache, const pahq_kv_b
  *     tree        uint64 [tokens][words >= 1]: those whose bit (j - base_b) % 64 of word (j - base_b) / 64 of its row is set (none behind
  *                 words * 64); for a drafted tree, of which the new tokens are the nodes, pahq_tree_bits fills HOST memory
  *                 with [n][(n + 63) / 64] words, a node's own bit and its ancestors', from parents [n]: parents[i] < i, -1 at a root
- * What a query does not see has no influence on it, infinities and NaN included.  One that sees nothing, or only scores of -inf, gets
- * zeros.  Products in the cache's dtype with sums in fp32, softmax in fp32, its weights rounded to the dtype for their product
+ * What a query does not see has no influence on it, infinities and NaN included; an infinite value that it sees counts however small its
+ * weight, and both infinities make NaN.  One that sees nothing, or only scores of -inf, gets zeros.  Products in the cache's dtype with sums in fp32, softmax in fp32, its weights rounded to the dtype for their product
  * with the values, the sum divided by the weights' sum and rounded once.  The same call gives the same bits.
  * q, out as in pahq_kv_append; out may be q itself with the same strides.  tokens * (q_heads / heads) below 2^31 - 2^16; more than that is too
  * big, as are 2^24 tiles of 16 to 128 (token, query head) pairs of one cache head and sequence: fewer where tokens * q_heads / 16 + batch * heads

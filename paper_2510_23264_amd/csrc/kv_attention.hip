@@ -341,6 +341,23 @@ template <typename T, typename F> __device__ __forceinline__ F take_kinds(F* v) 
   }
   return kinds;
 }
+// That is done in masked blocks.  In the others an infinite value times a weight that rounded to zero, or an infinite sum that is rescaled by
+// zero, leaves NaN where infinity belongs, for the weight is positive in the definition: a tile with a NaN is done once more with all its
+// blocks masked, and sums are rescaled so there, and where parts of them meet, that infinities stay.
+template <typename V> __device__ __forceinline__ V rescaled(V x, float by) { return __builtin_elementwise_abs(x) == INFINITY ? x : x * by; }
+template <typename V> __device__ __forceinline__ bool has_nan(const V& x) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(V) / 4); i++) bad |= x[i] != x[i];
+  return bad;
+}
+// Whether one of the waves said so in LDS, as every lane's value
+template <int NW> __device__ __forceinline__ bool any_of(const int* said) {
+  int any = 0;
+#pragma unroll
+  for (int w = 0; w < NW; w++) any |= said[w];
+  return __builtin_amdgcn_readfirstlane(any);
+}
 // 1 where a bit is set, else 0
 template <typename T> __device__ __forceinline__ T one_bit(uint32_t seen, int n) { return (T)__uint_as_float((seen >> n & 1u) * 0x3F800000u); }
 __device__ __forceinline__ float of_kinds(float count) {
@@ -370,6 +387,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   static_assert(2 * STAGE >= ROWS * D * 4 && 2 * ASKS + 1 < 64, "the waves' sums fit their stages");
   extern __shared__ __align__(1024) char lds[];       // [NW][2][STAGE], [NW][4][64] pages' numbers
   __shared__ float stat[NW][ROWS][2];
+  __shared__ int lost[NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, h4 = lane >> 4;
   Finder<KVB * NW, true> f;
   f.look(args_again(), ROWS);
@@ -378,7 +396,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   f.begin(args_again(), ROWS, wg);
   uint32_t at = f.plan.wgs ? kv_from(f.plan, wg) : blockIdx.x;
   const uint32_t stop = f.plan.wgs ? kv_from(f.plan, wg + 1) : at + 1;
-  for (bool first = true; at < stop; first = false) {
+  for (bool first = true, again = false; at < stop; first = false) {
   Item it;
   const uint32_t take = f.next(args_again(), ROWS, wg, at, stop, &it);
   if (!take) return;
@@ -427,6 +445,8 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
       ask_chunk<true>(a.c.values + head, x, to + HALF + j * 1024);
     }
   };
+  // blocks that every query of the tile sees whole come first
+  const int sure = again ? 0 : min(end, it.s.base + (a.tree ? 0 : (int)((long long)it.tile * ROWS / group) + 1));
   v4f o[RT][DT] = {};
   float m[RT], l[RT];
 #pragma unroll
@@ -487,7 +507,9 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
         if (more) m[r] = top;
         l[r] *= f;
 #pragma unroll
-        for (int d = 0; d < DT; d++) o[r][d] *= f;
+        for (int d = 0; d < DT; d++)
+          if (masked && sure == 0) o[r][d] = rescaled(o[r][d], f);
+          else o[r][d] *= f;
       }
       const float from = (m[r] == -INFINITY ? 0.f : m[r]) - LIFT<T>;
 #pragma unroll
@@ -552,13 +574,12 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
       }
     }
   };
-  // blocks that every query of the tile sees whole come first
-  const int sure = min(end, it.s.base + (a.tree ? 0 : (int)((long long)it.tile * ROWS / group) + 1));
   int n = 0;
   for (; n < turns && first_row(n) + KVB <= sure; n++) block(n, std::false_type());
   for (; n < turns; n++) block(n, std::true_type());
 
   // the waves' sums: [row][d] in the wave's stages, chunks of four swizzled by the row
+  bool bad = false;
 #pragma unroll
   for (int r = 0; r < RT; r++) {
     l[r] += __shfl_xor(l[r], 16, 64);
@@ -566,9 +587,18 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     const int row = 16 * r + l16;
     if (h4 == 0) stat[wave][row][0] = m[r], stat[wave][row][1] = l[r];
 #pragma unroll
-    for (int d = 0; d < DT; d++) *(v4f*)(mine + row * (D * 4) + (((4 * d + h4) ^ (row & 15)) * 16)) = o[r][d];
+    for (int d = 0; d < DT; d++) {
+      *(v4f*)(mine + row * (D * 4) + (((4 * d + h4) ^ (row & 15)) * 16)) = o[r][d];
+      bad |= has_nan(o[r][d]);
+    }
   }
+  lost[wave] = __any(bad);
   __syncthreads();
+  again = !again && any_of<NW>(lost);
+  if (again) {
+    at -= take;
+    continue;
+  }
   const AttendArgs k = args_again();
   for (int e = threadIdx.x; e < ROWS * (D / 4); e += NW * 64) {
     const int row = e / (D / 4), c = e % (D / 4);
@@ -582,7 +612,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     for (int w = 0; w < NW; w++) {
       const float f = __builtin_amdgcn_exp2f(stat[w][row][0] - (top == -INFINITY ? 0.f : top));
       sum += f * stat[w][row][1];
-      y += f * *(const v4f*)(lds + w * 2 * STAGE + row * (D * 4) + ((c ^ (row & 15)) * 16));
+      y += rescaled(*(const v4f*)(lds + w * 2 * STAGE + row * (D * 4) + ((c ^ (row & 15)) * 16)), f);
     }
     if (it.slot >= 0) {
       const long long slot = it.slot;
@@ -618,6 +648,7 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
   constexpr int HALF = KVB * D * EB, MINE = KVB / NW, ASKS = HALF / 1024 / NW, DT = D / 32;
   static_assert(ASKS >= 1 && MINE * CH == ASKS * 64 && KVB <= 64, "a wave asks for whole rows");
   extern __shared__ __align__(1024) char lds[];     // [2] keys [HALF] and values [HALF], [NW][2][64] pages' numbers
+  __shared__ int lost[NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h2 = lane >> 5;
   Finder<KVB, false> f;
   f.look(args_again(), ROWS);
@@ -626,7 +657,7 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
   f.begin(args_again(), ROWS, wg);
   uint32_t at = f.plan.wgs ? kv_from(f.plan, wg) : blockIdx.x;
   const uint32_t stop = f.plan.wgs ? kv_from(f.plan, wg + 1) : at + 1;
-  for (bool first = true; at < stop; first = false) {
+  for (bool first = true, again = false; at < stop; first = false) {
     Item it;
     const uint32_t take = f.next(args_again(), ROWS, wg, at, stop, &it);
     if (!take) return;
@@ -653,7 +684,7 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
     }
     // what the wave's rows see at least (unmasked) and at most: blocks behind the latter are left out
     const int last = min(it.s.n - 1, (int)((row0 + 31) / group));
-    const int sure = min(end, it.s.base + (a.tree ? 0 : (int)(row0 / group) + 1));
+    const int sure = again ? 0 : min(end, it.s.base + (a.tree ? 0 : (int)(row0 / group) + 1));
     const int wave_end = row0 >= (long long)it.s.n * group ? 0 : a.tree ? end : min(end, it.s.base + last + 1);
 
     const int* const pages = a.b.pages + it.b * a.b.ld;
@@ -758,7 +789,9 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
         m = to;
         l *= by;
 #pragma unroll
-        for (int d = 0; d < DT; d++) o[d] *= by;
+        for (int d = 0; d < DT; d++)
+          if (masked && sure == 0) o[d] = rescaled(o[d], by);
+          else o[d] *= by;
         weights(LIFT<T> - (m == -INFINITY ? 0.f : m));       // nothing seen so far, or only scores of -inf: zeros
       }
       l += sum;
@@ -807,6 +840,18 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
     int n = 0;
     for (; n < blocks && begin + n * KVB + KVB <= sure; n++) block(n, std::false_type());
     for (; n < blocks; n++) block(n, std::true_type());
+    bool bad = false;
+#pragma unroll
+    for (int d = 0; d < DT; d++) bad |= has_nan(o[d]);
+    if (!again) {                                   // the stages are all waves': all of them again or none
+      lost[wave] = __any(bad);
+      __syncthreads();
+    }
+    again = !again && any_of<NW>(lost);
+    if (again) {
+      at -= take;
+      continue;
+    }
     l += __shfl_xor(l, 32, 64);
     if (there) {
       const AttendArgs k = args_again();
@@ -873,16 +918,17 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
 #pragma unroll
       for (int k = 0; k < FLY; k++) most = fmaxf(most, top[k]);
       const float safe = most == -INFINITY ? 0.f : most, by = __builtin_amdgcn_exp2f(m - safe);
-      y *= by;
+      y = rescaled(y, by);
       l *= by;
       m = most;
 #pragma unroll
       for (int k = 0; k < FLY; k++) {
         const float f = __builtin_amdgcn_exp2f(top[k] - safe);
         const bool there = p + k * share < pieces;  // not again what stands in for a part behind the last
+        const v4f more = rescaled(x[k], f);
         l += there ? sum[k] * f : 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; j++) y[j] += there ? x[k][j] * f : 0.f;
+        for (int j = 0; j < 4; j++) y[j] += there ? more[j] : 0.f;
       }
     }
     if (r0 > first) __syncthreads();
@@ -898,7 +944,7 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
     for (int p = 0; p < share; p++) {
       const float f = __builtin_amdgcn_exp2f(stat[p * few * quads + e][0] - safe);
       sum += f * stat[p * few * quads + e][1];
-      y += f * sums[p * few * quads + e];
+      y += rescaled(sums[p * few * quads + e], f);
     }
     const long long of = (long long)tile * rows + r;
     const int i = (int)(of / a.group), g = (int)(of - (long long)i * a.group);

@@ -72,3 +72,51 @@ def test_weights_are_divided_by_their_own_sum(P, dtype, group, d):
     got = run(P, case, scale=1.0).cpu()
     off = (got != want.to(dtype)[:, None]) & clear[:, None]
     assert not off.any(), (int(off.sum()), int(clear.sum()) * group)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new, lengths", SHAPES)
+@pytest.mark.parametrize("weight", ["small", "gone", "overtaken"])
+def test_infinite_values_count_whatever_their_weight(P, dtype, d, new, lengths, weight):
+    """A value that is infinite in one column of a row that every query sees, or in a new token's row that some see.  Its weight is exp(-25), which 16
+    bits may not hold, or exp(-120), which fp32 does not hold, or it was exp(0) until later rows' scores of 120 took over: positive
+    in the definition.  The column is infinite for those that see the row (NaN for both signs), and nothing else changes by a bit."""
+    def made():
+        case = wide(Case(new, lengths, 2, 1, d, 16, dtype, seed=sum(lengths)))
+        case.q *= 0.0625
+        case.q[:, :, 0] = 1
+        there = ~case.keys[:, :, :, 0].isnan()
+        case.keys[:, :, :, 0][there] = 0.0
+        return case
+
+    def row(case, name, j):
+        return getattr(case, name)[case.table[0][j // 16], 0, j % 16]
+    for at in (5, lengths[0] - max(1, new[0] // 2)):
+        def prepared():
+            case = made()
+            if weight == "overtaken":
+                for j in range(at + 1, lengths[0]):
+                    case.keys[case.table[0][j // 16], :, j % 16, 0] = 120.0
+            else:
+                row(case, "keys", at)[0] = row(case, "keys", at - 1)[0] = -25.0 if weight == "small" else -120.0
+            return case
+        tree = torch.full((made().tokens, -(-max(new) // 64)), -1)
+        tree[: new[0] // 2, (at - lengths[0] + new[0]) // 64 if at >= lengths[0] - new[0] else 0] = 0
+        for mask in (None, tree):
+            clean = run(P, prepared(), mask, scale=1.0).cpu()
+            from plain_kv import seen_of
+            sees = seen_of(made(), 0, mask)[:, at - 1:at + 1]
+            for first, second in ((float("inf"), 0.5), (0.5, -float("inf")), (float("inf"), -float("inf"))):
+                case = prepared()
+                row(case, "values", at - 1)[3], row(case, "values", at)[3] = first, second
+                got = run(P, case, mask, scale=1.0).cpu()
+                want = clean.clone()
+                for i in range(new[0]):
+                    bad = [x for x, s in zip((first, second), sees[i].tolist()) if s and abs(x) > 1]
+                    if bad:
+                        want[i, 0, 3] = sum(bad)
+                    elif sees[i].any():
+                        want[i, 0, 3] = got[i, 0, 3]                     # 0.5 where a number stood, of a weight that counts in the "overtaken" row
+                        assert got[i, 0, 3].isfinite()
+                assert torch.equal(torch.nan_to_num(got, 1e4, 2e4, 3e4), torch.nan_to_num(want, 1e4, 2e4, 3e4)), (at, mask is None, first, second)
