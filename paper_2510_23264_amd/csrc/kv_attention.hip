@@ -31,7 +31,7 @@ struct AttendArgs {
   KvRows q, out;
   const unsigned long long* tree;
   int words, group;                                 // group: query heads of a cache head
-  float scale, sign;                                // of the scores: times log2 e and positive; of the queries: its sign, 0 for a scale of 0
+  float scale, sign;                                // of the scores: times log2 e and positive; of the queries: its sign, 0 for a scale of 0, which multiplies them
   float* part;                                      // [slot][rows][d] sums of a part, [slot][rows][2] maximum and sum, then how many of Left there are, and they
   int slots, least, over, enough, brief;            // of ranges (kv_plan.h); slots 0: nothing is cut
   int by_pair;                                      // Left are counted by tile and head, or by range: whichever are fewer
@@ -273,6 +273,12 @@ __device__ __forceinline__ float sum_of(v4f x, float acc) { return acc + ((x[0] 
 
 alignas(16) __device__ const uint32_t kv_chunk[4][4] = {{0, 0, 0, 0}, {0x7FC00000, 0x7FC00000, 0x7FC00000, 0x7FC00000},
                                                         {0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0}, {0x7E007E00, 0x7E007E00, 0x7E007E00, 0x7E007E00}};
+// A scale of 0: queries of zeros, and NaN where they were not finite
+template <typename T, typename F> __device__ __forceinline__ F times_zero(F q) {
+#pragma unroll
+  for (int j = 0; j < 16 / (int)sizeof(T); j++) q[j] = (T)((float)q[j] * 0.f);
+  return q;
+}
 template <typename T> constexpr uint32_t SIGNS = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
 template <typename T> constexpr int NAN_CHUNK = sizeof(T) == 4 ? 1 : __is_same(T, bf16_t) ? 2 : 3;
 
@@ -410,7 +416,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   F q[RT][CH / 4];
   {
     const AttendArgs k = args_again();
-    const uint32_t keep = k.sign == 0.f ? 0u : ~0u, flip = k.sign < 0.f ? SIGNS<T> : 0u;
+    const uint32_t flip = k.sign < 0.f ? SIGNS<T> : 0u;
 #pragma unroll
     for (int r = 0; r < RT; r++) {
       const long long row = (long long)it.tile * ROWS + 16 * r + l16;
@@ -421,7 +427,8 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
 #pragma unroll
       for (int s = 0; s < CH / 4; s++) {
         const int e0 = (h4 + 4 * s) * (16 / EB);
-        q[r][s] = __builtin_bit_cast(F, (load16(x + (e0 < k.c.d ? e0 : 0)) & (there && e0 < k.c.d ? keep : 0u)) ^ flip);
+        q[r][s] = __builtin_bit_cast(F, (load16(x + (e0 < k.c.d ? e0 : 0)) & (there && e0 < k.c.d ? ~0u : 0u)) ^ flip);
+        if (k.sign == 0.f) q[r][s] = times_zero<T>(q[r][s]);
       }
     }
   }
@@ -673,13 +680,14 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
     F q[CH / 2];
     {
       const AttendArgs k = args_again();
-      const uint32_t keep = k.sign == 0.f ? 0u : ~0u, flip = k.sign < 0.f ? SIGNS<T> : 0u;
+      const uint32_t flip = k.sign < 0.f ? SIGNS<T> : 0u;
       const int g = there ? (int)(row - (long long)token * group) : 0;
       const T* const x = (const T*)(k.q.at + (it.s.t0 + (there ? token : 0)) * k.q.token + (h * group + g) * k.q.head);
 #pragma unroll
       for (int c = 0; c < CH / 2; c++) {
         const int e0 = (h2 + 2 * c) * N;
-        q[c] = __builtin_bit_cast(F, (load16(x + (e0 < k.c.d ? e0 : 0)) & (there && e0 < k.c.d ? keep : 0u)) ^ flip);
+        q[c] = __builtin_bit_cast(F, (load16(x + (e0 < k.c.d ? e0 : 0)) & (there && e0 < k.c.d ? ~0u : 0u)) ^ flip);
+        if (k.sign == 0.f) q[c] = times_zero<T>(q[c]);
       }
     }
     // what the wave's rows see at least (unmasked) and at most: blocks behind the latter are left out

@@ -3,7 +3,7 @@ their range.  Each on tiles of 16, 32 and 128 rows, whole and cut."""
 import pytest
 import torch
 
-from plain_kv import Case
+from plain_kv import Case, attend, check, seen_of
 
 pytestmark = pytest.mark.gpu
 DTYPES = [torch.float32, torch.bfloat16, torch.float16]
@@ -105,7 +105,6 @@ def test_infinite_values_count_whatever_their_weight(P, dtype, d, new, lengths, 
         tree[: new[0] // 2, (at - lengths[0] + new[0]) // 64 if at >= lengths[0] - new[0] else 0] = 0
         for mask in (None, tree):
             clean = run(P, prepared(), mask, scale=1.0).cpu()
-            from plain_kv import seen_of
             sees = seen_of(made(), 0, mask)[:, at - 1:at + 1]
             for first, second in ((float("inf"), 0.5), (0.5, -float("inf")), (float("inf"), -float("inf"))):
                 case = prepared()
@@ -120,3 +119,18 @@ def test_infinite_values_count_whatever_their_weight(P, dtype, d, new, lengths, 
                         want[i, 0, 3] = got[i, 0, 3]                     # 0.5 where a number stood, of a weight that counts in the "overtaken" row
                         assert got[i, 0, 3].isfinite()
                 assert torch.equal(torch.nan_to_num(got, 1e4, 2e4, 3e4), torch.nan_to_num(want, 1e4, 2e4, 3e4)), (at, mask is None, first, second)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("new, lengths", SHAPES)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_a_scale_of_zero_hides_no_query(P, dtype, new, lengths, bad):
+    """Scores are 0 times the product: NaN where a query is not finite, its own rows only; 0 for the others, which get the values' mean."""
+    case = wide(Case(new, lengths, 2, 1, 64, 16, dtype, seed=7))
+    clean = run(P, case, scale=0.0).cpu()
+    check(clean, *attend(case, scale=0.0))
+    case.q[case.tokens // 2, 1, 17] = bad
+    got = run(P, case, scale=0.0).cpu()
+    assert got[case.tokens // 2, 1].isnan().all()
+    got[case.tokens // 2, 1] = clean[case.tokens // 2, 1]
+    assert torch.equal(got, clean)
