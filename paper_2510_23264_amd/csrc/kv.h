@@ -6,18 +6,10 @@
 #include <stdint.h>
 #include "../../include/pahq.h"
 #include "device_tensor.h"
+#include "kv_address.h"
 
 namespace pahq {
 
-constexpr int KV_MAX_LENGTH = 0x7FFF0000;           // rows of a sequence: a tile behind the last one is still counted in 31 bits
-
-struct KvCache {
-  char *keys, *values;
-  long long page, head, slot;                       // strides in bytes
-  int pages, page_size, heads, d;
-  uint32_t magic;                                   // j / page_size = j * magic >> shift for j < 2^31
-  int shift;
-};
 struct KvBatch {
   const int *starts, *lengths, *pages;
   long long ld;
@@ -29,15 +21,6 @@ struct KvRows {
 };
 
 // ---------------------------------------------------------------- host
-// ceil(2^(31 + s) / p), 2^s the power of two at or above p: fits 32 bits, and j * (its excess over the exact quotient) stays
-// below 2^(31 + s) for every j < 2^31, so the shifted product is the quotient.
-inline void kv_divider(uint32_t p, uint32_t* magic, int* shift) {
-  int s = 0;
-  while ((1ull << s) < p) s++;
-  *magic = (uint32_t)(((1ull << (31 + s)) + p - 1) / p);
-  *shift = 31 + s;
-}
-
 // A range of memory, and whether rows of `row` bytes at the strides have a place each (sorted by stride, each behind the extent of the
 // ones before); false where no memory is as large.
 struct KvRange { const void* at; size_t bytes; };
@@ -125,16 +108,9 @@ inline bool kv_rows_apart(const KvRows& out, const KvRange& om, int out_heads, c
 }
 
 // ---------------------------------------------------------------- device
-// A sequence: its new tokens are rows t0 .. t0 + n - 1 of the operator's, its rows base .. base + n - 1 (base may be negative).
-struct KvSequence { int t0, n, length, base; };
-__device__ __forceinline__ int kv_start(const KvBatch& q, int b) { return min(max(q.starts[b], 0), q.tokens); }
+__device__ __forceinline__ int kv_start(const KvBatch& q, int b) { return kv_clipped_start(q.starts[b], q.tokens); }
 __device__ __forceinline__ KvSequence kv_sequence(const KvBatch& q, int b) {
-  KvSequence s;
-  s.t0 = kv_start(q, b);
-  s.n = max(kv_start(q, b + 1) - s.t0, 0);
-  s.length = min(max(q.lengths[b], 0), q.most);
-  s.base = s.length - s.n;
-  return s;
+  return kv_clipped(q.starts[b], q.starts[b + 1], q.lengths[b], q.tokens, q.most);
 }
 // The sequence that token t belongs to: the last b in [0, batch] with start(b) <= t, -1 for none (and `batch` for tokens behind the last).
 // Of starts that do not grow any one comes out; the caller checks that t lies in its sequence.
@@ -147,10 +123,7 @@ template <typename F> __device__ __forceinline__ int kv_owner(int batch, int t, 
   }
   return lo;
 }
-// Bytes from the cache's start to row j < q.most of sequence b in head 0, -1 where its page is none of the cache's
-__device__ __forceinline__ long long kv_row(const KvCache& c, const int* pages, int j) {
-  const int in_list = (int)((unsigned long long)(uint32_t)j * c.magic >> c.shift), slot = j - in_list * c.page_size, page = pages[in_list];
-  return (uint32_t)page < (uint32_t)c.pages ? page * c.page + slot * c.slot : -1;
-}
+// Bytes from the cache's start to row j < q.most of sequence b in head 0, KV_ROW_NONE where its page is none of the cache's
+__device__ __forceinline__ long long kv_row(const KvCache& c, const int* pages, int j) { return kv_row_in(c, j, pages[kv_in_list(c, j)]); }
 
 }  // namespace pahq

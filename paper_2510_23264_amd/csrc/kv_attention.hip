@@ -21,7 +21,6 @@
 #include "device_util.h"
 #include "mma_util.h"
 #include "kv.h"
-#include "kv_plan.h"
 
 namespace pahq {
 
@@ -78,37 +77,30 @@ __device__ __forceinline__ uint32_t wave_sum_up_to(uint32_t v) {
 #undef STEP
   return v;
 }
+__device__ __forceinline__ KvCall call_of(const AttendArgs& a) { return {!a.tree, a.c.heads, a.group, a.slots, a.over}; }
 // Sequences in lanes, 64 at a time from b0 on, and the sums of their tiles (with heads) and units up to and with each
-struct Share { KvSequence s; int tiles, each; uint32_t pairs, units, pairs_to, units_to; };        // each: units of a tile, or of a couple of them
-__device__ __forceinline__ bool in_couples(const AttendArgs& a, int tiles) { return !a.tree && tiles > 1; }
+struct Share { KvSequence s; int tiles, each; uint32_t pairs, units, pairs_to, units_to; };
 template <int UNIT> __device__ __forceinline__ Share share_of(const AttendArgs& a, int rows, int b0, uint32_t pairs_before, uint32_t units_before) {
   const int b = b0 + (threadIdx.x & 63);
   Share x = {};
   if (b < a.b.batch) {
     x.s = kv_sequence(a.b, b);
-    x.tiles = kv_tiles((long long)x.s.n * a.group, rows);
-    x.pairs = kv_pairs(x.tiles, a.c.heads);
-    if (a.slots) {
-      const bool couples = in_couples(a, x.tiles);
-      x.each = couples ? kv_couple_units(x.s.base, x.tiles, rows, a.group, UNIT, a.over) : kv_units_of(x.s.length, UNIT, a.over);
-      x.units = kv_units(couples ? kv_pairs((x.tiles + 1) / 2, a.c.heads) : x.pairs, x.each);
-    }
+    const KvShare y = kv_share(call_of(a), x.s, rows, UNIT);
+    x.tiles = y.tiles;
+    x.each = y.each;
+    x.pairs = y.pairs;
+    x.units = y.units;
   }
   x.pairs_to = __builtin_elementwise_add_sat(wave_sum_up_to(x.pairs), pairs_before);
   x.units_to = __builtin_elementwise_add_sat(wave_sum_up_to(x.units), units_before);
   return x;
 }
-// What the join needs of a tile that lies in several ranges, of which `w0` is the first; pieces 0: of one that does not
-struct Left { int t0, rows, tile, h, pieces, w0, unused[2]; };
-__device__ __forceinline__ int* count_of(const AttendArgs& a, int rows) { return (int*)(a.part + 2ll * a.slots * rows * (a.c.d + 2)); }
-__device__ __forceinline__ Left* left_of(const AttendArgs& a, int rows) { return (Left*)(count_of(a, rows) + 8); }
+__device__ __forceinline__ int* count_of(const AttendArgs& a, int rows) { return (int*)(a.part + kv_count_at(a.slots, rows, a.c.d)); }
+__device__ __forceinline__ KvLeft* left_of(const AttendArgs& a, int rows) { return (KvLeft*)(a.part + kv_left_at(a.slots, rows, a.c.d)); }
 struct Item {
   KvSequence s;
   int b, tile, h, begin, end, slot;                 // rows of the cache; slot in the workspace, -1: the whole tile
 };
-__device__ __forceinline__ int tile_end(const AttendArgs& a, const KvSequence& s, int tile, int rows) {
-  return a.tree ? s.length : kv_tile_end(s.n, s.base, tile, rows, a.group);
-}
 // Where a workgroup finds its part; every wave looks by itself.  Of up to 64 sequences KEEP keeps what was read.
 template <int UNIT, bool KEEP> struct Finder {
   Share x;
@@ -144,9 +136,10 @@ template <int UNIT, bool KEEP> struct Finder {
   __device__ __forceinline__ KvSequence sequence(int l) const { return {lane_of(x.s.t0, l), lane_of(x.s.n, l), lane_of(x.s.length, l), lane_of(x.s.base, l)}; }
   // What workgroup `wg` does at `at`, up to `stop` at most.  Returns how many units that takes, 0 if there is nothing.
   __device__ __forceinline__ uint32_t next(const AttendArgs& a, int rows, int wg, uint32_t at, uint32_t stop, Item* it) {
-    const uint32_t begun = at, over = (uint32_t)a.over;
-    int b0, l;
-    uint32_t tiles, off, take, whole;
+    const uint32_t begun = at;
+    const KvCall c = call_of(a);
+    int b0, l, tiles;
+    KvStretch x;
     for (;;) {
       l = lane_with(a, rows, at, plan.wgs, &b0);
       if (l < 0) return 0;
@@ -154,43 +147,31 @@ template <int UNIT, bool KEEP> struct Finder {
       it->s = sequence(l);
       it->begin = 0;
       it->slot = -1;
-      tiles = lane_of(x.tiles, l);
-      if (!plan.wgs) {                              // heads in turn, and the last tiles, which see the most rows, first
-        const uint32_t local = at - (lane_of(x.pairs_to, l) - lane_of(x.pairs, l)), heads = a.c.heads;
-        it->h = local % heads;
-        it->tile = tiles - 1 - local / heads;
-        it->end = tile_end(a, it->s, it->tile, rows);
+      tiles = lane_of(this->x.tiles, l);
+      if (!plan.wgs) {
+        const KvTile t = kv_whole_tile(c, tiles, at - (lane_of(this->x.pairs_to, l) - lane_of(this->x.pairs, l)));
+        it->h = t.h;
+        it->tile = t.tile;
+        it->end = kv_end_of(c, it->s, it->tile, rows);
         return 1;
       }
-      const bool couples = in_couples(a, tiles);
-      const uint32_t local = at - (lane_of(x.units_to, l) - lane_of(x.units, l)), each = lane_of(x.each, l), lines = couples ? (tiles + 1) / 2 : tiles;
-      const uint32_t line = local / each, in = local - line * each;
-      it->h = line / lines;
-      const int i = line - it->h * lines;
-      it->tile = couples ? (int)tiles - 1 - i : i;
-      off = in;
-      whole = kv_units_of(tile_end(a, it->s, it->tile, rows), UNIT, a.over);
-      if (off >= whole && i != it->tile) {          // behind the late tile the early one
-        off -= whole;
-        it->tile = i;
-        whole = kv_units_of(tile_end(a, it->s, i, rows), UNIT, a.over);
-      }
-      const bool work = off < whole;
-      take = min(work ? whole - off : each - in, stop - at);
-      at += take;
-      if (work && off + take > over) break;
+      x = kv_stretch(c, it->s, tiles, lane_of(this->x.each, l), rows, UNIT, at - (lane_of(this->x.units_to, l) - lane_of(this->x.units, l)), stop - at);
+      it->h = x.h;
+      it->tile = x.tile;
+      at += x.take;
+      if (x.work && x.off + x.take > (uint32_t)c.over) break;
       if (at >= stop) return 0;
     }
-    it->end = tile_end(a, it->s, it->tile, rows);
-    const bool starts = off <= over, ends = off + take == whole;
-    if (!starts) it->begin = (int)min((uint32_t)min((uint64_t)(off - over) * UNIT, (uint64_t)KV_MAX_LENGTH), (uint32_t)it->end);
-    if (!ends) it->end = min(it->end, (int)((off + take - over) * UNIT));
-    if (!starts || !ends) it->slot = 2 * wg + starts;
+    it->end = kv_end_of(c, it->s, it->tile, rows);
+    const bool starts = kv_begins(c, x), ends = kv_ends(x);
+    if (!starts) it->begin = kv_begin_of(c, x, UNIT, it->end);
+    if (!ends) it->end = kv_stop_of(c, x, UNIT, it->end);
+    if (!starts || !ends) it->slot = kv_slot(wg, starts);
     if (starts && (!ends || a.by_pair) && threadIdx.x == 0) {
-      const uint32_t number = lane_of(x.pairs_to, l) - lane_of(x.pairs, l) + it->h * tiles + it->tile;
+      const uint32_t number = kv_number(lane_of(this->x.pairs_to, l) - lane_of(this->x.pairs, l), it->h, tiles, it->tile);
       if (!a.by_pair || number < (uint32_t)a.slots)
         left_of(a, rows)[a.by_pair ? number : wg] = {it->s.t0, (int)min((long long)it->s.n * a.group - (long long)it->tile * rows, (long long)rows), it->tile, it->h,
-                                                     ends ? 0 : kv_holder(plan, at - take - off + whole - 1) - wg + 1, wg, {}};
+                                                     ends ? 0 : kv_holder(plan, at - x.take - x.off + x.whole - 1) - wg + 1, wg, {}};
     }
     return at - begun;
   }
@@ -201,17 +182,8 @@ template <int UNIT, bool KEEP> struct Finder {
     if (plan.wgs ? wg == 0 : blockIdx.x == 0) *count_of(a, rows) = plan.wgs ? (int)(a.by_pair ? min(pairs, (uint32_t)a.slots) : plan.wgs) : 0;
   }
 };
-// Bit x: whether new token i sees row k0 + x of the cache; none for i < 0.  Without branches: lanes part here otherwise, and registers that
-// hold what is every lane's are not safe in the compiler's hands where lanes are off.
 __device__ __forceinline__ unsigned long long seen_bits(const AttendArgs& a, const KvSequence& s, int i, int k0, int end) {
-  auto low = [](int n) { return n >= 64 ? ~0ull : (1ull << max(n, 0)) - 1; };
-  const unsigned long long here = low(end - k0) & (i < 0 ? 0ull : ~0ull);
-  if (!a.tree) return low(s.base + i + 1 - k0) & here;
-  const int ahead = k0 - s.base, word = ahead >> 6, shift = ahead & 63;            // rounded down
-  const unsigned long long* const w = a.tree + (long long)(s.t0 + max(i, 0)) * a.words;
-  const unsigned long long first = w[min(max(word, 0), a.words - 1)], second = w[min(max(word + 1, 0), a.words - 1)];
-  const unsigned long long of_first = word >= 0 && word < a.words ? ~0ull : 0ull, of_second = shift && word + 1 >= 0 && word + 1 < a.words ? ~0ull : 0ull;
-  return (low(s.base - k0) | (first >> shift & of_first) | (second << (64 - shift & 63) & of_second)) & here;
+  return kv_seen(a.tree, a.words, s, i, k0, end);
 }
 // x where bit n of seen is set, else -infinity
 __device__ __forceinline__ float seen_score(uint32_t seen, int n, float x) {
@@ -282,14 +254,7 @@ template <typename T, typename F> __device__ __forceinline__ F times_zero(F q) {
 template <typename T> constexpr uint32_t SIGNS = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
 template <typename T> constexpr int NAN_CHUNK = sizeof(T) == 4 ? 1 : __is_same(T, bf16_t) ? 2 : 3;
 
-// Where chunk c of a row lies among the row's CH chunks.  Rows 4 apart in the low bits, so that four rows' 64 neighbouring bytes (what a
-// transposing read takes) lie in different quarters of the 64 banks, and so do one chunk of sixteen rows (what K's reads take).
-template <int CH> __device__ __forceinline__ int swizzle(int row) {
-  static_assert(CH >= 8, "rows of 128 bytes and more");
-  return CH >= 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
-}
-// What lies at an address of LDS.  The reads of a block differ from one base in the chunk, which XOR changes in place (rows begin at multiples of
-// their size), and in rows a constant apart: `base` is hidden from the compiler so that it derives each address where it is used instead of
+// What lies at an address of LDS.  The reads of a block differ from one base by constants (kv_address.h): `base` is hidden from the compiler so that it derives each address where it is used instead of
 // keeping sixteen of them.
 template <typename F> __device__ __forceinline__ F at_lds(uint32_t a) { return *(const __attribute__((address_space(3))) F*)(uintptr_t)a; }
 __device__ __forceinline__ v4s at_lds_turned(uint32_t a) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)a); }
@@ -300,24 +265,15 @@ __device__ __forceinline__ uint32_t hidden(uint32_t base) {
 
 // Rows of the cache on their way into LDS.  A lane keeps where its row of a block lies; the pages' numbers came through LDS themselves
 // (`ids`, asked for two blocks ahead), because a load into a register would make the compiler wait for everything in flight.
-constexpr long long ROW_BEHIND = -2, ROW_NONE = -1;
-__device__ __forceinline__ void ask_page(const KvCache& c, const int* pages, int row, int end, uint32_t lds) {
-  const int j = max(min(row, end - 1), 0);
-  lds_load4(pages + (int)((unsigned long long)(uint32_t)j * c.magic >> c.shift), lds);
-}
-__device__ __forceinline__ long long row_at(const KvCache& c, int row, int end, int page) {
-  if (row >= end) return ROW_BEHIND;
-  const int slot = row - (int)((unsigned long long)(uint32_t)row * c.magic >> c.shift) * c.page_size;
-  return (uint32_t)page < (uint32_t)c.pages ? page * c.page + slot * c.slot : ROW_NONE;
-}
+__device__ __forceinline__ void ask_page(const KvCache& c, const int* pages, int row, int end, uint32_t lds) { lds_load4(pages + kv_asked(c, row, end), lds); }
 // Rows r0 .. of a block, 64 / CH of them (r0 a multiple of that), chunk by chunk: lane l writes the l-th 16 bytes behind lds.  Their
 // offsets lie in lanes `first` and on.  A lane's chunk: bytes behind the head's first row, or what stands for a chunk that is none.
 struct Chunk { long long off; const char* fill; };
 template <typename T, int CH> __device__ __forceinline__ Chunk chunk_of(const KvCache& c, int lane, long long mine, int first, int r0) {
-  const int chunk = (lane % CH ^ swizzle<CH>(lane / CH)) ^ swizzle<CH>(r0);
-  const long long at = (long long)__shfl((unsigned long long)mine, first + lane / CH, 64);
+  const int chunk = kv_asks_chunk<CH>(lane, r0);
+  const long long at = (long long)__shfl((unsigned long long)mine, first + kv_asks_row<CH>(lane), 64);
   const bool behind = chunk * 16 >= c.d * (int)sizeof(T);
-  return {at + chunk * 16, at < 0 || behind ? (const char*)kv_chunk[at == ROW_NONE && !behind ? NAN_CHUNK<T> : 0] : nullptr};
+  return {at + chunk * 16, at < 0 || behind ? (const char*)kv_chunk[at == KV_ROW_NONE && !behind ? NAN_CHUNK<T> : 0] : nullptr};
 }
 template <bool ONCE> __device__ __forceinline__ void ask_chunk(const char* from, const Chunk& x, uint32_t lds) {
   const uint8_t* const at = (const uint8_t*)(x.fill ? x.fill : from + x.off);
@@ -388,14 +344,13 @@ __device__ __forceinline__ float of_kinds(float count) {
 template <typename T, int D, int RT, int NW>
 __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
   typedef typename Frag<T>::type F;
-  constexpr int EB = sizeof(T), CH = D * EB / 16, KT = EB == 2 ? 2 : 1, KVB = 16 * KT, ROWS = 16 * RT;
-  constexpr int HALF = KVB * D * EB, STAGE = 2 * HALF, ASKS = HALF / 1024, DT = D / 16;
-  static_assert(2 * STAGE >= ROWS * D * 4 && 2 * ASKS + 1 < 64, "the waves' sums fit their stages");
-  extern __shared__ __align__(1024) char lds[];       // [NW][2][STAGE], [NW][4][64] pages' numbers
+  typedef KvFew<sizeof(T), D, RT, NW> L;
+  constexpr int EB = sizeof(T), CH = L::CH, KT = L::KT, KVB = L::KVB, ROWS = L::ROWS, HALF = L::HALF, ASKS = L::ASKS, DT = L::DT;
+  extern __shared__ __align__(1024) char lds[];
   __shared__ float stat[NW][ROWS][2];
   __shared__ int lost[NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, h4 = lane >> 4;
-  Finder<KVB * NW, true> f;
+  Finder<L::UNIT, true> f;
   f.look(args_again(), ROWS);
   const int wg = f.plan.wgs ? kv_wg_of(blockIdx.x, f.plan.wgs) : 0;
   if (wg < 0) return;
@@ -421,9 +376,8 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     for (int r = 0; r < RT; r++) {
       const long long row = (long long)it.tile * ROWS + 16 * r + l16;
       const bool there = row < (long long)it.s.n * group;
-      token[r] = there ? (int)(row / group) : -1;
-      const int t = there ? token[r] : 0, g = there ? (int)(row - (long long)t * group) : 0;
-      const T* const x = (const T*)(k.q.at + (it.s.t0 + t) * k.q.token + (h * group + g) * k.q.head);
+      token[r] = there ? kv_token(row, group) : -1;
+      const T* const x = (const T*)(k.q.at + kv_query_at(it.s.t0, there ? kv_query(row, token[r], group) : KvQuery{0, 0}, h, group, k.q.token, k.q.head));
 #pragma unroll
       for (int s = 0; s < CH / 4; s++) {
         const int e0 = (h4 + 4 * s) * (16 / EB);
@@ -435,16 +389,15 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
 
   const int* const pages = a.b.pages + it.b * a.b.ld;
   const long long head = h * a.c.head;
-  char* const mine = lds + wave * 2 * STAGE;
-  const uint32_t stage0 = __builtin_amdgcn_readfirstlane(lds_addr_of(mine));
-  int* const ids = (int*)(lds + NW * 2 * STAGE) + wave * 4 * 64;
+  const uint32_t stage0 = __builtin_amdgcn_readfirstlane(lds_addr_of(lds + L::stages(wave)));
+  const int* const ids = (const int*)(lds + L::ids(wave));
   const uint32_t ids0 = __builtin_amdgcn_readfirstlane(lds_addr_of(ids));
   const int blocks = end > begin ? (end - begin + KVB - 1) / KVB : 0, turns = blocks > wave ? (blocks - wave + NW - 1) / NW : 0;
   auto first_row = [&](int n) { return begin + (wave + n * NW) * KVB; };
-  auto ask_ids = [&](int n) INLINE { ask_page(a.c, pages, first_row(n) + (lane & (KVB - 1)), end, ids0 + (n & 3) * 256); };
+  auto ask_ids = [&](int n) INLINE { ask_page(a.c, pages, first_row(n) + (lane & (KVB - 1)), end, ids0 + L::ids_of(n)); };
   auto ask_block = [&](int n) INLINE {
-    const long long at = row_at(a.c, first_row(n) + (lane & (KVB - 1)), end, ids[(n & 3) * 64 + lane]);
-    const uint32_t to = stage0 + (n & 1) * STAGE;
+    const long long at = kv_row_or_behind(a.c, first_row(n) + (lane & (KVB - 1)), end, ids[L::ids_of(n) / 4 + lane]);
+    const uint32_t to = stage0 + L::stage(n);
 #pragma unroll
     for (int j = 0; j < ASKS; j++) {
       const Chunk x = chunk_of<T, CH>(a.c, lane, at, j * (64 / CH), j * (64 / CH));
@@ -477,8 +430,8 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     } else {
       wait_vm_lds<0>();
     }
-    const uint32_t stage = stage0 + (n & 1) * STAGE;
-    const uint32_t ks = hidden(stage + l16 * (D * EB) + ((h4 ^ swizzle<CH>(l16)) * 16));
+    const uint32_t stage = stage0 + L::stage(n);
+    const uint32_t ks = hidden(stage + L::key0(l16, h4));
     v4f s[RT][KT];
 #pragma unroll
     for (int t = 0; t < KT; t++) {
@@ -486,7 +439,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
       for (int r = 0; r < RT; r++) s[r][t] = (v4f){0, 0, 0, 0};
 #pragma unroll
       for (int c = 0; c < CH / 4; c++) {
-        const F k = at_lds<F>((ks ^ (4 * c * 16)) + 16 * t * (D * EB));
+        const F k = at_lds<F>(L::key(ks, t, c));
 #pragma unroll
         for (int r = 0; r < RT; r++) s[r][t] = Frag<T>::mma16(k, q[r][c], s[r][t]);
       }
@@ -527,9 +480,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
           if (EB == 4) l[r] += p[r][t][i];
         }
     }
-    const int vrow = 4 * h4 + (EB == 2 ? l16 / 4 : 0);
-    const uint32_t vs = EB == 2 ? hidden(stage + HALF + vrow * (D * EB) + (((l16 & 3) / 2 ^ swizzle<CH>(vrow)) * 16) + (l16 & 1) * 8)
-                                : hidden(stage + HALF + vrow * (D * EB) + ((l16 / 4 ^ swizzle<CH>(vrow)) * 16) + (l16 & 3) * 4);
+    const uint32_t vs = hidden(stage + L::value0(l16, h4));
     if constexpr (EB == 2) {
       F w[RT];
 #pragma unroll
@@ -542,7 +493,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
       for (int d = 0; d < DT; d++) {
         union { F f; v4s half[2]; } v;
 #pragma unroll
-        for (int t = 0; t < 2; t++) v.half[t] = at_lds_turned((vs ^ (2 * d * 16)) + 16 * t * (D * EB));
+        for (int t = 0; t < 2; t++) v.half[t] = at_lds_turned(L::value_16_bit(vs, t, d));
         if (masked && __any(not_finite<T>(v.f))) {
           const F kinds = take_kinds<T>(&v.f);
 #pragma unroll
@@ -563,7 +514,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
       for (int d = 0; d < DT; d++) {
         F v;
 #pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = at_lds<float>((vs ^ ((4 * d ^ swizzle<CH>(i)) * 16)) + i * (D * EB));
+        for (int i = 0; i < 4; i++) v[i] = at_lds<float>(L::value_fp32(vs, i, d));
         if (masked && __any(not_finite<T>(v))) {
           const F kinds = take_kinds<T>(&v);
 #pragma unroll
@@ -595,7 +546,7 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     if (h4 == 0) stat[wave][row][0] = m[r], stat[wave][row][1] = l[r];
 #pragma unroll
     for (int d = 0; d < DT; d++) {
-      *(v4f*)(mine + row * (D * 4) + (((4 * d + h4) ^ (row & 15)) * 16)) = o[r][d];
+      *(v4f*)(lds + L::sum(wave, row, 4 * d + h4)) = o[r][d];
       bad |= has_nan(o[r][d]);
     }
   }
@@ -619,19 +570,17 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
     for (int w = 0; w < NW; w++) {
       const float f = __builtin_amdgcn_exp2f(stat[w][row][0] - (top == -INFINITY ? 0.f : top));
       sum += f * stat[w][row][1];
-      y += rescaled(*(const v4f*)(lds + w * 2 * STAGE + row * (D * 4) + ((c ^ (row & 15)) * 16)), f);
+      y += rescaled(*(const v4f*)(lds + L::sum(w, row, c)), f);
     }
     if (it.slot >= 0) {
-      const long long slot = it.slot;
-      *(v4f*)(k.part + (slot * ROWS + row) * k.c.d + c * 4) = y;
-      float* const st = k.part + 2ll * k.slots * ROWS * k.c.d + (slot * ROWS + row) * 2;
+      *(v4f*)(k.part + kv_part_at(it.slot, ROWS, row, k.c.d) + c * 4) = y;
+      float* const st = k.part + kv_stat_at(k.slots, it.slot, ROWS, row, k.c.d);
       if (c == 0) st[0] = top, st[1] = sum;
     } else {
-      const int i = (int)(of / group), g = (int)(of - (long long)i * group);
       Pack<T, 4> z;
 #pragma unroll
       for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(sum == 0.f ? 0.f : y[j] / sum);
-      *(Pack<T, 4>*)((T*)(const_cast<char*>(k.out.at) + (it.s.t0 + i) * k.out.token + (h * group + g) * k.out.head) + c * 4) = z;
+      *(Pack<T, 4>*)((T*)(const_cast<char*>(k.out.at) + kv_query_at(it.s.t0, kv_query(of, kv_token(of, group), group), h, group, k.out.token, k.out.head)) + c * 4) = z;
     }
   }
   }
@@ -651,11 +600,11 @@ template <typename T, int D> constexpr int TILE_WAVES = D * sizeof(T) <= 128 ? 3
 template <typename T, int D, int KVB>
 __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs a) {
   typedef typename Frag<T>::type F;
-  constexpr int EB = sizeof(T), CH = D * EB / 16, KT = KVB / 32, NW = 4, ROWS = 32 * NW, N = 16 / EB;
-  constexpr int HALF = KVB * D * EB, MINE = KVB / NW, ASKS = HALF / 1024 / NW, DT = D / 32;
-  static_assert(ASKS >= 1 && MINE * CH == ASKS * 64 && KVB <= 64, "a wave asks for whole rows");
-  extern __shared__ __align__(1024) char lds[];     // [2] keys [HALF] and values [HALF], [NW][2][64] pages' numbers
-  __shared__ int lost[NW];
+  typedef KvWide<sizeof(T), D> L;
+  constexpr int EB = sizeof(T), CH = L::CH, KT = L::KT, NW = L::NW, ROWS = L::ROWS, N = L::N, HALF = L::HALF, MINE = L::MINE, ASKS = L::ASKS, DT = L::DT;
+  static_assert(KVB == L::KVB, "what the addresses are for");
+  extern __shared__ __align__(1024) char lds[];
+  __shared__ int lost[2][NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h2 = lane >> 5;
   Finder<KVB, false> f;
   f.look(args_again(), ROWS);
@@ -664,25 +613,24 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
   f.begin(args_again(), ROWS, wg);
   uint32_t at = f.plan.wgs ? kv_from(f.plan, wg) : blockIdx.x;
   const uint32_t stop = f.plan.wgs ? kv_from(f.plan, wg + 1) : at + 1;
-  for (bool first = true, again = false; at < stop; first = false) {
+  int pass = 0;
+  for (bool again = false; at < stop; pass ^= 1) {
     Item it;
     const uint32_t take = f.next(args_again(), ROWS, wg, at, stop, &it);
     if (!take) return;
     at += take;
     const int begin = it.begin, end = it.end, h = it.h;
-    if (!first) __syncthreads();                    // the stages held the last tile's rows
 
     const int group = a.group;
     // the wave's queries: lane l32 holds chunks h2, h2 + 2, ... of its row; zeros where there is none, from memory that is there
     const long long row0 = (long long)it.tile * ROWS + wave * 32, row = row0 + l32;
     const bool there = row < (long long)it.s.n * group;
-    const int token = there ? (int)(row / group) : -1;
+    const int token = there ? kv_token(row, group) : -1;
     F q[CH / 2];
     {
       const AttendArgs k = args_again();
       const uint32_t flip = k.sign < 0.f ? SIGNS<T> : 0u;
-      const int g = there ? (int)(row - (long long)token * group) : 0;
-      const T* const x = (const T*)(k.q.at + (it.s.t0 + (there ? token : 0)) * k.q.token + (h * group + g) * k.q.head);
+      const T* const x = (const T*)(k.q.at + kv_query_at(it.s.t0, there ? kv_query(row, token, group) : KvQuery{0, 0}, h, group, k.q.token, k.q.head));
 #pragma unroll
       for (int c = 0; c < CH / 2; c++) {
         const int e0 = (h2 + 2 * c) * N;
@@ -698,24 +646,22 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
     const int* const pages = a.b.pages + it.b * a.b.ld;
     const long long head = h * a.c.head;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(lds));
-    int* const ids = (int*)(lds + 4 * HALF) + wave * 2 * 64;
+    const int* const ids = (const int*)(lds + L::ids(wave));
     const uint32_t ids0 = __builtin_amdgcn_readfirstlane(lds_addr_of(ids));
     const int blocks = end > begin ? (end - begin + KVB - 1) / KVB : 0;
-    const bool simple = a.c.page_size % MINE == 0 && a.c.d == D && a.c.slot < 1 << 24;
+    const bool simple = L::simple(a.c);
     auto row_of = [&](int n) INLINE { return begin + n * KVB + wave * MINE; };
-    auto ask_ids = [&](int n) INLINE { ask_page(a.c, pages, row_of(n) + (lane & (MINE - 1)), end, ids0 + (n & 1) * 256); };
-    // Rows in one page, as those of a wave are where pages hold whole shares of a block: their place is the wave's, a lane's chunk an offset.
-    // Anything else row by row, which takes a hundred instructions instead of a dozen.
+    auto ask_ids = [&](int n) INLINE { ask_page(a.c, pages, row_of(n) + (lane & (MINE - 1)), end, ids0 + L::ids_of(n)); };
+    // Rows in one page by an offset from the wave's place, anything else row by row, which takes a hundred instructions instead of a dozen.
     auto ask_block = [&](int n, bool whole) INLINE {
-      const uint32_t to = lds0 + (n & 1) * 2 * HALF + wave * ASKS * 1024;
-      const int page = __builtin_amdgcn_readfirstlane(ids[(n & 1) * 64]);
-      if (whole && (uint32_t)page < (uint32_t)a.c.pages) {
-        const int slot = row_of(n) - (int)((unsigned long long)(uint32_t)row_of(n) * a.c.magic >> a.c.shift) * a.c.page_size;
-        const char* k = a.c.keys + (head + page * a.c.page + slot * a.c.slot);
+      const uint32_t to = lds0 + L::stage(n) + L::share(wave);
+      const int page = __builtin_amdgcn_readfirstlane(ids[L::ids_of(n) / 4]);
+      if (whole && kv_is_page(a.c, page)) {
+        const char* k = a.c.keys + (head + kv_row_of_page(a.c, row_of(n), page));
         const long long apart = a.c.values - a.c.keys;
 #pragma unroll
         for (int j = 0; j < ASKS; j++) {
-          const uint32_t off = ((lane % CH ^ swizzle<CH>(lane / CH)) ^ swizzle<CH>(wave * MINE + j * (64 / CH))) * 16 + lane / CH * (uint32_t)a.c.slot;
+          const uint32_t off = L::simple_offset(lane, wave * MINE + j * (64 / CH), (uint32_t)a.c.slot);
           slab_load16s((const uint8_t*)k, off, to + j * 1024);
           slab_load16s((const uint8_t*)k + apart, off, to + HALF + j * 1024);
           k += 64 / CH * a.c.slot;
@@ -723,7 +669,7 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
       } else {
         const int l = hidden(lane);                 // nothing of this is worth a register beside the blocks that do without it
         const AttendArgs k = args_again();
-        const long long mine = row_at(k.c, row_of(n) + (l & (MINE - 1)), end, ids[(n & 1) * 64 + l]);
+        const long long mine = kv_row_or_behind(k.c, row_of(n) + (l & (MINE - 1)), end, ids[L::ids_of(n) / 4 + l]);
 #pragma unroll
         for (int j = 0; j < ASKS; j++) {
           const Chunk x = chunk_of<T, CH>(k.c, l, mine, j * (64 / CH), wave * MINE + j * (64 / CH));
@@ -732,11 +678,7 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
         }
       }
     };
-    const uint32_t k_at = l32 * (D * EB) + ((h2 ^ swizzle<CH>(l32)) * 16);
-    const int v_row = 4 * h2 + (EB == 2 ? (lane & 15) / 4 : 0);
-    const uint32_t v_at = HALF + v_row * (D * EB) +
-                          (EB == 2 ? ((2 * (lane >> 4 & 1) + (lane & 3) / 2 ^ swizzle<CH>(v_row)) * 16) + (lane & 1) * 8
-                                   : ((l32 / 4 ^ swizzle<CH>(v_row)) * 16) + (l32 & 3) * 4);
+    const uint32_t k_at = L::key0(l32, h2), v_at = L::value0(lane);
     v16f o[DT] = {};
     float m = -INFINITY, l = 0.f;
     auto block = [&](int n, auto is_masked) INLINE {
@@ -744,16 +686,16 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
       const int k0 = begin + n * KVB;
       wait_vm_barrier<0>();
       if (n + 1 < blocks) {
-        ask_block(n + 1, simple && k0 + 2 * KVB <= end);
+        ask_block(n + 1, simple && L::simple_block(k0 + KVB, end));
         ask_ids(n + 2);
       }
       if (masked && k0 >= wave_end) return;
-      const uint32_t ks = hidden(lds0 + (n & 1) * 2 * HALF + k_at);
+      const uint32_t ks = hidden(lds0 + L::stage(n) + k_at);
       // products and the reads AHEAD of them in a fixed order: left alone, the compiler waits for every read in front of its product
-      constexpr int QK = KT * CH / 2, STEPS = 16 / N, PV = KT * STEPS * DT, AHEAD = 4;         // a step: 16 rows, or 8
+      constexpr int QK = KT * CH / 2, STEPS = L::STEPS, PV = KT * STEPS * DT, AHEAD = 4;
       v16f s[KT];
       F k[AHEAD];
-      auto key = [&](int i) INLINE { return at_lds<F>((ks ^ (2 * (i % (CH / 2)) * 16)) + 32 * (i / (CH / 2)) * (D * EB)); };
+      auto key = [&](int i) INLINE { return at_lds<F>(L::key(ks, i / (CH / 2), i % (CH / 2))); };
 #pragma unroll
       for (int i = 0; i < AHEAD; i++) k[i] = key(i);
 #pragma unroll
@@ -803,7 +745,7 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
         weights(LIFT<T> - (m == -INFINITY ? 0.f : m));       // nothing seen so far, or only scores of -inf: zeros
       }
       l += sum;
-      const uint32_t vs = hidden(lds0 + (n & 1) * 2 * HALF + v_at);
+      const uint32_t vs = hidden(lds0 + L::stage(n) + v_at);
       F v[AHEAD];
       auto value = [&](int i) INLINE {
         const int d = i % DT, row = i / DT * 2 * N;
@@ -811,11 +753,11 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
         if constexpr (EB == 2) {
           union { F f; v4s half[2]; } y;
 #pragma unroll
-          for (int j = 0; j < 2; j++) y.half[j] = at_lds_turned((vs ^ ((4 * d ^ swizzle<CH>(8 * j)) * 16)) + (row + 8 * j) * (D * EB));
+          for (int j = 0; j < 2; j++) y.half[j] = at_lds_turned(L::value_16_bit(vs, row, j, d));
           x = y.f;
         } else {
 #pragma unroll
-          for (int j = 0; j < 4; j++) x[j] = at_lds<float>((vs ^ ((8 * d ^ swizzle<CH>(row % 32 + j)) * 16)) + (row + j) * (D * EB));
+          for (int j = 0; j < 4; j++) x[j] = at_lds<float>(L::value_fp32(vs, row, j, d));
         }
         return x;
       };
@@ -841,7 +783,7 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
     if (blocks > 0) {
       ask_ids(0);
       wait_vm_lds<0>();
-      ask_block(0, simple && begin + KVB <= end);
+      ask_block(0, simple && L::simple_block(begin, end));
       ask_ids(1);
     }
     // blocks that every query of the wave sees whole come first
@@ -851,24 +793,14 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
     bool bad = false;
 #pragma unroll
     for (int d = 0; d < DT; d++) bad |= has_nan(o[d]);
-    if (!again) {                                   // the stages are all waves': all of them again or none
-      lost[wave] = __any(bad);
-      __syncthreads();
-    }
-    again = !again && any_of<NW>(lost);
-    if (again) {
-      at -= take;
-      continue;
-    }
+    lost[pass][wave] = __any(bad);                  // read while others say the next one
     l += __shfl_xor(l, 32, 64);
-    if (there) {
+    if (there && it.slot >= 0) {
       const AttendArgs k = args_again();
-      const long long in = row - (long long)it.tile * ROWS;
-      float* const part = k.part + ((long long)it.slot * ROWS + in) * k.c.d;
-      T* const out = (T*)(const_cast<char*>(k.out.at) + (it.s.t0 + token) * k.out.token + (h * group + (int)(row - (long long)token * group)) * k.out.head);
-      const float by = l == 0.f ? 0.f : 1.f / l;
-      if (it.slot >= 0 && h2 == 0) {
-        float* const st = k.part + 2ll * k.slots * ROWS * k.c.d + ((long long)it.slot * ROWS + in) * 2;
+      const int in = wave * 32 + l32;
+      float* const part = k.part + kv_part_at(it.slot, ROWS, in, k.c.d);
+      if (h2 == 0) {
+        float* const st = k.part + kv_stat_at(k.slots, it.slot, ROWS, in, k.c.d);
         st[0] = m, st[1] = l;
       }
 #pragma unroll
@@ -876,15 +808,29 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
 #pragma unroll
         for (int p = 0; p < 4; p++) {
           const int e = 32 * d + 8 * p + 4 * h2;
-          if (e >= k.c.d) continue;
-          if (it.slot >= 0) {
-            *(v4f*)(part + e) = (v4f){o[d][4 * p], o[d][4 * p + 1], o[d][4 * p + 2], o[d][4 * p + 3]};
-          } else {
-            Pack<T, 4> z;
+          if (e < k.c.d) *(v4f*)(part + e) = (v4f){o[d][4 * p], o[d][4 * p + 1], o[d][4 * p + 2], o[d][4 * p + 3]};
+        }
+    }
+    __syncthreads();                                // the stages are free, and all waves go over the tile again or none; results may lie where queries did
+    again = !again && any_of<NW>(lost[pass]);
+    if (again) {
+      at -= take;
+      continue;
+    }
+    if (there && it.slot < 0) {
+      const AttendArgs k = args_again();
+      T* const out = (T*)(const_cast<char*>(k.out.at) + kv_query_at(it.s.t0, kv_query(row, token, group), h, group, k.out.token, k.out.head));
+      const float by = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-            for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(l == 0.f ? 0.f : o[d][4 * p + j] * by);
-            *(Pack<T, 4>*)(out + e) = z;
-          }
+      for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int p = 0; p < 4; p++) {
+          const int e = 32 * d + 8 * p + 4 * h2;
+          if (e >= k.c.d) continue;
+          Pack<T, 4> z;
+#pragma unroll
+          for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(l == 0.f ? 0.f : o[d][4 * p + j] * by);
+          *(Pack<T, 4>*)(out + e) = z;
         }
     }
   }
@@ -900,7 +846,7 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
   __shared__ v4f sums[256];
   __shared__ float stat[256][2];
   const int first = blockIdx.y * per, count = *count_of(a, rows);
-  const Left t = left_of(a, rows)[blockIdx.x];      // behind the count: whatever the memory held
+  const KvLeft t = left_of(a, rows)[blockIdx.x];      // behind the count: whatever the memory held
   if ((int)blockIdx.x >= count || t.pieces <= 1 || first >= t.rows) return;
   const int pieces = t.pieces, there = t.rows, tile = t.tile, h = t.h, w0 = t.w0;
   const int quads = a.c.d / 4, share = 256 / (few * quads), e = threadIdx.x % (few * quads), part = threadIdx.x / (few * quads), c = e % quads;
@@ -916,9 +862,9 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
 #pragma unroll
       for (int k = 0; k < FLY; k++) {
         const int at = min(p + k * share, pieces - 1);
-        const long long slot = 2 * (w0 + at) + (at == 0);
-        const float* const st = a.part + 2ll * a.slots * rows * a.c.d + (slot * rows + r) * 2;
-        x[k] = *(const v4f*)(a.part + (slot * rows + r) * a.c.d + c * 4);
+        const int slot = kv_slot_of(w0, at);
+        const float* const st = a.part + kv_stat_at(a.slots, slot, rows, r, a.c.d);
+        x[k] = *(const v4f*)(a.part + kv_part_at(slot, rows, r, a.c.d) + c * 4);
         top[k] = p + k * share < pieces ? st[0] : -INFINITY;
         sum[k] = st[1];
       }
@@ -954,12 +900,12 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
       sum += f * stat[p * few * quads + e][1];
       y += rescaled(sums[p * few * quads + e], f);
     }
-    const long long of = (long long)tile * rows + r;
-    const int i = (int)(of / a.group), g = (int)(of - (long long)i * a.group);
+    const long long row = (long long)tile * rows + r;
+    const KvQuery of = kv_query(row, kv_token(row, a.group), a.group);
     Pack<T, 4> z;
 #pragma unroll
     for (int j = 0; j < 4; j++) z.v[j] = from_float<T>(sum == 0.f ? 0.f : y[j] / sum);
-    *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + (t.t0 + i) * a.out.token + (h * a.group + g) * a.out.head) + c * 4) = z;
+    *(Pack<T, 4>*)((T*)(const_cast<char*>(a.out.at) + kv_query_at(t.t0, of, h, a.group, a.out.token, a.out.head)) + c * 4) = z;
   }
 }
 
@@ -974,50 +920,9 @@ int attend_args(const pahq_kv_cache* cache, const pahq_kv_batch* batch, int q_he
   return PAHQ_OK;
 }
 
-// How a call is cut.  What the host sees of it decides, as the size of the workspace does too.
-struct Cut {
-  int rows;                                         // of a tile
-  bool waves;                                       // of few rows: a workgroup has a compute unit to itself, and so many waves
-  int slots;                                        // ranges at most (kv_plan.h), 0: tiles are given out whole in any case
-  int least, over;                                  // units of a range at least, and what beginning a tile counts
-  int enough, brief;                                // where that pays, see kv_cut_from
-};
-long long tiles_of(const AttendArgs& a, const Cut& k) { return kv_most_tiles(a.b.tokens, a.b.batch, a.group, k.rows) * a.c.heads; }
-Cut cut_of(const AttendArgs& a, int eb) {
-  Cut k;
-  // Rows a sequence and head.  Every tile reads its sequence's rows of the cache, so they decide: 8 sequences of 64 tokens, 4 heads of a
-  // group, over up to 8000 rows take 44 us in tiles of 128 and 140 us in tiles of 16; 64 single tokens of 4 heads over up to 16384 rows
-  // take 172 us in tiles of 16 and 198 us in tiles of 128, which then mostly hold nothing.
-  const long long mean = (((long long)a.b.tokens + a.b.batch - 1) / std::max(a.b.batch, 1)) * a.group;
-  // heads of more than 128 columns in fp32 stay with 16: more rows of theirs do not fit the registers
-  k.rows = mean <= 16 || (eb == 4 && a.c.d > 128) ? 16 : mean <= 32 ? 32 : 128;
-  const long long tiles = tiles_of(a, k);
-  // Few tiles: one workgroup of many waves on a compute unit has half the parts to join, and 4 us less of 94 to do for a token over 131072
-  // rows.  Many short ones hide each other's beginnings in two workgroups (256 tokens over 1024 rows, 8 heads: 181 us instead of 198).
-  k.waves = k.rows < 128 && tiles < 1024;
-  k.slots = k.waves ? 256 : 512;
-  k.least = 4;
-  k.over = k.rows < 128 ? 2 : 5;
-  // Equal tiles, some for each range, are cut for the last ones would leave workgroups idle: 40 tokens over 4096 rows, 8 heads, 109 us
-  // instead of 138, 200 over 512 80 instead of 90, 200 over 2048 274 instead of 291; at eight for a range (500 over 1024) it would lose 2 %.
-  // Prompts' do not: the first tiles see little, and are done while the last ones run.
-  k.enough = k.rows < 128 ? 5 * k.slots : 0;
-  // What cutting costs in units: the parts' way through memory and the join, 5 to 15 us.  One token of 4 heads over 500 rows takes 12.5 us
-  // whole and 16.5 cut, over 1000 rows 19 and 17; 1500 tokens of a prompt 42 and 67; 128 behind 640 others 22 and 24, behind 1372 37 and 27.
-  // In fp32, whose units take longer, 300 tokens of a prompt 28 and 32, 100 behind 300 others 66 and 36.
-  k.brief = k.rows < 128 ? 8 : eb == 2 ? 18 : 12;
-  // Not even the longest sequence that the lists of pages have room for would be cut, or the new tokens alone are so much work that a range is as
-  // long as any sequence can be
-  const int wide = eb * (a.c.d <= 64 ? 64 : a.c.d <= 128 ? 128 : 256), unit = k.rows < 128 ? 32768 / wide : wide <= 256 ? 64 : 32;
-  const bool few = k.rows == 128 || tiles <= KV_FEW_TILES;
-  const double work = (double)a.b.tokens * a.b.tokens * a.group / ((double)k.rows * std::max(a.b.batch, 1)) * a.c.heads / k.slots;
-  if (a.b.most <= 256 || (few && kv_units_of(a.b.most, unit, k.over) <= k.brief) || a.b.most <= work) {
-    k.slots = 0;
-    k.waves = k.rows < 128 && tiles <= KV_FEW_TILES;
-  }
-  return k;
-}
-size_t part_bytes(const AttendArgs& a, const Cut& k) { return k.slots ? 2ull * k.slots * k.rows * (a.c.d + 2) * 4 + 32 + k.slots * sizeof(Left) : 0; }
+KvCut cut_of(const AttendArgs& a, int eb) { return kv_cut(a.b.tokens, a.b.batch, a.group, a.c.heads, a.b.most, a.c.d, eb); }
+long long tiles_of(const AttendArgs& a, const KvCut& k) { return kv_call_tiles(a.b.tokens, a.b.batch, a.group, a.c.heads, k.rows); }
+size_t part_bytes(const AttendArgs& a, const KvCut& k) { return kv_part_bytes(k.slots, k.rows, a.c.d); }
 
 template <void (*K)(AttendArgs), int THREADS, int LDS>
 int launch(hipStream_t st, unsigned grid, const AttendArgs& a) {
@@ -1035,31 +940,25 @@ int launch(hipStream_t st, unsigned grid, const AttendArgs& a) {
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
 template <typename T, int D>
-int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
-  constexpr int EB = sizeof(T), WIDE = D * EB, STAGES = 4 * (EB == 2 ? 32 : 16) * WIDE;       // a wave's
-  constexpr int NW = std::max(2, 65536 / STAGES), MANY = std::max(NW, 131072 / STAGES);
-  constexpr int KVB = WIDE <= 256 ? 64 : 32;
+int attend_as(hipStream_t st, const AttendArgs& a, const KvCut& k) {
+  constexpr int EB = sizeof(T), NW = KvWaves<EB, D>::NW, MANY = KvWaves<EB, D>::MANY;
   const long long tiles = tiles_of(a, k);
   const unsigned grid = (unsigned)std::max<long long>(tiles, k.slots);
   int rc = PAHQ_EHIP;
-  if (k.rows == 16) rc = k.waves ? launch<kv_few_k<T, D, 1, MANY>, MANY * 64, MANY * (STAGES + 1024)>(st, grid, a)
-                                 : launch<kv_few_k<T, D, 1, NW>, NW * 64, NW * (STAGES + 1024)>(st, grid, a);
-  if constexpr (WIDE <= 512) {
-    if (k.rows == 32) rc = k.waves ? launch<kv_few_k<T, D, 2, MANY>, MANY * 64, MANY * (STAGES + 1024)>(st, grid, a)
-                                   : launch<kv_few_k<T, D, 2, NW>, NW * 64, NW * (STAGES + 1024)>(st, grid, a);
-    if (k.rows == 128) rc = launch<kv_tile_k<T, D, KVB>, 256, 4 * KVB * WIDE + 2048>(st, grid, a);
+  if (k.rows == 16) rc = k.waves ? launch<kv_few_k<T, D, 1, MANY>, MANY * 64, KvFew<EB, D, 1, MANY>::LDS>(st, grid, a)
+                                 : launch<kv_few_k<T, D, 1, NW>, NW * 64, KvFew<EB, D, 1, NW>::LDS>(st, grid, a);
+  if constexpr (D * EB <= 512) {
+    if (k.rows == 32) rc = k.waves ? launch<kv_few_k<T, D, 2, MANY>, MANY * 64, KvFew<EB, D, 2, MANY>::LDS>(st, grid, a)
+                                   : launch<kv_few_k<T, D, 2, NW>, NW * 64, KvFew<EB, D, 2, NW>::LDS>(st, grid, a);
+    if (k.rows == 128) rc = launch<kv_tile_k<T, D, KvWide<EB, D>::KVB>, 256, KvWide<EB, D>::LDS>(st, grid, a);
   }
   if (rc || !k.slots) return rc;
-  // as many rows of a workgroup that its launch, a workgroup in 3 to 4 ns, does not take longer than what they do
-  const int left = (int)std::min<long long>(tiles, k.slots);
-  int per = 1, few = 1;
-  while (per < k.rows && left * (k.rows / per) > 2048) per *= 2;
-  while (few * 2 <= std::min(per, 8) && few * 2 * (a.c.d / 4) <= 256) few *= 2;
-  hipLaunchKernelGGL(kv_join_k<T>, dim3(left, k.rows / per), dim3(256), 0, st, a, k.rows, per, few);
+  const KvJoin j = kv_join(tiles, k.slots, k.rows, a.c.d);
+  hipLaunchKernelGGL(kv_join_k<T>, dim3(j.left, k.rows / j.per), dim3(256), 0, st, a, k.rows, j.per, j.few);
   return hipGetLastError() == hipSuccess ? PAHQ_OK : PAHQ_EHIP;
 }
 template <typename T>
-int attend_as(hipStream_t st, const AttendArgs& a, const Cut& k) {
+int attend_as(hipStream_t st, const AttendArgs& a, const KvCut& k) {
   return a.c.d <= 64 ? attend_as<T, 64>(st, a, k) : a.c.d <= 128 ? attend_as<T, 128>(st, a, k) : attend_as<T, 256>(st, a, k);
 }
 }  // namespace
@@ -1075,7 +974,7 @@ extern "C" int pahq_kv_attention_workspace(const pahq_kv_cache* cache, const pah
   if (const int rc = attend_args(cache, batch, q_heads, &a, held, lists)) return rc;
   *bytes = 0;
   if (a.b.batch == 0 || a.b.tokens == 0) return PAHQ_OK;
-  const Cut cut = cut_of(a, dtype_bytes(cache->dtype));
+  const KvCut cut = cut_of(a, dtype_bytes(cache->dtype));
   if (tiles_of(a, cut) >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;
   *bytes = part_bytes(a, cut);
   return PAHQ_OK;
@@ -1091,7 +990,7 @@ extern "C" int pahq_kv_attention(void* hip_stream, const pahq_kv_cache* cache, c
   if (batch->batch == 0 || batch->tokens == 0) return PAHQ_OK;
   const int eb = dtype_bytes(cache->dtype), tokens = batch->tokens;
   if (!kv_rows_args(q, tokens, q_heads, a.c.d, eb, false, &a.q, &qr) || !kv_rows_args(out, tokens, q_heads, a.c.d, eb, true, &a.out, &outr)) return PAHQ_EINVAL;
-  const Cut cut = cut_of(a, eb);
+  const KvCut cut = cut_of(a, eb);
   if (tiles_of(a, cut) >= KV_MOST_ITEMS) return PAHQ_ETOOBIG;      // workgroups of a launch, whose threads are counted in 32 bits
   const size_t need = part_bytes(a, cut);
   if (need && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return PAHQ_EINVAL;
