@@ -1,6 +1,7 @@
 """Builds libpahq.so (HIP, gfx950 only) in-tree with hipcc, and _tensors.so, the torch side of its operators on device tensors."""
 import importlib.util
 import os
+import re
 import shutil
 import subprocess
 import sysconfig
@@ -21,10 +22,33 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=o
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
+# Kernels that may not keep registers in scratch memory: their waits count the memory operations that they have in flight themselves, and
+# one that spilled on its way to its addresses would reach memory with what it read back.
+NO_SCRATCH = {"kv_cache.hip", "kv_attention.hip"}
+RESOURCES = "-Rpass-analysis=kernel-resource-usage"
+
+
+def scratch_of(remarks):
+    """{kernel: bytes of scratch a lane} of the kernels that have any, from what the compiler says with RESOURCES."""
+    found = re.findall(r"Function Name: (\S+)|ScratchSize \[bytes/lane\]: (\d+)|(Dynamic Stack: True)", remarks)
+    out, name = {}, None
+    for function, size, stack in found:
+        name = function or name
+        if stack or int(size or 0):
+            out[name] = int(size or 0)
+    return out
+
+
 def _compile(src):
     obj = os.path.join(HERE, "_build", src.replace(".hip", ".o"))
-    subprocess.run(["hipcc", *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj], check=True,
-                   stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    said = subprocess.run(["hipcc", *FLAGS, *([RESOURCES] if src in NO_SCRATCH else []), "-c", os.path.join(CSRC, src), "-o", obj], check=True,
+                          stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    if src in NO_SCRATCH and said is not None:
+        remarks = said.stdout.decode(errors="replace")
+        spilled = scratch_of(remarks)
+        if spilled or "ScratchSize" not in remarks:
+            os.remove(obj)
+            raise RuntimeError("%s: kernels with registers in scratch memory: %s" % (src, spilled or "the compiler does not say"))
     return obj
 
 
