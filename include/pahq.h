@@ -523,9 +523,9 @@ int pahq_rotary(void* hip_stream, const void* x, int32_t dtype, int32_t tokens, 
  *                   last ones; `pages` [batch][width], row stride ld_pages >= width.  With n_b = starts[b + 1] - starts[b], new
  *                   token i of sequence b is its row base_b + i, base_b = lengths[b] - n_b
  * What the device arrays hold is not the host's to check, and whatever it is, no memory is touched that is not the operands': starts
- * are clipped to 0 .. tokens and a negative n_b is 0; a length is clipped to width * page_size; a token whose row would be negative
- * or behind its list of pages, or whose page is not 0 .. pages - 1, is not written, and a query that sees a row of such a
- * page gets NaN.  Rows of tokens in front of starts[0] or behind starts[batch] are not written.  Two tokens with one place (a page
+ * are clipped to 0 .. tokens and a negative n_b is 0; a length is clipped to width * page_size, and of a sequence that is longer no token
+ * is written and no row moves; a token whose row would be negative, or whose page is not 0 .. pages - 1, is not written, and a query that
+ * sees a row of such a page gets NaN.  Rows of tokens in front of starts[0] or behind starts[batch] are not written.  Two tokens with one place (a page
  * in two lists, or twice in one) are written in any order.
  *
  * pahq_kv_append writes new tokens' rows: keys turned as pahq_rotary turns them, values as they are; and out gets the queries, turned the same way.

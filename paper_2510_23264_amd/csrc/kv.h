@@ -112,6 +112,8 @@ __device__ __forceinline__ int kv_start(const KvBatch& q, int b) { return kv_cli
 __device__ __forceinline__ KvSequence kv_sequence(const KvBatch& q, int b) {
   return kv_clipped(q.starts[b], q.starts[b + 1], q.lengths[b], q.tokens, q.most);
 }
+// Where a sequence has outgrown its list of pages its clipped rows are other ones than those it means: nothing is written there
+__device__ __forceinline__ bool kv_has_room(const KvBatch& q, int b) { return q.lengths[b] <= q.most; }
 // The sequence that token t belongs to: the last b in [0, batch] with start(b) <= t, -1 for none (and `batch` for tokens behind the last).
 // Of starts that do not grow any one comes out; the caller checks that t lies in its sequence.
 template <typename F> __device__ __forceinline__ int kv_owner(int batch, int t, F start) {

@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256) void kv_append_k(AppendArgs a) {
       const KvSequence s = kv_sequence(a.b, b);
       if (t < s.t0 + s.n) {
         const int row = s.base + (t - s.t0);
-        p = row >= 0 ? kv_row(a.c, a.b.pages + b * a.b.ld, row) : -1;
+        p = row >= 0 && kv_has_room(a.b, b) ? kv_row(a.c, a.b.pages + b * a.b.ld, row) : -1;
         at_row[threadIdx.x] = row;
       }
     }
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256) void kv_keep_k(KvCache c, KvBatch q, const int
     }
   }
   __syncthreads();
-  const int chunks = row_bytes / 16, step = 256 / chunks, mine = threadIdx.x / chunks, at = (threadIdx.x - mine * chunks) * 16, n = stay;
+  const int chunks = row_bytes / 16, step = 256 / chunks, mine = threadIdx.x / chunks, at = (threadIdx.x - mine * chunks) * 16, n = kv_has_room(q, b) ? stay : 0;
   const int* const pages = q.pages + b * q.ld;
   for (int i0 = 0; i0 < n; i0 += step) {
     const int i = i0 + mine;

@@ -91,6 +91,26 @@ def test_tokens_without_a_place(P):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=str)
+def test_a_list_that_is_too_short_costs_no_row(P, dtype):
+    """A sequence that has outgrown its list of pages: nothing of it is written or moved, and the rows that it has stay."""
+    for length in (33, 40, 1000, 2 ** 31 - 1):
+        case = Case((3, 2), (32, 20), 2, 2, 64, 16, dtype)
+        cache, batch, q = case.device(P)
+        k, v = torch.randn(2, 5, 2, 64, device="cuda").to(dtype)
+        batch.lengths[0] = length
+        keys, values = case.keys.clone(), case.values.clone()
+        for i, row in enumerate((18, 19)):                              # the other sequence's rows
+            keys[case.table[1][row // 16], :, row % 16], values[case.table[1][row // 16], :, row % 16] = k[3 + i].cpu(), v[3 + i].cpu()
+        P.kv_append(cache, batch, k, v)
+        assert same(cache.keys, keys) and same(cache.values, values)
+        after = P.kv_keep(cache, batch, torch.tensor([[1, 2], [1, -1]], dtype=torch.int32, device="cuda"))
+        assert after[1] == 19
+        for rows in (keys, values):
+            rows[case.table[1][18 // 16], :, 18 % 16] = rows[case.table[1][19 // 16], :, 19 % 16]
+        assert same(cache.keys, keys) and same(cache.values, values)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
 @pytest.mark.parametrize("heads, d, page, order", [(1, 8, 1, "heads"), (2, 128, 16, "joined"), (3, 256, 7, "slots"), (12, 64, 32, "outer slots"), (5, 80, 24, "heads")])
 def test_keep_moves_a_path(P, dtype, heads, d, page, order):
     """Against moving all rows at once: paths of every kind, also ones that end early because they do not grow or leave the tree."""
