@@ -134,3 +134,27 @@ def test_a_scale_of_zero_hides_no_query(P, dtype, new, lengths, bad):
     assert got[case.tokens // 2, 1].isnan().all()
     got[case.tokens // 2, 1] = clean[case.tokens // 2, 1]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("new, lengths", SHAPES)
+@pytest.mark.parametrize("d", [64, 128, 192, 256])
+def test_the_same_call_gives_the_same_bits(P, dtype, new, lengths, d):
+    """Trees and causal calls, over and over, with memory of other values where the workspace and results come to lie; in place too; and with an
+    infinite value, for which tiles are done twice."""
+    case = wide(Case(new, lengths, 2, 3, d, 16, dtype, seed=d))
+    tree = torch.randint(-2 ** 63, 2 ** 63 - 1, (case.tokens, -(-max(new) // 64)), generator=case.g).cuda()
+    cache, batch, q = case.device(P)
+    for infinite in (False, True):
+        if infinite:
+            cache.keys[case.table[0][0], :, 2, :] = cache.keys[case.table[0][0], :, 2, :] * 16
+            cache.values[case.table[0][0], :, 2, 5] = float("inf")
+        for mask in (None, tree):
+            first = P.kv_attention(q, cache, batch, tree=mask)
+            for k in range(6):
+                torch.full((1 << 22,), float(k), device="cuda")
+                assert torch.equal(P.kv_attention(q, cache, batch, tree=mask), first)
+            mine = q.clone()
+            P.kv_attention(mine, cache, batch, tree=mask, out=mine)
+            assert torch.equal(mine, first)
+            assert infinite == bool((~first.isfinite()).any()) or (mask is not None and lengths[0] == new[0])
