@@ -158,3 +158,30 @@ def test_the_same_call_gives_the_same_bits(P, dtype, new, lengths, d):
             P.kv_attention(mine, cache, batch, tree=mask, out=mine)
             assert torch.equal(mine, first)
             assert infinite == bool((~first.isfinite()).any()) or (mask is not None and lengths[0] == new[0])
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
+@pytest.mark.parametrize("group", [1, 20, 40])
+@pytest.mark.parametrize("low", [15, 18, 20, 21, 22, 23, 24, 25])
+def test_many_small_weights_count_as_one_large_does(P, dtype, group, low):
+    """One row of score 0 and 16000 of 2^-low each, that together weigh 0.5 to 2^-11 of it; values 0 there, 1 here.  fp16 holds a weight down to 2^-31 of
+    the largest (2^-24 times 2^-7), some as numbers that are not normal, and the two sums have to take the same ones: sums of 16000 terms of one sign in
+    fp32, off by 16000 2^-24 = 2^-10 each, a weight rounded by half a step of its own or by 2^-32 of the largest, half a step of the result."""
+    n, d = 16001, 64
+    case = Case([1], [n], 1, group, d, 64, dtype)
+    case.q.zero_()
+    case.q[:, :, 0] = 1
+    there = ~case.keys[:, :, :, 0].isnan()
+    case.keys[:, :, :, 0][there] = 0.0
+    case.values[~case.values.isnan()] = 1.0
+    x = torch.tensor(low * 0.6931471805599453).to(dtype)
+    for j in range(0, n, 64):
+        case.keys[case.table[0][j // 64], 0, :min(64, n - j), 0] = -x
+    case.keys[case.table[0][100], 0, 5, 0] = 0.0
+    case.values[case.table[0][100], 0, 5] = 0.0
+    w = float(torch.exp(-x.double()))
+    want = 16000 * w / (1 + 16000 * w)
+    got = run(P, case, scale=1.0).double().cpu()
+    u = torch.finfo(dtype).eps / 2
+    lim = want * (2 * 2.0 ** -10 + 2 * u + (2.0 ** -32 / w if dtype == torch.float16 else 0.0))
+    assert (got - want).abs().max() <= lim, (float(got.min()), float(got.max()), want, lim)
