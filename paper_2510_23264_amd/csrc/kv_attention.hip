@@ -853,9 +853,12 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
   for (int r0 = first; r0 < first + per && r0 < there; r0 += few) {
     const int r = r0 + e / quads;
     const bool mine = part < share && r < there;
-    float m = -INFINITY, l = 0.f;
-    v4f y = {0, 0, 0, 0};
+    float m, l;
+    v4f y;
+    auto add_parts = [&](auto infinities) INLINE {  // they stay only where that is asked for: it takes as many instructions again
     constexpr int FLY = 4;                          // parts on their way at a time
+    m = -INFINITY, l = 0.f;
+    y = (v4f){0, 0, 0, 0};
     for (int p = part; mine && p < pieces; p += FLY * share) {
       v4f x[FLY];
       float top[FLY], sum[FLY];
@@ -872,19 +875,22 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
 #pragma unroll
       for (int k = 0; k < FLY; k++) most = fmaxf(most, top[k]);
       const float safe = most == -INFINITY ? 0.f : most, by = __builtin_amdgcn_exp2f(m - safe);
-      y = rescaled(y, by);
+      y = infinities ? rescaled(y, by) : y * by;
       l *= by;
       m = most;
 #pragma unroll
       for (int k = 0; k < FLY; k++) {
         const float f = __builtin_amdgcn_exp2f(top[k] - safe);
         const bool there = p + k * share < pieces;  // not again what stands in for a part behind the last
-        const v4f more = rescaled(x[k], f);
+        const v4f more = infinities ? rescaled(x[k], f) : x[k] * f;
         l += there ? sum[k] * f : 0.f;
 #pragma unroll
         for (int j = 0; j < 4; j++) y[j] += there ? more[j] : 0.f;
       }
     }
+    };
+    add_parts(std::false_type());
+    if (has_nan(y)) add_parts(std::true_type());
     if (r0 > first) __syncthreads();
     sums[threadIdx.x] = y;
     stat[threadIdx.x][0] = m, stat[threadIdx.x][1] = l;
