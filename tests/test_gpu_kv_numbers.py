@@ -185,3 +185,19 @@ def test_many_small_weights_count_as_one_large_does(P, dtype, group, low):
     u = torch.finfo(dtype).eps / 2
     lim = want * (2 * 2.0 ** -10 + 2 * u + (2.0 ** -32 / w if dtype == torch.float16 else 0.0))
     assert (got - want).abs().max() <= lim, (float(got.min()), float(got.max()), want, lim)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("new, lengths", SHAPES)
+def test_large_values_do_not_overflow(P, dtype, new, lengths):
+    """Values times 2^104 give 2^104 times the answer, every rounding being the same: values below 2^3 and lengths below 2^11 leave all sums below 2^128.
+    Growing scores, with which weights are as large as they get."""
+    case = wide(Case(new, lengths, 2, 1, 64, 16, dtype, seed=1))
+    case.q[:, :, 0] = 1
+    for b, n in enumerate(lengths):
+        for j in range(n):
+            case.keys[case.table[b][j // 16], :, j % 16, 0] = 0.125 * j
+    assert case.values[~case.values.isnan()].abs().max() < 8
+    plain = run(P, case)
+    case.values *= 2.0 ** 104
+    assert torch.equal(run(P, case), plain * 2.0 ** 104) and plain.isfinite().all()
