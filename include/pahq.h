@@ -563,7 +563,8 @@ int pahq_kv_append(void* hip_stream, const pahq_kv_cache* cache, const pahq_kv_b
  *                 with [n][(n + 63) / 64] words, a node's own bit and its ancestors', from parents [n]: parents[i] < i, -1 at a root
  * What a query does not see has no influence on it, infinities and NaN included; an infinite value that it sees counts however small its
  * weight, and both infinities make NaN.  One that sees nothing, or only scores of -inf, gets zeros.  Products in the cache's dtype with sums in fp32, softmax in fp32, its weights rounded to the dtype for their product
- * with the values, the sum divided by the weights' sum and rounded once.  The same call gives the same bits.
+ * with the values, the sum divided by the weights' sum and rounded once.  Before the division a sequence's weights come to 2^10 times its
+ * length at most: no sum overflows for values below 2^118 / length in size.  The same call gives the same bits.
  * q, out as in pahq_kv_append; out may be q itself with the same strides.  tokens * (q_heads / heads) below 2^31 - 2^16; more than that is too
  * big, as are 2^24 tiles of 16 to 128 (token, query head) pairs of one cache head and sequence: fewer where tokens * q_heads / 16 + batch * heads
  * is below 2^24.

@@ -305,7 +305,8 @@ template <typename T, typename F> __device__ __forceinline__ F take_kinds(F* v) 
 }
 // That is done in masked blocks.  In the others an infinite value times a weight that rounded to zero, or an infinite sum that is rescaled by
 // zero, leaves NaN where infinity belongs, for the weight is positive in the definition: a tile with a NaN is done once more with all its
-// blocks masked, and sums are rescaled so there, and where parts of them meet, that infinities stay.
+// blocks masked, and sums are rescaled so there, and where parts of them meet, that infinities stay.  To look for a NaN and to have all
+// waves know takes 0.5 us of a call of 9 us, 1.5 us of the 44 us of the trees below, nothing to 0.5 % of the long ones.
 template <typename V> __device__ __forceinline__ V rescaled(V x, float by) { return __builtin_elementwise_abs(x) == INFINITY ? x : x * by; }
 template <typename V> __device__ __forceinline__ bool has_nan(const V& x) {
   bool bad = false;
@@ -339,7 +340,7 @@ __device__ __forceinline__ float of_kinds(float count) {
 // RT = 2 serves 17 to 32 rows with one pass instead of two (16 sequences, 8 tokens of 4 heads, 4096 rows: 58 us, 63 in tiles of 16, 65 of 128).
 //
 // Measured, bf16, 8 heads of 128 columns for 32 of queries: 64 tokens over 1024 to 16384 rows, 1.07 GB, 172 us (6.2 TB/s); one token over 131072
-// rows, 537 MB, 87 us (6.1 TB/s); fp32, 12 heads of 64 columns, one token over 200 rows 9.5 us, most of it the launch and the reads of the lists, the
+// rows, 537 MB, 88 us (6.1 TB/s); fp32, 12 heads of 64 columns, one token over 200 rows 9.6 us, most of it the launch and the reads of the lists, the
 // page's number and its rows, which wait for one another.
 template <typename T, int D, int RT, int NW>
 __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
@@ -590,12 +591,12 @@ __global__ __launch_bounds__(NW * 64) void kv_few_k(AttendArgs a) {
 // The same sums.  Four waves of 32 rows each share blocks of KVB rows of the cache, in two stages of LDS: a block's products run while the next one
 // arrives.  4 d operations for each row of queries against 2 d elements for all 128 of them: bound by instructions, not memory.  32x32 products
 // rather than 16x16, for they read half of the LDS for the same work.  K and V are read from LDS AHEAD = 4 products before they are used, held
-// there by in_order(): left to the compiler each product waits for its own read (the prompt below: 552 us with one read ahead, 519 with two, 517
-// with four; more do not fit the registers).  KVB is 64 where two stages of it fit twice into LDS (32: 553 us), 32 for rows of more than 256 bytes.
+// there by in_order(): left to the compiler each product waits for its own read (the prompt below, on one card: 552 us with one read ahead, 519
+// with two, 517 with four; more do not fit the registers).  KVB is 64 where two stages of it fit twice into LDS (32: 553 us), 32 for rows of more than 256 bytes.
 //
-// Measured, bf16, 8 heads of 128 columns for 32 of queries: a prompt of 8192 tokens 517 to 540 us (1.02 to 1.06 PFLOP/s; the matrix cores are busy for
-// about half of it, the exponentials, masks and roundings beside them take the other half of the issue slots); 8 trees of 64 tokens over up to 8000
-// rows 44 us; 512 tokens of a prompt 18 us.
+// Measured, bf16, 8 heads of 128 columns for 32 of queries: a prompt of 8192 tokens 517 to 558 us, by card and state (0.99 to 1.06 PFLOP/s; the
+// matrix cores are busy for about half of it, the exponentials, masks and roundings beside them take the other half of the issue slots);
+// 8 trees of 64 tokens over up to 8000 rows 44 us; 512 tokens of a prompt 19 us.
 template <typename T, int D> constexpr int TILE_WAVES = D * sizeof(T) <= 128 ? 3 : D * sizeof(T) <= 256 ? 2 : 1;       // of a SIMD
 template <typename T, int D, int KVB>
 __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs a) {
@@ -837,8 +838,9 @@ __global__ __launch_bounds__(256, (TILE_WAVES<T, D>)) void kv_tile_k(AttendArgs 
 }
 
 // The parts of a tile become its rows: with m the largest of the parts' maxima,  O = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p,  in the parts'
-// order, so that a call's result does not depend on which workgroup ended first.  A launch of its own, not an atomic count at the end of the others: 4 us
-// of one token over 131072 rows; bound by the latency of the list and of a part behind it, so parts are read four at a time.
+// order, so that a call's result does not depend on which workgroup ended first.  A launch of its own, 4 us of one token over 131072 rows, bound by
+// the latency of the list and of a part behind it, so parts are read four at a time.  The last workgroup of a tile to end could do
+// the same in the same order without that launch, if it saw the parts of the others through the L2s of eight XCDs; not built or measured.
 // Of the blockIdx.x-th Left, rows blockIdx.y * per and on, `few` at a time: for each of them the parts are
 // shared out over the threads that are left beside four elements each, and joined in LDS.
 template <typename T>

@@ -4,8 +4,9 @@
 // sequence's length, in units of some rows of the cache.  The host knows neither the lengths nor how the tokens are spread over the
 // sequences, so each workgroup finds its part from the batch.  Where it does not pay to cut them (kv_cut_from) tiles
 // are given out whole, as workgroups end.  Otherwise the units of all tiles, heads and sequences stand in one line, which is cut into
-// equal ranges for at most `slots` workgroups, about as many as the chip holds at a time: one long sequence beside short ones, or
-// one alone, takes the whole chip.  A range ends inside tiles at its ends only, so every workgroup leaves at most two parts
+// equal ranges for at most `slots` workgroups: one long sequence beside short ones, or one alone, takes the whole chip.  That is as many as the chip
+// holds at a time, but for heads of more than 128 columns and, in tiles of 128 rows, of more than 64 in fp32: LDS or registers leave room for
+// one workgroup on a compute unit there, and 512 ranges take two rounds.  A range ends inside tiles at its ends only, so every workgroup leaves at most two parts
 // of tiles in the workspace: in slot 2 w what it began inside of a tile, in slot 2 w + 1 what it left unfinished.  A tile's first `over`
 // units stand for what it costs to begin one; a range that ends among them leaves the tile to the next.
 #pragma once
