@@ -858,38 +858,38 @@ __global__ __launch_bounds__(256) void kv_join_k(AttendArgs a, int rows, int per
     float m, l;
     v4f y;
     auto add_parts = [&](auto infinities) INLINE {  // they stay only where that is asked for: it takes as many instructions again
-    constexpr int FLY = 4;                          // parts on their way at a time
-    m = -INFINITY, l = 0.f;
-    y = (v4f){0, 0, 0, 0};
-    for (int p = part; mine && p < pieces; p += FLY * share) {
-      v4f x[FLY];
-      float top[FLY], sum[FLY];
+      constexpr int FLY = 4;                          // parts on their way at a time
+      m = -INFINITY, l = 0.f;
+      y = (v4f){0, 0, 0, 0};
+      for (int p = part; mine && p < pieces; p += FLY * share) {
+        v4f x[FLY];
+        float top[FLY], sum[FLY];
 #pragma unroll
-      for (int k = 0; k < FLY; k++) {
-        const int at = min(p + k * share, pieces - 1);
-        const int slot = kv_slot_of(w0, at);
-        const float* const st = a.part + kv_stat_at(a.slots, slot, rows, r, a.c.d);
-        x[k] = *(const v4f*)(a.part + kv_part_at(slot, rows, r, a.c.d) + c * 4);
-        top[k] = p + k * share < pieces ? st[0] : -INFINITY;
-        sum[k] = st[1];
+        for (int k = 0; k < FLY; k++) {
+          const int at = min(p + k * share, pieces - 1);
+          const int slot = kv_slot_of(w0, at);
+          const float* const st = a.part + kv_stat_at(a.slots, slot, rows, r, a.c.d);
+          x[k] = *(const v4f*)(a.part + kv_part_at(slot, rows, r, a.c.d) + c * 4);
+          top[k] = p + k * share < pieces ? st[0] : -INFINITY;
+          sum[k] = st[1];
+        }
+        float most = m;
+#pragma unroll
+        for (int k = 0; k < FLY; k++) most = fmaxf(most, top[k]);
+        const float safe = most == -INFINITY ? 0.f : most, by = __builtin_amdgcn_exp2f(m - safe);
+        y = infinities ? rescaled(y, by) : y * by;
+        l *= by;
+        m = most;
+#pragma unroll
+        for (int k = 0; k < FLY; k++) {
+          const float f = __builtin_amdgcn_exp2f(top[k] - safe);
+          const bool there = p + k * share < pieces;  // not again what stands in for a part behind the last
+          const v4f more = infinities ? rescaled(x[k], f) : x[k] * f;
+          l += there ? sum[k] * f : 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; j++) y[j] += there ? more[j] : 0.f;
+        }
       }
-      float most = m;
-#pragma unroll
-      for (int k = 0; k < FLY; k++) most = fmaxf(most, top[k]);
-      const float safe = most == -INFINITY ? 0.f : most, by = __builtin_amdgcn_exp2f(m - safe);
-      y = infinities ? rescaled(y, by) : y * by;
-      l *= by;
-      m = most;
-#pragma unroll
-      for (int k = 0; k < FLY; k++) {
-        const float f = __builtin_amdgcn_exp2f(top[k] - safe);
-        const bool there = p + k * share < pieces;  // not again what stands in for a part behind the last
-        const v4f more = infinities ? rescaled(x[k], f) : x[k] * f;
-        l += there ? sum[k] * f : 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; j++) y[j] += there ? more[j] : 0.f;
-      }
-    }
     };
     add_parts(std::false_type());
     if (has_nan(y)) add_parts(std::true_type());
